@@ -18,7 +18,8 @@
  *    is launched; a call that returns an error has launched nothing.
  *  - Alignment of DEVICE pointers is part of that validation (DYSPEC_BAD_ARG otherwise):
  *    attention tensors, logit tables, row_stats and the tree-attention workspace 16 bytes;
- *    ancestor masks and the builders' workspaces 8 bytes; every other array 4 bytes.
+ *    ancestor masks and the builders' workspaces 8 bytes; every other array 4 bytes.  (The
+ *    calls around a paged cache and dyspec_prompt_attn say their own: they take strided rows.)
  *  - A batch holds n_seq independent sequences packed back to back.  Sequence s owns tree
  *    rows [node_offset[s], node_offset[s+1]) of every per-node array and prefix rows
  *    [kv_offset[s], kv_offset[s] + prefix_len[s]) of k_prefix / v_prefix.  Row 0 of each
@@ -347,6 +348,127 @@ dyspec_status dyspec_verify_bf16(const void* draft_logits, const void* target_lo
                                  int32_t* accepted_nodes, int32_t* n_accepted, int32_t* final_token,
                                  float* min_margin, void* workspace, size_t workspace_bytes,
                                  void* hip_stream);
+
+/* ================================================================================================
+ * The paged cache around a speculative step.  A server keeps the keys and values of all its sequences in
+ * one pool of pages; a step appends its new tokens (a chunk of a prompt, one token, a draft tree), lets
+ * them attend to what the pages hold, and after dyspec_verify keeps the accepted path.
+ *
+ * Here a batch's node_offset counts NEW tokens (0 .. DYSPEC_MAX_CHUNK per sequence; a sequence may have
+ * none) and prefix_len the tokens that the cache holds before them; kv_offset is not read.  New token j of
+ * sequence s has place prefix_len[s] + j, which is row (place % page_size) of page
+ * page_table[s][place / page_size].
+ * ================================================================================================ */
+#define DYSPEC_MAX_CHUNK (1 << 20)          /* new tokens per sequence                                  */
+#define DYSPEC_MAX_CONTEXT (1 << 30)        /* tokens of a sequence, new ones included                  */
+#define DYSPEC_PAGED_COUNTER_BYTES 16384    /* head of a dyspec_paged_attn workspace                    */
+
+/* One layer's pool.  Page p's rows are k + p * page_stride + row * n_kv_heads * head_dim (elements), dense
+ * in the page; pages may lie apart (K and V pages in turns: page_stride of two pages). */
+typedef struct {
+    void* k;                         /* DEVICE [n_pages, page_size, n_kv_heads, head_dim], 16-byte aligned */
+    void* v;                         /* DEVICE, as k                                      */
+    const int32_t* page_table;       /* DEVICE [n_seq, max_pages], rows table_stride apart */
+    int32_t n_pages;                 /* pages of the pool                                 */
+    int32_t page_size;               /* rows of a page: a power of two, 8 .. 65536        */
+    int32_t max_pages;               /* entries of a table row                            */
+    int32_t table_stride;            /* >= max_pages                                      */
+    int64_t page_stride;             /* elements, >= page_size * n_kv_heads * head_dim, a multiple of 16 bytes */
+} dyspec_paged_kv;
+/* Table entries that the places of a sequence reach are page numbers in [0, n_pages); others are not read.
+ * One outside that range is an error of the caller that is kept inside the cache: nothing is written for its
+ * rows, and attention reads some page of the pool in its place.  Sequences may share pages that none of their
+ * new tokens lie in. */
+
+/*
+ * dyspec_kv_append -- the new tokens' keys and values go into the pages, keys and queries rotated by their
+ * position on the way.
+ *
+ * Rotation: token j has position pos = prefix_len[s] + (rel_pos ? rel_pos[j] : j) (a draft tree passes its
+ * depths) and pair i of a head, i < n_freq, is turned by the angle a = pos * inv_freq[i], taken in 64 bits:
+ *   (x, y) -> (x cos a - y sin a, x sin a + y cos a), rounded once.
+ * Pair i is elements (i, i + n_freq) of the head, or (2i, 2i + 1) if interleaved != 0; elements from
+ * 2 * n_freq on, and all of V, are copied.
+ *
+ *   q          DEVICE [sum N, n_q_heads, head_dim], tokens q_stride elements apart, or NULL (n_q_heads 0)
+ *   k, v       DEVICE [sum N, n_kv_heads, head_dim], tokens k_stride / v_stride elements apart
+ *              (slices of one projection's rows can be passed as they are; heads are dense)
+ *   rel_pos    DEVICE [sum N] i32 or NULL
+ *   inv_freq   DEVICE [n_freq] fp32 (NULL if n_freq is 0: nothing is turned)
+ *   n_freq     0 .. head_dim / 2
+ *   q_out      DEVICE [sum N, n_q_heads, head_dim] dense; may be q where that is dense
+ *   k_out      DEVICE [sum N, n_kv_heads, head_dim] dense: the rotated keys once more, or NULL; may be k
+ *              where that is dense
+ *   head_dim   4 .. 256, a multiple of 4;  dtype DYSPEC_F32 or DYSPEC_BF16, of all tensors
+ * q, k, v, q_out and k_out are aligned to their elements; where they, the strides, head_dim and n_freq allow
+ * 16-byte pieces those are used.
+ */
+dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const dyspec_paged_kv* cache,
+                               const dyspec_batch* batch, const int32_t* rel_pos, const float* inv_freq,
+                               int32_t n_freq, int32_t interleaved, int32_t n_q_heads, int32_t n_kv_heads,
+                               int32_t head_dim, int32_t dtype, void* q_out, void* k_out, void* hip_stream);
+
+/*
+ * dyspec_paged_attn -- one layer of attention of the new tokens over the pages that they were appended to:
+ *   out[j,h,:] = softmax_k( scale * <q[j,h,:], K[k, h/G, :]> ) . V[k, h/G, :],  G = n_q_heads / n_kv_heads,
+ * over every key of the context and, of the new tokens, key i if i <= j and (with a mask) bit i of
+ * anc_mask row j is set.  A row that sees no key comes out as zeros.  Keys that a row does not see do not
+ * matter to it, whatever they hold (infinities and NaN among it); rows of the pages behind a sequence's
+ * last token are not read.
+ *
+ *   q, out     DEVICE [sum N, n_q_heads, head_dim] dense, distinct, 16-byte aligned
+ *   anc_mask   NULL: causal.  Else DEVICE [sum N, mask_words] u64 as written by dyspec_build_tree, 8-byte
+ *              aligned, mask_words = max(1, ceil(max_s N_s / 64)), and N <= DYSPEC_MAX_NODES; rows of the
+ *              tree are appended in the order of the mask's rows
+ *   dtype      DYSPEC_F32 or DYSPEC_BF16, head_dim 4 .. 256 in steps of 4 (bf16 with 64 and 128: bf16
+ *              matrix cores, weights rounded to bf16; else fp32 arithmetic throughout)
+ *   workspace  DEVICE, 16-byte aligned, dyspec_paged_attn_workspace_bytes() bytes: parts of walks that are
+ *              shared out over workgroups.  Its first DYSPEC_PAGED_COUNTER_BYTES must be ZERO when a call
+ *              starts and are zero again when it ends (clear it once, after it is allocated); the rest is
+ *              overwritten.  Calls that may overlap need workspaces of their own.  NULL or fewer bytes:
+ *              every walk in one piece (slower; results differ in the rounding of the last bits of fp32).
+ */
+dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
+                                const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads,
+                                int32_t head_dim, int32_t dtype, float softmax_scale, void* out,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                         int32_t head_dim, int32_t dtype);
+
+/*
+ * dyspec_kv_keep -- keeps the accepted path of verified trees: in every layer, the rows of place
+ * prefix_len[s] + accepted_nodes[i] move to place prefix_len[s] + 1 + i, i < n_accepted[s], so that the
+ * root and the path lie end to end and the sequence goes on with prefix_len[s] + 1 + n_accepted[s] tokens.
+ * (A row's position is its depth in the tree, so a rotated key is already what its new place wants.)
+ * Rows from there on, and everything outside the new tokens' places, stay as they are.
+ *
+ *   accepted_nodes  DEVICE [sum N] i32, n_accepted DEVICE [n_seq] i32: as written by dyspec_verify.  Entries
+ *                   are ascending rows of the tree without the root; one that is not behind its new place's
+ *                   predecessor (<= i) or not below N moves nothing
+ *   cache           layer 0; layer l's pages are l * layer_stride elements further (a multiple of 16 bytes)
+ *   n_layers        1 .. 32767
+ */
+dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int64_t layer_stride,
+                             const dyspec_batch* batch, const int32_t* accepted_nodes, const int32_t* n_accepted,
+                             int32_t n_kv_heads, int32_t head_dim, int32_t dtype, void* hip_stream);
+
+/*
+ * dyspec_prompt_attn -- one layer of causal attention of whole prompts to themselves, packed end to end
+ * (what fills the dense prefix of dyspec_tree_attn): row j of a sequence attends to rows 0 .. j of it.
+ * The batch's node_offset packs the prompts; its prefix_len is NULL or zeros.
+ *
+ *   q          DEVICE [sum N, n_q_heads, head_dim], tokens q_stride elements apart
+ *   k, v       DEVICE [sum N, n_kv_heads, head_dim], tokens k_stride / v_stride elements apart
+ *   out        DEVICE [sum N, n_q_heads, head_dim] dense, none of the inputs
+ *   dtype, head_dim, rounding and unseen keys as for dyspec_paged_attn
+ * Strides are multiples of 4 elements, q, k, v and out aligned to 4 elements (slices of one projection's
+ * rows can be passed as they are; 16-byte aligned ones are faster in bf16).
+ */
+dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                 const void* v, int64_t v_stride, const dyspec_batch* batch,
+                                 int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                 float softmax_scale, void* out, void* hip_stream);
 
 /*
  * Measurement helpers (no part of the method): ceilings to set beside the published peaks

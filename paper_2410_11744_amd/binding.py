@@ -6,6 +6,7 @@ CPU fallback: if the library is missing or fails to load, importing callers get 
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -17,11 +18,13 @@ from . import build as _build
 
 F32, BF16, BF16_WAVE = 0, 1, 0x101
 MAX_SEQ, MAX_NODES, MAX_BUILD_NODES, MAX_VOCAB = 64, 2048, 1024, 32768
+PAGED_COUNTER_BYTES = 16384
 WS_BUILD_TREE, WS_TREE_ATTN, WS_VERIFY = 0, 1, 2
 EXPORTS = ("dyspec_init", "dyspec_mask_words", "dyspec_workspace_bytes", "dyspec_status_string",
            "dyspec_build_tree", "dyspec_build_tree_threshold", "dyspec_build_tree_threshold_workspace_bytes",
            "dyspec_dfs_reorder", "dyspec_tree_attn", "dyspec_tree_attn_static_scratch", "dyspec_tree_attn_layers",
            "dyspec_tree_attn_layers_workspace_bytes", "dyspec_verify", "dyspec_verify_bf16",
+           "dyspec_kv_append", "dyspec_kv_keep", "dyspec_paged_attn", "dyspec_paged_attn_workspace_bytes", "dyspec_prompt_attn",
            "dyspec_probe_mfma_bf16", "dyspec_probe_clock", "dyspec_probe_hbm_read")
 
 
@@ -41,6 +44,11 @@ class _Batch(ctypes.Structure):
 class _Tree(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("parent", "token", "sib_rank", "first_child", "next_sibling", "depth")]
+
+
+class _PagedKV(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -94,6 +102,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dyspec_verify_bf16.argtypes = lib.dyspec_verify.argtypes
     lib.dyspec_dfs_reorder.restype = I32
     lib.dyspec_dfs_reorder.argtypes = [PB, PT, PT, V, V, V]
+    I64, PC = ctypes.c_int64, ctypes.POINTER(_PagedKV)
+    lib.dyspec_kv_append.restype = I32
+    lib.dyspec_kv_append.argtypes = [V, I64, V, I64, V, I64, PC, PB, V, V, I32, I32, I32, I32, I32, I32, V, V, V]
+    lib.dyspec_kv_keep.restype = I32
+    lib.dyspec_kv_keep.argtypes = [PC, I32, I64, PB, V, V, I32, I32, I32, V]
+    lib.dyspec_paged_attn.restype = I32
+    lib.dyspec_paged_attn.argtypes = [V, PC, PB, V, I32, I32, I32, I32, F, V, V, SZ, V]
+    lib.dyspec_paged_attn_workspace_bytes.restype = SZ
+    lib.dyspec_paged_attn_workspace_bytes.argtypes = [PB, I32, I32, I32, I32]
+    lib.dyspec_prompt_attn.restype = I32
+    lib.dyspec_prompt_attn.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, V, V]
     lib.dyspec_probe_mfma_bf16.restype = I32
     lib.dyspec_probe_mfma_bf16.argtypes = [I32, I32, ctypes.POINTER(ctypes.c_double), V, V]
     lib.dyspec_probe_clock.restype = I32
@@ -551,6 +570,290 @@ def verify_call(draft_logits, target_logits, batch: Batch, tree: Tree, draft_tem
             _stream(stream))
     keep = (draft_logits, target_logits, batch, tree, cb, ct, da, ta, out)
     return PreparedCall(entry, args, keep, "dyspec_verify_bf16" if bf16 else "dyspec_verify", out)
+
+
+# ---------------------------------------------------------------------------------------- the paged cache and prompts
+
+@dataclass(frozen=True)
+class PagedCache:
+    """A pool of K/V pages and the sequences' page tables (see dyspec_paged_kv in include/dyspec.h).
+
+    k, v        [n_pages, page_size, Hkv, d], or [L, n_pages, page_size, Hkv, d] for all layers of a model; rows dense in a
+                page, pages (and layers) may be strided: halves of one [n_pages, 2, page_size, Hkv, d] pool will do
+    page_table  int32 [n_seq or more, max_pages]; rows may be strided
+
+    kv_append and paged_attn work on one layer (`layer(l)`), kv_keep on all at once."""
+    k: "torch.Tensor"
+    v: "torch.Tensor"
+    page_table: "torch.Tensor"
+
+    def __post_init__(self):
+        k, v, table = self.k, self.v, self.page_table
+        if k.dim() not in (4, 5) or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v need one shape ([layers,] pages, rows, heads, head_dim) and dtype")
+        n_pages, page, Hkv, d = k.shape[-4:]
+        for t in (k, v):
+            if not t.is_cuda:
+                raise ValueError("device tensor required")
+            if (d > 1 and t.stride(-1) != 1) or (Hkv > 1 and t.stride(-2) != d) or (page > 1 and t.stride(-3) != Hkv * d):
+                raise ValueError("a page's rows must be dense")
+        if (n_pages > 1 and k.stride(-4) != v.stride(-4)) or (k.dim() == 5 and k.shape[0] > 1 and k.stride(0) != v.stride(0)):
+            raise ValueError("k and v must share their strides")
+        if table.dim() != 2 or table.dtype is not _dtype("int32") or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("page_table must be an int32 device tensor [n_seq, max_pages]")
+        if v.device != k.device or table.device != k.device:
+            raise ValueError("k, v and page_table must share a device")
+        columns = int(table.shape[1])
+        c = _PagedKV(k.data_ptr(), v.data_ptr(), table.data_ptr(), int(n_pages), int(page), columns,
+                     int(table.stride(0)) if table.shape[0] > 1 else columns, int(k.stride(-4)) if n_pages > 1 else int(page * Hkv * d))
+        object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_ref", ctypes.byref(c))
+        object.__setattr__(self, "_heads", (int(Hkv), int(d)))
+        object.__setattr__(self, "_dtype", _code(k.dtype))
+
+    @property
+    def n_layers(self) -> int:
+        return int(self.k.shape[0]) if self.k.dim() == 5 else 1
+
+    def layer(self, index: int) -> "PagedCache":
+        return PagedCache(self.k[index], self.v[index], self.page_table)
+
+
+def _code(dtype) -> int:
+    code = {_dtype("float32"): F32, _dtype("bfloat16"): BF16}.get(dtype)
+    if code is None:
+        raise ValueError(f"float32 or bfloat16 expected, got {dtype}")
+    return code
+
+
+class DeviceCall(PreparedCall):
+    """A PreparedCall that is issued on its tensors' device whichever device is current."""
+    __slots__ = ("_device",)
+
+    def __init__(self, fn, args, keep, where, out, device):
+        super().__init__(fn, args, keep, where, out)
+        self._device = device
+
+    def __call__(self):
+        if _torch.cuda.current_device() == self._device:
+            return super().__call__()
+        with _torch.cuda.device(self._device):
+            return super().__call__()
+
+
+def _token_rows(t, shape, dtype, device, what: str) -> int:
+    """Elements between the tokens of t [tokens, heads, d], heads dense."""
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{what}: {tuple(shape)} of {dtype} on {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    n, heads, d = shape
+    s = t.stride()
+    if (d > 1 and s[2] != 1) or (heads > 1 and s[1] != d):
+        raise ValueError(f"{what}: a token's heads must be dense")
+    return s[0] if n > 1 else heads * d
+
+
+def _dense(t, shape, dtype, device, what: str) -> int:
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} on {device} expected")
+    return t.data_ptr()
+
+
+_on_stream = contextlib.nullcontext()
+
+
+def _stream_of(stream, device):
+    """(raw handle, context in which memory belongs to that stream) of the given stream or the device's current one."""
+    torch = _torch
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index), _on_stream
+    if stream.device != device:
+        raise ValueError("the stream is another device's")
+    return int(stream.cuda_stream), torch.cuda.stream(stream)
+
+
+def _hand_over(stream, *tensors) -> None:
+    """Memory that was given out for other streams is not to be reused while this one reads it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+_attend_scratch: dict = {}
+
+
+def _attend_workspace(device, raw: int, where, nbytes: int, prepared: bool):
+    """A paged_attn workspace, its head zero.  Calls of one stream run in order and share one; a prepared call, and a call that a
+    graph records, has its own, because whatever runs beside the graph may use the stream's."""
+    torch = _torch
+    with where:
+        capturing = torch.cuda.is_current_stream_capturing()
+        if prepared and capturing:
+            raise ValueError("prepare the call before the graph is recorded: its workspace has to be cleared first")
+        if not prepared and not capturing:
+            buf = _attend_scratch.get((device.index, raw))
+            if buf is not None and buf.numel() >= nbytes:
+                return buf
+        buf = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        if not prepared and not capturing:
+            _attend_scratch[(device.index, raw)] = buf
+        return buf
+
+
+def kv_append(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
+              out=None, k_out=None, stream=None):
+    """dyspec_kv_append: the new tokens' keys (rotated) and values go into their places in the pages; returns the rotated
+    queries (None without q).  k, v [sum N, Hkv, d] and q [sum N, Hq, d] may be slices of one projection's rows.
+    rel_pos: int32 positions relative to each sequence's context (a tree's depths), by default 0, 1, ...; inv_freq: fp32 [n],
+    the frequencies of the first n pairs of a head (None: nothing is rotated); out: the queries' place (may be q, where that is
+    dense); k_out: the rotated keys as dense rows as well."""
+    return kv_append_call(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_out, stream)()
+
+
+def kv_append_call(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
+                   out=None, k_out=None, stream=None) -> PreparedCall:
+    """kv_append's call, prepared: nothing is launched until the returned object is called."""
+    lib = _lib or load_library()
+    torch, total = _torch, batch.total_nodes
+    kc, (Hkv, d) = cache.k, cache._heads
+    device, dtype = kc.device, kc.dtype
+    if kc.dim() != 4 or cache.page_table.shape[0] < batch.n_seq:
+        raise ValueError("kv_append takes one layer's cache, with a table row per sequence")
+    shape = (total, Hkv, d)
+    ks, vs = _token_rows(k, shape, dtype, device, "k"), _token_rows(v, shape, dtype, device, "v")
+    raw, where = _stream_of(stream, device)
+    qp = qs = op = Hq = 0
+    if q is not None:
+        Hq = int(q.shape[1])
+        qs, qp = _token_rows(q, (total, Hq, d), dtype, device, "q"), q.data_ptr()
+        if out is None:
+            with where:
+                out = torch.empty((total, Hq, d), dtype=dtype, device=device)
+        op = _dense(out, (total, Hq, d), dtype, device, "out")
+    elif out is not None:
+        raise ValueError("out is the queries' place: q is missing")
+    kp = 0 if k_out is None else _dense(k_out, shape, dtype, device, "k_out")
+    rp = 0 if rel_pos is None else _dense(rel_pos, (total,), torch.int32, device, "rel_pos")
+    n_freq = fp = 0
+    if inv_freq is not None:
+        n_freq = inv_freq.numel()
+        fp = _dense(inv_freq, (n_freq,), torch.float32, device, "inv_freq")
+    if total == 0:
+        return _Nothing(out)
+    _hand_over(stream, q, k, v, out, k_out, rel_pos, inv_freq, kc, cache.v, cache.page_table)
+    cb = batch._c()
+    args = (qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, cache._ref, ctypes.byref(cb), rp, fp, n_freq, 1 if interleaved else 0,
+            Hq, Hkv, d, cache._dtype, op, kp, raw)
+    return DeviceCall(lib.dyspec_kv_append, args, (q, k, v, cache, cb, batch, rel_pos, inv_freq, out, k_out), "dyspec_kv_append", out,
+                      device.index)
+
+
+class _Nothing(PreparedCall):
+    """The call of a batch without a token: empty tensors have no address to hand over."""
+    __slots__ = ()
+
+    def __init__(self, out):
+        super().__init__(None, (), (), "", out)
+
+    def __call__(self):
+        return self.out
+
+
+def kv_keep(cache: PagedCache, batch: Batch, accepted_nodes, n_accepted, stream=None) -> None:
+    """dyspec_kv_keep: after verify, the accepted path's rows move up behind the root's, in every layer of the cache.
+    `batch` describes the trees as they were appended; accepted_nodes and n_accepted are verify's."""
+    lib = _lib or load_library()
+    torch, total = _torch, batch.total_nodes
+    k = cache.k
+    device, (Hkv, d) = k.device, cache._heads
+    if cache.page_table.shape[0] < batch.n_seq:
+        raise ValueError("a table row per sequence is needed")
+    ap = _dense(accepted_nodes, (total,), torch.int32, device, "accepted_nodes")
+    np_ = _dense(n_accepted, (batch.n_seq,), torch.int32, device, "n_accepted")
+    if total == 0:
+        return
+    raw, _ = _stream_of(stream, device)
+    _hand_over(stream, accepted_nodes, n_accepted, k, cache.v, cache.page_table)
+    cb = batch._c()
+    layers = cache.n_layers
+    DeviceCall(lib.dyspec_kv_keep, (cache._ref, layers, int(k.stride(0)) if layers > 1 else 0, ctypes.byref(cb), ap, np_, Hkv, d, cache._dtype, raw),
+               (), "dyspec_kv_keep", None, device.index)()
+
+
+def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None):
+    """dyspec_paged_attn: the new tokens (appended before) attend to the pages: to their context and, causally or by an ancestor
+    mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d]."""
+    return _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, False)()
+
+
+def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None) -> PreparedCall:
+    """paged_attn's call, prepared: nothing is launched until the returned object is called.  It has a workspace of its own."""
+    return _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, True)
+
+
+def _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared) -> PreparedCall:
+    lib = _lib or load_library()
+    torch = _torch
+    kc, (Hkv, d), code = cache.k, cache._heads, cache._dtype
+    device, dtype = kc.device, kc.dtype
+    memo = batch._memo()
+    total, Hq = int(batch.node_offset[-1]), int(q.shape[1])
+    if kc.dim() != 4 or cache.page_table.shape[0] < batch.n_seq:
+        raise ValueError("paged_attn takes one layer's cache, with a table row per sequence")
+    qp = _dense(q, (total, Hq, d), dtype, device, "q")
+    mp = 0
+    if anc_mask is not None:
+        words = memo.get("chunk_words")
+        if words is None:
+            words = memo["chunk_words"] = max(1, -(-int(np.diff(batch.node_offset).max()) // 64))
+        mp = _dense(anc_mask, (total, words), torch.int64, device, "anc_mask")
+    raw, where = _stream_of(stream, device)
+    if out is None:
+        with where:
+            out = torch.empty_like(q)
+    op = _dense(out, q.shape, dtype, device, "out")
+    if total == 0:
+        return _Nothing(out)
+    cb = batch._c(memo)
+    ref = ctypes.byref(cb)
+    key = ("ws_paged", Hq, Hkv, d, code)
+    nbytes = memo.get(key)
+    if nbytes is None:
+        nbytes = memo[key] = int(lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code))
+    ws = _attend_workspace(device, raw, where, nbytes, prepared) if nbytes else None
+    _hand_over(stream, q, out, anc_mask, kc, cache.v, cache.page_table)
+    args = (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, op, ws.data_ptr() if nbytes else 0, nbytes, raw)
+    return DeviceCall(lib.dyspec_paged_attn, args, (q, cache, cb, batch, anc_mask, out, ws), "dyspec_paged_attn", out, device.index)
+
+
+def prompt_attn(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None):
+    """dyspec_prompt_attn: packed prompts attend to themselves, causally.  q [sum N, Hq, d], k, v [sum N, Hkv, d], which may be
+    slices of one projection's rows; the batch's n_nodes are the prompts' lengths, its prefix_len zeros."""
+    return prompt_attn_call(q, k, v, batch, softmax_scale, out, stream)()
+
+
+def prompt_attn_call(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None) -> PreparedCall:
+    """prompt_attn's call, prepared: nothing is launched until the returned object is called."""
+    lib = _lib or load_library()
+    torch, total = _torch, batch.total_nodes
+    device, dtype = q.device, q.dtype
+    if not q.is_cuda:
+        raise ValueError("device tensor required")
+    code, (Hq, d), Hkv = _code(dtype), q.shape[1:], int(k.shape[1])
+    Hq, d = int(Hq), int(d)
+    qs = _token_rows(q, (total, Hq, d), dtype, device, "q")
+    ks, vs = _token_rows(k, (total, Hkv, d), dtype, device, "k"), _token_rows(v, (total, Hkv, d), dtype, device, "v")
+    raw, where = _stream_of(stream, device)
+    if out is None:
+        with where:
+            out = torch.empty((total, Hq, d), dtype=dtype, device=device)
+    op = _dense(out, (total, Hq, d), dtype, device, "out")
+    if total == 0:
+        return _Nothing(out)
+    _hand_over(stream, q, k, v, out)
+    cb = batch._c()
+    args = (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ctypes.byref(cb), Hq, Hkv, d, code, softmax_scale, op, raw)
+    return DeviceCall(lib.dyspec_prompt_attn, args, (q, k, v, cb, batch, out), "dyspec_prompt_attn", out, device.index)
 
 
 def probe_mfma_bf16(iterations: int, sink, stream=None, random_operands: bool = False) -> float:

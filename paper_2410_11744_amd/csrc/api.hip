@@ -2,7 +2,8 @@
 // for the contract of every entry point.
 #include <atomic>
 
-#include "dyspec_device.h"
+#include "attend.h"
+#include "kv_cache.h"
 
 namespace dyspec {
 
@@ -124,7 +125,7 @@ dyspec_status dyspec_init(void)
 {
     void* scratch_address = nullptr;
     if (prepare_tree_attn() != hipSuccess || prepare_build_tree() != hipSuccess || prepare_build_threshold() != hipSuccess || prepare_verify() != hipSuccess ||
-        prepare_reorder() != hipSuccess ||
+        prepare_reorder() != hipSuccess || prepare_attend() != hipSuccess ||
         static_scratch_address(&scratch_address) != hipSuccess)
         return DYSPEC_HIP_ERROR;
     return DYSPEC_OK;
@@ -415,6 +416,189 @@ dyspec_status dyspec_verify_bf16(const void* draft_logits, const void* target_lo
 {
     return verify_common(draft_logits, target_logits, true, vocab, batch, tree, draft_temp, target_temp, seed, emit_bonus,
                          row_stats, accept_ratio, accepted_nodes, n_accepted, final_token, min_margin, hip_stream);
+}
+
+// ---- the paged cache and prompts
+
+// New tokens and context of every sequence (a batch whose sequences may have no new tokens).
+static dyspec_status check_chunks(const dyspec_batch* b, bool context, int max_new, AttendBatch* ab)
+{
+    if (!b || !b->node_offset || (context && !b->prefix_len)) return DYSPEC_BAD_ARG;
+    if (b->n_seq < 1 || b->n_seq > DYSPEC_MAX_SEQ || b->node_offset[0] != 0) return DYSPEC_BAD_SHAPE;
+    ab->n_seq = b->n_seq;
+    for (int s = 0; s < b->n_seq; ++s) {
+        const long long n = (long long)b->node_offset[s + 1] - b->node_offset[s];
+        const long long c = b->prefix_len ? b->prefix_len[s] : 0;
+        if (n < 0 || n > max_new || c < 0 || c + n > DYSPEC_MAX_CONTEXT || (!context && c != 0)) return DYSPEC_BAD_SHAPE;
+        ab->row0[s] = b->node_offset[s];
+        ab->context[s] = (int)c;
+    }
+    ab->row0[b->n_seq] = b->node_offset[b->n_seq];
+    return DYSPEC_OK;
+}
+
+static dyspec_status check_heads(int Hq, int Hkv, int d, int dtype)
+{
+    if (Hkv < 1 || Hq < 0 || Hq % Hkv != 0) return DYSPEC_BAD_SHAPE;
+    if ((dtype != DYSPEC_F32 && dtype != DYSPEC_BF16) || d < 4 || d > 256 || d % 4) return DYSPEC_UNSUPPORTED;
+    // a token's heads stay below 4 MB: eight rows of a page are addressed with 32-bit offsets
+    if ((long long)max(Hq, Hkv) * d > 1 << 20) return DYSPEC_BAD_SHAPE;
+    return DYSPEC_OK;
+}
+
+// Rows are numbered in 32 bits and divided by G with one multiplication, exact for rows * G up to 2^32.
+static bool rows_ok(const AttendBatch& b, int Hq, int G)
+{
+    int most = 0;
+    for (int s = 0; s < b.n_seq; ++s) most = max(most, b.row0[s + 1] - b.row0[s]);
+    return (long long)most * G * G <= 0xffffffffLL && (long long)b.row0[b.n_seq] * Hq <= 1LL << 34;
+}
+
+static int log2_of(int x) { int s = 0; while ((1 << s) < x) ++s; return s; }
+
+static dyspec_status check_cache(const dyspec_paged_kv* c, const AttendBatch& b, int Hkv, int d, int dtype)
+{
+    if (!c || !c->k || !c->v || !c->page_table) return DYSPEC_BAD_ARG;
+    if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->page_table, 4)) return DYSPEC_BAD_ARG;
+    if (c->page_size < 8 || c->page_size > 65536 || (c->page_size & (c->page_size - 1))) return DYSPEC_UNSUPPORTED;
+    if (c->n_pages < 1 || c->max_pages < 0 || c->table_stride < c->max_pages) return DYSPEC_BAD_SHAPE;
+    const int elt = dtype == DYSPEC_F32 ? 4 : 2;
+    if (c->page_stride < (int64_t)c->page_size * Hkv * d || c->page_stride > INT64_MAX / 4 || (c->page_stride * elt) % 16) return DYSPEC_BAD_SHAPE;
+    for (int s = 0; s < b.n_seq; ++s) {
+        const int n = b.row0[s + 1] - b.row0[s];
+        if (n > 0 && ((long long)b.context[s] + n + c->page_size - 1) / c->page_size > c->max_pages) return DYSPEC_BAD_SHAPE;
+    }
+    return DYSPEC_OK;
+}
+
+static AttendArgs attend_args(int Hq, int Hkv, int d, float scale)
+{
+    AttendArgs a;
+    a.table = nullptr; a.mask = nullptr; a.part = nullptr; a.counters = nullptr;
+    a.page_bytes = 0; a.table_stride = 0; a.page_shift = 0; a.n_pages = 0; a.mask_words = 0;
+    a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.d = d;
+    a.g_magic = a.G == 1 ? 0u : (uint32_t)((0xffffffffull + a.G) / a.G);
+    a.c2 = scale * 1.4426950408889634f;
+    return a;
+}
+
+static bool scale_ok(float x) { return x > 0.0f && x <= 3.4e38f; }
+
+dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               const dyspec_paged_kv* cache, const dyspec_batch* batch, const int32_t* rel_pos, const float* inv_freq,
+                               int32_t n_freq, int32_t interleaved, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                               int32_t dtype, void* q_out, void* k_out, void* hip_stream)
+{
+    AttendBatch b;
+    dyspec_status st = check_chunks(batch, true, DYSPEC_MAX_CHUNK, &b);
+    if (st == DYSPEC_OK) st = check_heads(n_kv_heads > 0 ? (n_q_heads + n_kv_heads - 1) / n_kv_heads * n_kv_heads : 1, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK) st = check_cache(cache, b, n_kv_heads, head_dim, dtype);
+    if (st != DYSPEC_OK) return st;
+    if (!k || !v || n_q_heads < 0 || (n_q_heads > 0) != (q != nullptr) || (q && !q_out)) return DYSPEC_BAD_ARG;
+    if (n_freq < 0 || n_freq > head_dim / 2) return DYSPEC_BAD_SHAPE;
+    if (n_freq > 0 && !inv_freq) return DYSPEC_BAD_ARG;
+    const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim, most = (int64_t)1 << 40;
+    if ((q && (q_stride < q_row || q_stride > most)) || k_stride < kv_row || v_stride < kv_row || k_stride > most || v_stride > most) return DYSPEC_BAD_SHAPE;
+    const int elt = dtype == DYSPEC_F32 ? 4 : 2;
+    if (!aligned(q, elt) || !aligned(k, elt) || !aligned(v, elt) || !aligned(q_out, elt) || !aligned(k_out, elt) || !aligned(rel_pos, 4) || !aligned(inv_freq, 4))
+        return DYSPEC_BAD_ARG;
+    if ((q && q == q_out && q_stride != q_row) || (k == k_out && k_stride != kv_row)) return DYSPEC_BAD_ARG;      // in place: dense only
+    AppendArgs a;
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_out = k_out; a.k_pages = cache->k; a.v_pages = cache->v;
+    a.table = cache->page_table; a.rel_pos = rel_pos; a.inv_freq = inv_freq;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.page_stride = cache->page_stride;
+    a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
+    a.Hq = q ? n_q_heads : 0; a.Hkv = n_kv_heads; a.d = head_dim; a.half = n_freq; a.interleaved = interleaved != 0;
+    a.total = b.row0[b.n_seq]; a.tokens = 1; a.n_seq = b.n_seq;
+    for (int s = 0; s < b.n_seq; ++s) { a.row0[s] = b.row0[s]; a.context[s] = b.context[s]; }
+    a.row0[b.n_seq] = b.row0[b.n_seq];
+    const int vec = 16 / elt;
+    const bool wide = head_dim % vec == 0 && n_freq % vec == 0 && aligned(k, 16) && aligned(v, 16) && aligned(k_out, 16) && k_stride % vec == 0 &&
+                      v_stride % vec == 0 && (!q || (aligned(q, 16) && aligned(q_out, 16) && q_stride % vec == 0));
+    return launch_kv_append(a, dtype, wide, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+}
+
+dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int64_t layer_stride, const dyspec_batch* batch,
+                             const int32_t* accepted_nodes, const int32_t* n_accepted, int32_t n_kv_heads, int32_t head_dim,
+                             int32_t dtype, void* hip_stream)
+{
+    AttendBatch b;
+    dyspec_status st = check_chunks(batch, true, DYSPEC_MAX_CHUNK, &b);
+    if (st == DYSPEC_OK) st = check_heads(n_kv_heads, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK) st = check_cache(cache, b, n_kv_heads, head_dim, dtype);
+    if (st != DYSPEC_OK) return st;
+    if (!accepted_nodes || !n_accepted || !aligned(accepted_nodes, 4) || !aligned(n_accepted, 4)) return DYSPEC_BAD_ARG;
+    const int elt = dtype == DYSPEC_F32 ? 4 : 2;
+    if (n_layers < 1 || n_layers > 32767 || layer_stride < 0 || layer_stride > ((int64_t)1 << 44) || (layer_stride * elt) % 16) return DYSPEC_BAD_SHAPE;
+    KeepArgs a;
+    a.k_pages = static_cast<char*>(cache->k); a.v_pages = static_cast<char*>(cache->v);
+    a.table = cache->page_table; a.accepted = accepted_nodes; a.n_accepted = n_accepted;
+    a.layer_bytes = layer_stride * elt; a.page_bytes = cache->page_stride * elt; a.row_bytes = (long long)n_kv_heads * head_dim * elt;
+    a.piece_bytes = a.row_bytes % 16 ? 8 : 16;
+    a.row_pieces = (int)(a.row_bytes / a.piece_bytes);
+    a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
+    a.n_seq = b.n_seq;
+    for (int s = 0; s < b.n_seq; ++s) { a.row0[s] = b.row0[s]; a.context[s] = b.context[s]; }
+    a.row0[b.n_seq] = b.row0[b.n_seq];
+    return launch_kv_keep(a, n_layers, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+}
+
+size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype)
+{
+    AttendBatch b;
+    if (check_chunks(batch, true, DYSPEC_MAX_CHUNK, &b) != DYSPEC_OK || n_q_heads < 1 || check_heads(n_q_heads, n_kv_heads, head_dim, dtype) != DYSPEC_OK) return 0;
+    return attend_workspace_bytes(b, dtype, n_q_heads, n_kv_heads, head_dim);
+}
+
+dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch, const uint64_t* anc_mask,
+                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, float softmax_scale,
+                                void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    AttendBatch b;
+    dyspec_status st = check_chunks(batch, true, anc_mask ? DYSPEC_MAX_NODES : DYSPEC_MAX_CHUNK, &b);
+    if (st == DYSPEC_OK) st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK && (n_q_heads < 1 || !rows_ok(b, n_q_heads, n_q_heads / n_kv_heads))) st = DYSPEC_BAD_SHAPE;
+    if (st == DYSPEC_OK) st = check_cache(cache, b, n_kv_heads, head_dim, dtype);
+    if (st != DYSPEC_OK) return st;
+    if (!q || !out || q == out || !scale_ok(softmax_scale)) return DYSPEC_BAD_ARG;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(anc_mask, 8) || !aligned(workspace, 16)) return DYSPEC_BAD_ARG;
+    const long long elt = dtype == DYSPEC_F32 ? 4 : 2;
+    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim, softmax_scale);
+    a.q = static_cast<const char*>(q); a.out = static_cast<char*>(out);
+    a.k = static_cast<const char*>(cache->k); a.v = static_cast<const char*>(cache->v);
+    a.table = cache->page_table; a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
+    a.page_bytes = cache->page_stride * elt;
+    a.q_stride = a.out_stride = (long long)n_q_heads * head_dim * elt;
+    a.k_stride = a.v_stride = (long long)n_kv_heads * head_dim * elt;
+    if (anc_mask) {
+        int most = 1;
+        for (int s = 0; s < b.n_seq; ++s) most = max(most, b.row0[s + 1] - b.row0[s]);
+        a.mask = reinterpret_cast<const uint32_t*>(anc_mask);
+        a.mask_words = 2 * ((most + 63) / 64);
+    }
+    return launch_attend(a, b, dtype, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess
+               ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+}
+
+dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                 const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                 float softmax_scale, void* out, void* hip_stream)
+{
+    AttendBatch b;
+    dyspec_status st = check_chunks(batch, false, DYSPEC_MAX_CHUNK, &b);
+    if (st == DYSPEC_OK) st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK && (n_q_heads < 1 || !rows_ok(b, n_q_heads, n_q_heads / n_kv_heads))) st = DYSPEC_BAD_SHAPE;
+    if (st != DYSPEC_OK) return st;
+    if (!q || !k || !v || !out || out == q || out == k || out == v || !scale_ok(softmax_scale)) return DYSPEC_BAD_ARG;
+    const long long elt = dtype == DYSPEC_F32 ? 4 : 2;
+    const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim, most = (int64_t)1 << 24;
+    if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride > most || k_stride > most || v_stride > most) return DYSPEC_BAD_SHAPE;
+    const size_t four = 4 * elt;
+    if (q_stride % 4 || k_stride % 4 || v_stride % 4 || !aligned(q, four) || !aligned(k, four) || !aligned(v, four) || !aligned(out, four)) return DYSPEC_BAD_ARG;
+    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim, softmax_scale);
+    a.q = static_cast<const char*>(q); a.k = static_cast<const char*>(k); a.v = static_cast<const char*>(v); a.out = static_cast<char*>(out);
+    a.q_stride = q_stride * elt; a.k_stride = k_stride * elt; a.v_stride = v_stride * elt; a.out_stride = q_row * elt;
+    return launch_attend(a, b, dtype, nullptr, 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
 }  // extern "C"

@@ -1,0 +1,35 @@
+// Arguments and launchers of the paged cache's calls (kv_cache.hip).
+#pragma once
+#include "dyspec_device.h"
+
+namespace dyspec {
+
+constexpr int kAppendTokens = 4;                 // tokens of a workgroup at most
+
+struct AppendArgs {
+    const void *q, *k, *v;
+    void *q_out, *k_out, *k_pages, *v_pages;     // k_out: nullptr or the rotated keys as dense rows
+    const int *table, *rel_pos;
+    const float* inv_freq;
+    long long q_stride, k_stride, v_stride, page_stride;         // elements
+    int table_stride, page_shift, n_pages;
+    int Hq, Hkv, d, half, interleaved;           // Hq 0: no queries
+    int total, tokens;                           // tokens of the call, of a workgroup
+    int n_seq;
+    int row0[DYSPEC_MAX_SEQ + 1], context[DYSPEC_MAX_SEQ];
+};
+// `wide`: rows, strides and dims allow 16-byte pieces
+hipError_t launch_kv_append(AppendArgs a, int dtype, bool wide, hipStream_t stream);
+
+struct KeepArgs {
+    char *k_pages, *v_pages;
+    const int *table, *accepted, *n_accepted;
+    long long layer_bytes, page_bytes, row_bytes;
+    int row_pieces, piece_bytes;                 // a row in pieces of 16 or 8 bytes
+    int table_stride, page_shift, n_pages;
+    int n_seq;
+    int row0[DYSPEC_MAX_SEQ + 1], context[DYSPEC_MAX_SEQ];
+};
+hipError_t launch_kv_keep(const KeepArgs& a, int n_layers, hipStream_t stream);
+
+}  // namespace dyspec
