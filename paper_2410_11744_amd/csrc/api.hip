@@ -591,7 +591,7 @@ dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k,
     if (st != DYSPEC_OK) return st;
     if (!q || !k || !v || !out || out == q || out == k || out == v || !scale_ok(softmax_scale)) return DYSPEC_BAD_ARG;
     const long long elt = dtype == DYSPEC_F32 ? 4 : 2;
-    const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim, most = (int64_t)1 << 24;
+    const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim, most = (int64_t)1 << 22;
     if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride > most || k_stride > most || v_stride > most) return DYSPEC_BAD_SHAPE;
     const size_t four = 4 * elt;
     if (q_stride % 4 || k_stride % 4 || v_stride % 4 || !aligned(q, four) || !aligned(k, four) || !aligned(v, four) || !aligned(out, four)) return DYSPEC_BAD_ARG;

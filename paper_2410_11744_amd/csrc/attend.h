@@ -23,6 +23,7 @@ struct AttendSeq {
     int N, C;         // new tokens, tokens before them
     int parts;        // items per row block
     int share;        // keys per part, a multiple of the kernel's step
+    int slot0;        // parts > 1: first item's place among the slots
 };
 
 struct AttendArgs {
@@ -30,7 +31,7 @@ struct AttendArgs {
     char* out;
     const int* table;              // nullptr: k and v are rows of tokens like q
     const uint32_t* mask;          // nullptr: causal
-    float* part;                   // [items * Hkv][R * (d + 2)]: rows times their weight, then (max, sum) per row
+    float* part;                   // [slots * Hkv][R * (d + 2)]: rows times their weight, then (max, sum) per row
     unsigned* counters;            // [row blocks * Hkv], zero between launches
     long long q_stride, out_stride, k_stride, v_stride;      // bytes between tokens (in a page: between its rows)
     long long page_bytes;          // between pages
@@ -43,8 +44,15 @@ struct AttendArgs {
     AttendSeq seq[DYSPEC_MAX_SEQ];
 };
 
+// The arguments where they are: read from the kernel's argument segment, whose first parameter they have to be.  (Taken as a
+// by-value parameter, the table of sequences, indexed at run time, would be copied to scratch memory by every lane.)
+__device__ __forceinline__ const AttendArgs& attend_args_here()
+{
+    return *(const AttendArgs*)(__attribute__((address_space(4))) const AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+}
+
 // A workgroup's place: block of rows, part of the walk.
-struct AttendItem { AttendSeq s; int kvh, block, part; };
+struct AttendItem { AttendSeq s; int kvh, block, part, local; };      // local: the item's number in its sequence
 
 typedef __attribute__((address_space(4))) const int* scalar_ints;
 
@@ -60,6 +68,7 @@ __device__ __forceinline__ AttendItem attend_item(const AttendArgs& a, int index
         it.s = a.seq[__builtin_popcountll(__builtin_amdgcn_ballot_w64(item >= at)) - 1];
     }
     const int local = item - it.s.item0;
+    it.local = local;
     const int blocks = (a.G * it.s.N + rows_per_block - 1) / rows_per_block;
     const int lb = it.s.parts > 1 ? local / it.s.parts : local;
     it.part = local - lb * it.s.parts;
@@ -71,32 +80,38 @@ __device__ __forceinline__ int div_G(const AttendArgs& a, int r) { return a.g_ma
 
 // Byte offset of key `key` (uniform over the wave) from the pool's or the packed rows' start.  A page number outside the pool
 // reads its last page: a wrong result, but no access outside the cache.
+template <bool Paged>
 __device__ __forceinline__ long long key_offset(const AttendArgs& a, const AttendSeq& s, int key, long long stride)
 {
-    if (a.table) {
+    if constexpr (Paged) {
         const unsigned p = (unsigned)((scalar_ints)(a.table + (long long)s.id * a.table_stride))[key >> a.page_shift];
         return (long long)min(p, (unsigned)a.n_pages - 1u) * a.page_bytes + (long long)(key & ((1 << a.page_shift) - 1)) * stride;
     }
     return (long long)(s.row0 + key) * stride;
 }
+__device__ __forceinline__ long long key_offset(const AttendArgs& a, const AttendSeq& s, int key, long long stride)
+{
+    return a.table ? key_offset<true>(a, s, key, stride) : key_offset<false>(a, s, key, stride);
+}
 
+// 32-bit word q of row j's mask, numbered from the first new token; words before it are the context's, which every row sees.
+__device__ __forceinline__ uint32_t mask_word(const AttendArgs& a, const AttendSeq& s, int j, int q)
+{
+    return q < 0 ? ~0u : q < a.mask_words ? a.mask[(long long)(s.row0 + j) * a.mask_words + q] : 0u;
+}
+// Bit b: key k0 + b is not behind row j's own.
+__device__ __forceinline__ uint32_t causal_bits(const AttendSeq& s, int j, int k0)
+{
+    const int upto = s.C + j + 1 - k0;
+    return upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
+}
 // Bit b: row j of the new tokens sees key k0 + b.
 __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const AttendSeq& s, int j, int k0)
 {
-    const int upto = s.C + j + 1 - k0;                     // keys up to the row's own
-    uint32_t w = upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
-    const int i0 = k0 - s.C;                               // key k0 + b is new token i0 + b
-    if (a.mask && i0 > -32) {
-        const uint32_t* const row = a.mask + (long long)(s.row0 + j) * a.mask_words;
-        uint32_t m;
-        if (i0 < 0) {
-            m = (row[0] << -i0) | ((1u << -i0) - 1u);
-        } else {
-            const int q = i0 >> 5, r = i0 & 31;
-            const uint32_t lo = q < a.mask_words ? row[q] : 0u, hi = q + 1 < a.mask_words ? row[q + 1] : 0u;
-            m = __builtin_amdgcn_alignbit(hi, lo, r);
-        }
-        w &= m;
+    uint32_t w = causal_bits(s, j, k0);
+    if (a.mask) {
+        const int i0 = k0 - s.C;                           // key k0 + b is new token i0 + b
+        w &= __builtin_amdgcn_alignbit(mask_word(a, s, j, (i0 >> 5) + 1), mask_word(a, s, j, i0 >> 5), (uint32_t)i0 & 31u);
     }
     return w;
 }
@@ -134,20 +149,19 @@ __device__ __forceinline__ char* out_row(const AttendArgs& a, const AttendSeq& s
 //
 // A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
 // matrix product.  Such keys may hold anything (a later token that overflowed), so a row that comes out with a NaN is done again
-// by this: keys one at a time, those the row does not see left out.  One wave, lane i holds dims 4i..; a NaN of the row's own
-// keys comes out as one again.
+// by this: keys one at a time, those the row does not see left out, weights against the reference m that the row has.  One wave,
+// lane i holds dims 4i..; a NaN of the row's own keys comes out as one again.
 template <typename T>
-__device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& s, int kvh, int r, int k_begin, int k_end, float4& o, float& m, float& l)
+__device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& s, int kvh, int r, int k_begin, int k_end, float m, float4& o, float& l)
 {
     typedef typename Four<T>::raw raw;
     const int lane = threadIdx.x & 63;
     const bool mine = 4 * lane < a.d;
     const int piece = mine ? lane : 0;
     const int j = div_G(a, r), h = kvh * a.G + (r - j * a.G);
-    const float zero = 0.0f;
-    float4 q = Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * (int)sizeof(T)));
-    o = make_float4(zero, zero, zero, zero);
-    m = kLowest; l = 0.0f;
+    const float4 q = Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * (int)sizeof(T)));
+    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    l = 0.0f;
     const long long head = (long long)kvh * a.d * (int)sizeof(T);
 #pragma unroll 1
     for (int key = k_begin; key < k_end; ++key) {
@@ -155,11 +169,9 @@ __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& 
         const float4 k = Four<T>::wide(*reinterpret_cast<const raw*>(a.k + key_offset(a, s, key, a.k_stride) + head + 4 * piece * (int)sizeof(T)));
         const float4 v = Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head + 4 * piece * (int)sizeof(T)));
         const float dot = wave_sum(mine ? (q.x * k.x + q.y * k.y) + (q.z * k.z + q.w * k.w) : 0.0f);
-        const float up = fmaxf(m, dot);
-        const float f = exp2f((m - up) * a.c2), p = exp2f((dot - up) * a.c2);
-        m = up;
-        l = l * f + p;
-        o.x = o.x * f + p * v.x; o.y = o.y * f + p * v.y; o.z = o.z * f + p * v.z; o.w = o.w * f + p * v.w;
+        const float p = exp2f((dot - m) * a.c2);
+        l += p;
+        o.x += p * v.x; o.y += p * v.y; o.z += p * v.z; o.w += p * v.w;
     }
 }
 
@@ -168,7 +180,15 @@ __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& 
 // A walk cut into parts: every workgroup leaves its rows (times their weight, fp32: nothing is rounded twice) with their (max,
 // sum) in its slot and arrives at its row block's counter; the one that arrives last sums the slots in the order of the keys
 // and writes the rows.  The counter wraps to zero with the last arrival.  Slots go through device-scope accesses: they reach the
-// level of memory that all XCDs share without a write-back of whole caches.
+// level of memory that all XCDs share without a write-back of whole caches.  A slot holds the rows in the order in which the
+// kernel's lanes have them, four dims to a lane, so that each store of a wave is one run of a kilobyte.
+__device__ __forceinline__ void store_four(float* p, float x, float y, float z, float w)
+{
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    const f4 v = { x, y, z, w };
+    // (arrive_last waits for it; the wait states keep the next instruction from overwriting the data while they are read)
+    asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 3" :: "v"(p), "v"(v) : "memory");
+}
 __device__ __forceinline__ void store_pair(float* p, float x, float y)
 {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), ((unsigned long long)__float_as_uint(y) << 32) | __float_as_uint(x),
@@ -179,15 +199,40 @@ __device__ __forceinline__ float2 load_pair(const float* p)
     const unsigned long long w = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
 }
-// The workgroup's slot; part z of the same row block has its own z - part places further.
-__device__ __forceinline__ float* part_slot(const AttendArgs& a, int index, int rows_per_block)
+// Lane orders: blocks of 32 rows as O^T lies in 32x32 accumulators (attend_mfma.hip); row after row, eight dims to a lane
+// (attend_short.hip); blocks of 16 rows as in 16x16 accumulators, head_dim padded to 64s (attend_f32.hip).
+enum SlotOrder { kSlotMany, kSlotFew, kSlotF32 };
+constexpr __host__ __device__ int slot_dims(int d) { return (d + 63) / 64 * 64; }
+constexpr __host__ __device__ int slot_floats(int d, int rows_per_block) { return rows_per_block * (slot_dims(d) + 2); }
+// floats from the slot's start to dims 4 * piece .. of row `row`
+template <SlotOrder O> __device__ __forceinline__ int slot_place(int d, int row, int piece)
 {
-    return a.part + (long long)index * rows_per_block * (a.d + 2);
+    if constexpr (O == kSlotMany) return ((row >> 5) * (d / 8) + (piece >> 1)) * 256 + 4 * ((row & 31) + 32 * (piece & 1));
+    if constexpr (O == kSlotFew) { const int t = row * (d / 8) + (piece >> 1); return (t >> 6) * 512 + (piece & 1) * 256 + 4 * (t & 63); }
+    return ((row >> 4) * (slot_dims(d) / 16) + (piece >> 4) * 4 + (piece & 3)) * 256 + 4 * ((row & 15) + 16 * ((piece >> 2) & 3));
+}
+// ... and back: what lies at floats 4 * x ..
+template <SlotOrder O> __device__ __forceinline__ void slot_piece(int d, int x, int& row, int& piece)
+{
+    const int lane = x & 63, y = x >> 6;
+    if constexpr (O == kSlotMany) { const int b = y / (d / 8); row = 32 * b + (lane & 31); piece = 2 * (y - b * (d / 8)) + (lane >> 5); }
+    else if constexpr (O == kSlotFew) { const int t = (y >> 1) * 64 + lane; row = t / (d / 8); piece = 2 * (t - row * (d / 8)) + (y & 1); }
+    else { const int nb = slot_dims(d) / 64, b = (y >> 2) / nb; row = 16 * b + (lane & 15); piece = 16 * ((y >> 2) - b * nb) + 4 * (lane >> 4) + (y & 3); }
+}
+__device__ __forceinline__ float* slot_max_sum(const AttendArgs& a, float* slot, int rows_per_block, int row)
+{
+    return slot + rows_per_block * slot_dims(a.d) + 2 * row;
+}
+// The workgroup's slot; part z of the same row block has its own Hkv * (z - part) places further.
+__device__ __forceinline__ float* part_slot(const AttendArgs& a, const AttendItem& it, int rows_per_block)
+{
+    return a.part + ((long long)(it.s.slot0 + it.local) * a.Hkv + it.kvh) * slot_floats(a.d, rows_per_block);
 }
 // Called by all threads after their stores to the slot.  True in the workgroup that arrives last.
 __device__ __forceinline__ bool arrive_last(const AttendArgs& a, const AttendItem& it, int n_parts, int* flag)
 {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");     // every store of the thread has been acknowledged
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // every store of the wave has been acknowledged
     __syncthreads();
     if (threadIdx.x == 0) {
         const unsigned before = __builtin_amdgcn_atomic_inc32(a.counters + (long long)(it.s.group0 + it.block) * a.Hkv + it.kvh, (unsigned)n_parts - 1u,
@@ -197,26 +242,31 @@ __device__ __forceinline__ bool arrive_last(const AttendArgs& a, const AttendIte
     __syncthreads();
     return *flag != 0;
 }
-template <typename T>
-__device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendItem& it, int index, int n_parts, int rows_per_block, int n_threads)
+// (D: head_dim where the kernel knows it, or 0)
+template <typename T, SlotOrder O, int D>
+__device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendItem& it, int n_parts, int rows_per_block, int n_threads)
 {
+    const int d = D ? D : a.d;
     const int r0 = it.block * rows_per_block, rows = min(rows_per_block, a.G * it.s.N - r0);
-    const int pieces = a.d / 4;
-    const float* const first = part_slot(a, index - it.part * a.Hkv, rows_per_block);
-    const long long step = (long long)a.Hkv * rows_per_block * (a.d + 2);
+    const long long step = (long long)a.Hkv * slot_floats(d, rows_per_block);
+    float* const first = part_slot(a, it, rows_per_block) - it.part * step;
     constexpr int kBatch = 4;                              // parts per trip to memory
-    for (int x = threadIdx.x; x < rows * pieces; x += n_threads) {
-        const int row = x / pieces, piece = x - row * pieces;
+    for (int x = threadIdx.x; x < rows_per_block * slot_dims(d) / 4; x += n_threads) {
+        int row, piece;
+        slot_piece<O>(d, x, row, piece);
+        if (row >= rows || 4 * piece >= d) continue;
+        const float* const at = first + 4 * x;
+        const float* const ml_at = slot_max_sum(a, first, rows_per_block, row);
         float M = kLowest, L = 0.0f;
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int z0 = 0; z0 < n_parts; z0 += kBatch) {
             float2 ml[kBatch], lo[kBatch], hi[kBatch];
 #pragma unroll
             for (int z = 0; z < kBatch; ++z) {
-                const float* const slot = first + min(z0 + z, n_parts - 1) * step;
-                ml[z] = load_pair(slot + (long long)rows_per_block * a.d + 2 * row);
-                lo[z] = load_pair(slot + (long long)row * a.d + 4 * piece);
-                hi[z] = load_pair(slot + (long long)row * a.d + 4 * piece + 2);
+                const long long off = min(z0 + z, n_parts - 1) * step;
+                ml[z] = load_pair(ml_at + off);
+                lo[z] = load_pair(at + off);
+                hi[z] = load_pair(at + off + 2);
             }
             float up = M;
 #pragma unroll
@@ -238,10 +288,45 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendIte
     }
 }
 
-// ---- launches (one per source file); `a` without its sequences: those are picked and cut by the launcher's rule
+// The rows `bad` (bit b: row row0 + b of the block), dims dim0 .. dim1 - 1 of them, leave as exact_row has them: into the slot, or
+// finished.  m_of(row): the reference that the row's (max, sum) go by.
+template <typename T, SlotOrder O, typename F>
+__device__ __forceinline__ void leave_exact_rows(const AttendArgs& a, const AttendItem& it, uint32_t bad, int row0, int dim0, int dim1, int rows_per_block, int k_begin,
+                                                 int k_end, int n_parts, float* slot, F m_of)
+{
+    const int lane = threadIdx.x & 63, r0 = it.block * rows_per_block;
+    const bool mine = 4 * lane >= dim0 && 4 * lane < dim1;
+    while (bad) {
+        const int row = row0 + __builtin_ctz(bad);
+        bad &= bad - 1u;
+        float4 o;
+        float l;
+        exact_row<T>(a, it.s, it.kvh, r0 + row, k_begin, k_end, m_of(row), o, l);
+        if (!mine) continue;
+        if (n_parts > 1) {
+            store_four(slot + slot_place<O>(a.d, row, lane), o.x, o.y, o.z, o.w);
+        } else {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int j = div_G(a, r0 + row);
+            Four<T>::store(out_row(a, it.s, j, it.kvh * a.G + (r0 + row - j * a.G), sizeof(T)) + 4 * lane * (int)sizeof(T),
+                           make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+        }
+    }
+}
+
+// ---- launches
 struct AttendBatch { int n_seq; int row0[DYSPEC_MAX_SEQ + 1]; int context[DYSPEC_MAX_SEQ]; };
 size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d);
+// `a` without its sequences, which are dealt to the kernels and cut into items (attend.hip)
 hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
 hipError_t prepare_attend();
+
+// the kernels, on `items` items of a's sequences
+constexpr int kManyRows = 128, kFewRows = 32;                      // rows of a block: attend_mfma.hip, attend_short.hip
+hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream);      // blocks of 16 * row_waves rows
+hipError_t launch_attend_mfma(const AttendArgs& a, int items, hipStream_t stream);
+hipError_t launch_attend_short(const AttendArgs& a, int waves, int most_new, int items, hipStream_t stream);
+hipError_t prepare_attend_mfma();
+hipError_t prepare_attend_short();
 
 }  // namespace dyspec

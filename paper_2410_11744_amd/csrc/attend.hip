@@ -1,0 +1,233 @@
+// Attention of new tokens over pages or packed rows: which kernel takes which sequence, and how the walks are cut into items.
+//
+// bf16 with head_dim 64 or 128 goes to the bf16 matrix cores: attend_short.hip (blocks of 32 rows, the waves share out the keys)
+// and attend_mfma.hip (blocks of 128 rows).  Everything else goes to attend_f32.hip.
+#include "attend.h"
+
+namespace dyspec {
+
+// A kernel as the choice sees it: a launch, then workgroups of which the chip holds `slots` at a time; each costs `once` and
+// `step` per `keys` keys, more by the share `alone` over its sequence's row blocks: the first to read a key reads it from memory.
+// Microseconds.
+enum AttendKind { kFew8, kFew4, kMany, kF32Few, kF32Many, kKinds };
+struct KindCost { int rows, keys, slots; float launch, once, step, alone; };
+constexpr KindCost kCosts[2][kKinds] = {
+    // head_dim 128
+    { { kFewRows, 32, 256, 3.5f, 3.0f, 0.26f, 0.4f }, { kFewRows, 32, 512, 3.8f, 2.5f, 0.47f, 0.2f }, { kManyRows, 64, 256, 4.0f, 4.0f, 0.93f, 0.05f },
+      { 16, 128, 512, 4.0f, 3.0f, 2.0f, 0.0f }, { 64, 32, 512, 4.0f, 3.0f, 1.7f, 0.0f } },
+    // head_dim 64
+    { { kFewRows, 32, 256, 3.5f, 2.5f, 0.155f, 0.5f }, { kFewRows, 32, 512, 3.3f, 1.9f, 0.26f, 0.1f }, { kManyRows, 64, 256, 3.5f, 3.5f, 0.55f, 0.3f },
+      { 16, 128, 512, 4.0f, 3.0f, 1.0f, 0.0f }, { 64, 32, 512, 4.0f, 3.0f, 0.85f, 0.0f } },
+};
+constexpr float kBytesPerUs = 5.5e6f;          // K and V from memory
+constexpr float kPartBytesPerUs = 2.5e6f;      // parts to memory and back
+constexpr float kPartOnce = 3.0f;              // the arrival, and the last workgroup's trip
+constexpr int kUnit = 128;                     // a share is a multiple of this many keys
+
+static const KindCost& cost_of(const AttendArgs& a, AttendKind k) { return kCosts[a.d <= 64][k]; }
+
+// A set of sequences (indices, longest walks first) for one kernel, walks cut into shares of at most `share` keys.
+struct Set { AttendKind kind; int n, share; int seq[DYSPEC_MAX_SEQ]; };
+
+static int new_of(const AttendBatch& b, int s) { return b.row0[s + 1] - b.row0[s]; }
+static int keys_of(const AttendBatch& b, int s) { return b.context[s] + new_of(b, s); }
+static int blocks_of(const AttendArgs& a, const AttendBatch& b, int s, int rows) { return (int)(((long long)new_of(b, s) * a.G + rows - 1) / rows); }
+static int parts_of(int keys, int share) { return share >= keys ? 1 : (keys + share - 1) / share; }
+
+// Time of a set.  The chip is busy with everything that has been started; it ends no sooner than its longest item does, than
+// whole rounds of equally long items do, than the keys and values come from memory.
+// *floor: what no way of cutting can go below.
+static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, int elt, float* floor = nullptr)
+{
+    const KindCost& c = cost_of(a, set.kind);
+    float worst = 0.0f, bytes = 0.0f, slot_bytes = 0.0f;
+    double busy = 0.0;
+    long long before = 0;
+    for (int x = 0; x < set.n; ++x) {
+        const int s = set.seq[x], keys = keys_of(b, s), parts = parts_of(keys, set.share);
+        const long long items = (long long)blocks_of(a, b, s, c.rows) * parts * a.Hkv;
+        const float whole = (float)keys / (float)parts, mean = (float)(b.context[s] + (new_of(b, s) + 1) / 2) / (float)parts;
+        const float step = c.step * (1.0f + c.alone / (float)blocks_of(a, b, s, c.rows)) / (float)c.keys;
+        const float item = c.once + step * (whole + 0.5f * (float)c.keys), usual = c.once + step * (mean + 0.5f * (float)c.keys);
+        before += items;
+        busy += (double)items * usual;
+        worst = fmaxf(worst, fmaxf(item, (float)((before + c.slots - 1) / c.slots) * usual));
+        bytes += (float)keys * (float)a.Hkv * (float)(a.d * 2 * elt);
+        if (parts > 1) slot_bytes += (float)items * (float)(min((long long)c.rows, (long long)new_of(b, s) * a.G) * a.d * 4);
+    }
+    if (floor) *floor = c.launch + fmaxf((float)(busy / c.slots), bytes / kBytesPerUs);
+    if (set.n == 0) return 0.0f;
+    const float work = fmaxf(worst, (float)(busy / c.slots)), memory = bytes / kBytesPerUs;
+    float t = c.launch + cbrtf(work * work * work + memory * memory * memory);          // (where both are near, neither is reached)
+    if (slot_bytes > 0.0f) t += kPartOnce + 2.0f * slot_bytes / kPartBytesPerUs;
+    return t;
+}
+
+static long long counters_of(const AttendArgs& a, const AttendBatch& b, const Set& set)
+{
+    long long n = 0;
+    for (int x = 0; x < set.n; ++x) n += blocks_of(a, b, set.seq[x], cost_of(a, set.kind).rows);
+    return n * a.Hkv;
+}
+
+// The share that takes least time (its own, if counters and a workspace allow parts).
+static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, bool parts)
+{
+    set.share = DYSPEC_MAX_CONTEXT;
+    float floor, best = time_of(a, b, set, elt, &floor);
+    if (!parts || set.n == 0 || counters_of(a, b, set) * (long long)sizeof(unsigned) > DYSPEC_PAGED_COUNTER_BYTES / 2) return best;
+    if (best < 1.15f * floor) return best;
+    int best_share = set.share;
+    const int longest = keys_of(b, set.seq[0]);
+    constexpr int kTries[] = { 2, 3, 4, 6, 8, 12, 16, 24, 32 };
+    for (int p : kTries) {
+        const int share = ((longest + p - 1) / p + kUnit - 1) / kUnit * kUnit;
+        set.share = share;
+        const float t = time_of(a, b, set, elt);
+        if (t < 0.97f * best) { best = t; best_share = share; }
+        else if (t > 1.3f * best) break;
+        if (share == kUnit) break;
+    }
+    set.share = best_share;
+    return best;
+}
+
+struct Plan { int n; Set set[2]; };
+
+static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool parts, Plan& plan)
+{
+    int order[DYSPEC_MAX_SEQ], n = 0;
+    for (int s = 0; s < b.n_seq; ++s) {
+        if (new_of(b, s) == 0) continue;
+        int at = n++;
+        for (; at > 0 && keys_of(b, order[at - 1]) < keys_of(b, s); --at) order[at] = order[at - 1];
+        order[at] = s;
+    }
+    auto pieces = [](const void* p, long long stride) { return reinterpret_cast<size_t>(p) % 16 == 0 && stride % 16 == 0; };
+    const bool bf16 = dtype == DYSPEC_BF16 && (a.d == 64 || a.d == 128) && pieces(a.q, a.q_stride) && pieces(a.k, a.k_stride) &&
+                      pieces(a.v, a.v_stride) && pieces(a.out, a.out_stride);
+    const int elt = dtype == DYSPEC_BF16 ? 2 : 4;
+    // sequences of at most `rows` rows to `few`, the others to `many`; kept if that is the fastest so far
+    float best = 0.0f;
+    plan.n = 0;
+    auto consider = [&](long long rows, AttendKind few, AttendKind many) {
+        Plan p;
+        p.n = 2;
+        p.set[0].kind = many; p.set[1].kind = few;
+        p.set[0].n = p.set[1].n = 0;
+        for (int x = 0; x < n; ++x) {
+            Set& set = p.set[(long long)new_of(b, order[x]) * a.G <= rows];
+            set.seq[set.n++] = order[x];
+        }
+        const float t = cut(a, b, p.set[0], elt, parts) + cut(a, b, p.set[1], elt, parts);
+        if (plan.n == 0 || t < best) { plan = p; best = t; }
+    };
+    constexpr long long kAll = 1LL << 62;
+    if (!bf16) {
+        consider(16, kF32Few, kF32Many);
+        consider(kAll, kF32Few, kF32Many);
+    } else {
+        long long most = 0, blocks = 0;
+        for (int x = 0; x < n; ++x) {
+            most = max(most, (long long)new_of(b, order[x]) * a.G);
+            blocks += blocks_of(a, b, order[x], kFewRows);
+        }
+        consider(kAll, kFew8, kMany);
+        if (blocks * a.Hkv > cost_of(a, kFew8).slots) consider(kAll, kFew4, kMany);
+        if (most > kFewRows) {
+            consider(0, kFew8, kMany);
+            if (n > 1) consider(2 * kFewRows, kFew8, kMany);
+        }
+    }
+}
+
+static size_t slot_bytes(const AttendArgs& a, AttendKind k) { return (size_t)a.Hkv * slot_floats(a.d, cost_of(a, k).rows) * sizeof(float); }
+
+// The set's sequences in a's table; returns items, and the row blocks and slots they take.
+static int fill(AttendArgs& a, const AttendBatch& b, const Set& set, int* groups, long long* slots, int* most_new)
+{
+    int items = 0;
+    *groups = 0; *slots = 0; *most_new = 0;
+    a.n_seq = set.n;
+    for (int x = 0; x < set.n; ++x) {
+        const int s = set.seq[x], keys = keys_of(b, s), blocks = blocks_of(a, b, s, cost_of(a, set.kind).rows);
+        AttendSeq& q = a.seq[x];
+        q.id = s; q.row0 = b.row0[s]; q.N = new_of(b, s); q.C = b.context[s];
+        q.item0 = items; q.group0 = *groups; q.slot0 = (int)*slots;
+        q.parts = parts_of(keys, set.share);
+        q.share = q.parts == 1 ? keys : ((keys + q.parts - 1) / q.parts + kUnit - 1) / kUnit * kUnit;
+        q.parts = parts_of(keys, q.share);
+        items += blocks * q.parts;
+        *groups += blocks;
+        if (q.parts > 1) *slots += (long long)blocks * q.parts;
+        *most_new = max(*most_new, q.N);
+    }
+    return items;
+}
+
+size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d)
+{
+    AttendArgs a;
+    a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.d = d;
+    a.q = a.k = a.v = a.out = nullptr;
+    a.q_stride = a.out_stride = a.k_stride = a.v_stride = 16;
+    Plan plan;
+    plan_of(a, b, dtype, true, plan);
+    size_t bytes = 0;
+    for (int x = 0; x < plan.n; ++x) {
+        int groups, most;
+        long long slots;
+        fill(a, b, plan.set[x], &groups, &slots, &most);
+        bytes += (size_t)slots * slot_bytes(a, plan.set[x].kind);
+    }
+    return bytes ? DYSPEC_PAGED_COUNTER_BYTES + bytes : 0;
+}
+
+hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    Plan plan;
+    for (int parts = workspace != nullptr; parts >= 0; --parts) {
+        plan_of(a, b, dtype, parts != 0, plan);
+        size_t need = DYSPEC_PAGED_COUNTER_BYTES;
+        for (int x = 0; x < plan.n && parts; ++x) {
+            int groups, most;
+            long long slots;
+            fill(a, b, plan.set[x], &groups, &slots, &most);
+            need += (size_t)slots * slot_bytes(a, plan.set[x].kind);
+        }
+        if (!parts || need <= workspace_bytes || need == DYSPEC_PAGED_COUNTER_BYTES) break;      // no room: every walk in one piece
+    }
+    char* slots_at = static_cast<char*>(workspace) + DYSPEC_PAGED_COUNTER_BYTES;
+    unsigned* counters = static_cast<unsigned*>(workspace);
+    for (int x = 0; x < plan.n; ++x) {
+        const Set& set = plan.set[x];
+        int groups, most;
+        long long slots;
+        const int items = fill(a, b, set, &groups, &slots, &most);
+        if (items == 0) continue;
+        a.part = reinterpret_cast<float*>(slots_at);
+        a.counters = counters;
+        if (slots) {
+            slots_at += (size_t)slots * slot_bytes(a, set.kind);
+            counters += groups * a.Hkv;
+        }
+        hipError_t e = hipSuccess;
+        switch (set.kind) {
+            case kMany: e = launch_attend_mfma(a, items, stream); break;
+            case kFew8: e = launch_attend_short(a, 8, most, items, stream); break;
+            case kFew4: e = launch_attend_short(a, 4, most, items, stream); break;
+            case kF32Many: e = launch_attend_f32(a, dtype, 4, items, stream); break;
+            default: e = launch_attend_f32(a, dtype, 1, items, stream); break;
+        }
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t prepare_attend()
+{
+    const hipError_t e = prepare_attend_mfma();
+    return e == hipSuccess ? prepare_attend_short() : e;
+}
+
+}  // namespace dyspec

@@ -19,8 +19,9 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr int kF32Waves = 4;
 
 template <typename T, int DP>
-__global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs a, int row_waves)
+__global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, int row_waves)
 {
+    const AttendArgs& a = attend_args_here();
     typedef typename Four<T>::raw raw;
     constexpr int NS = DP / 16, NB = DP / 64;
     constexpr int KB = DP <= 128 ? 32 : 16, N16 = KB / 16;         // keys of a step
@@ -32,8 +33,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs a
     const int n = lane & 15, g = lane >> 4;
     const int R = 16 * row_waves, key_waves = kF32Waves / row_waves;
     const int wq = wave % row_waves, wk = wave / row_waves;
-    const int index = blockIdx.x;
-    const AttendItem it = attend_item(a, index, R);
+    const AttendItem it = attend_item(a, blockIdx.x, R);
     const AttendSeq& s = it.s;
     const int rows = a.G * s.N, r0 = it.block * R;
     const int r = r0 + 16 * wq + n, rc = min(r, rows - 1);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs a
         }
     }
     // ---- the rows leave: acc[b][c][i] is dim 64b + 16g + 4i + c
-    float* const slot = part_slot(a, index, R);
+    float* const slot = part_slot(a, it, R);
     if (wk == 0) {
         bool nan = l != l;
 #pragma unroll
@@ -209,19 +209,16 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs a
         uint32_t bad = (uint32_t)((lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu);
         const bool leave = r < rows && !((bad >> n) & 1u);
         if (n_parts > 1) {
+            if (g == 0 && r < rows) store_pair(slot_max_sum(a, slot, R, 16 * wq + n), m, l);
             if (leave) {
-                float* const dst = slot + (16 * wq + n) * a.d;
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int dim = 64 * b + 16 * g + 4 * i;
-                        if (dim < a.d) {
-                            store_pair(dst + dim, acc[b][0][i], acc[b][1][i]);
-                            store_pair(dst + dim + 2, acc[b][2][i], acc[b][3][i]);
-                        }
+                        if (dim < a.d)
+                            store_four(slot + slot_place<kSlotF32>(a.d, 16 * wq + n, dim / 4), acc[b][0][i], acc[b][1][i], acc[b][2][i], acc[b][3][i]);
                     }
-                if (g == 0) store_pair(slot + R * a.d + 2 * (16 * wq + n), m, l);
             }
         } else if (leave) {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -235,119 +232,26 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs a
                         Four<T>::store(dst + dim * size, make_float4(acc[b][0][i] * inv, acc[b][1][i] * inv, acc[b][2][i] * inv, acc[b][3][i] * inv));
                 }
         }
-        while (bad) {
-            const int row = 16 * wq + __builtin_ctz(bad);
-            bad &= bad - 1u;
-            float4 o;
-            float em, el;
-            exact_row<T>(a, s, it.kvh, r0 + row, k_begin, k_end, o, em, el);
-            if (n_parts > 1) {
-                if (4 * lane < a.d) {
-                    store_pair(slot + row * a.d + 4 * lane, o.x, o.y);
-                    store_pair(slot + row * a.d + 4 * lane + 2, o.z, o.w);
-                }
-                if (lane == 0) store_pair(slot + R * a.d + 2 * row, em, el);
-            } else if (4 * lane < a.d) {
-                const float inv = el == 0.0f ? 0.0f : 1.0f / el;
-                const int bj = div_G(a, r0 + row);
-                Four<T>::store(out_row(a, s, bj, it.kvh * a.G + (r0 + row - bj * a.G), size) + 4 * lane * size, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-            }
-        }
+        leave_exact_rows<T, kSlotF32>(a, it, bad, 16 * wq, 0, a.d, R, k_begin, k_end, n_parts, slot,
+                                   [=](int row) { return __shfl(m, row - 16 * wq, kWave); });
     }
-    if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<T>(a, it, index, n_parts, R, 64 * kF32Waves);
-}
-
-// ---- how a batch is cut
-//
-// A row block is one workgroup's as long as the blocks fill the chip; otherwise the walks are cut into shares of one length until
-// there are about two workgroups per CU, no share below 128 keys (four steps of a wave).
-constexpr int kF32Items = 512, kF32Share = 128;
-
-struct F32Cut { int row_waves, items, groups; bool split; };
-
-static F32Cut cut_f32(const AttendBatch& b, AttendArgs& a)
-{
-    F32Cut c;
-    int most = 0;
-    for (int s = 0; s < b.n_seq; ++s) most = max(most, b.row0[s + 1] - b.row0[s]);
-    c.row_waves = (long long)most * a.G <= 16 ? 1 : kF32Waves;
-    const int R = 16 * c.row_waves;
-    long long blocks = 0, keys = 0;
-    for (int s = 0; s < b.n_seq; ++s) {
-        const long long nb = ((long long)(b.row0[s + 1] - b.row0[s]) * a.G + R - 1) / R;
-        blocks += nb;
-        keys += nb * (b.context[s] + b.row0[s + 1] - b.row0[s]);
-    }
-    c.split = blocks * a.Hkv < kF32Items / 2 && blocks * a.Hkv * (long long)sizeof(unsigned) <= DYSPEC_PAGED_COUNTER_BYTES;
-    long long share = max(keys * a.Hkv / kF32Items, (long long)kF32Share);
-    share = (share + kF32Share - 1) / kF32Share * kF32Share;
-    a.n_seq = 0;
-    c.items = c.groups = 0;
-    // longest first
-    int order[DYSPEC_MAX_SEQ], n = 0;
-    for (int s = 0; s < b.n_seq; ++s)
-        if (b.row0[s + 1] > b.row0[s]) {
-            int at = n++;
-            for (; at > 0 && b.context[order[at - 1]] < b.context[s]; --at) order[at] = order[at - 1];
-            order[at] = s;
-        }
-    for (int x = 0; x < n; ++x) {
-        const int s = order[x];
-        AttendSeq& q = a.seq[a.n_seq++];
-        q.id = s; q.row0 = b.row0[s]; q.N = b.row0[s + 1] - b.row0[s]; q.C = b.context[s];
-        q.item0 = c.items; q.group0 = c.groups;
-        const int nb = (int)(((long long)q.N * a.G + R - 1) / R);
-        q.parts = c.split ? (int)((q.C + q.N + share - 1) / share) : 1;
-        q.share = (int)share;
-        c.items += nb * q.parts;
-        c.groups += nb;
-    }
-    c.split = c.items > c.groups;
-    return c;
+    if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<T, kSlotF32, 0>(a, it, n_parts, R, 64 * kF32Waves);
 }
 
 template <typename T>
-static void launch_f32(const AttendArgs& a, const F32Cut& c, hipStream_t stream)
+static void launch_f32(const AttendArgs& a, int row_waves, int blocks, hipStream_t stream)
 {
-    const int blocks = c.items * a.Hkv;
-    if (a.d <= 64) attend_f32_kernel<T, 64><<<blocks, 64 * kF32Waves, 0, stream>>>(a, c.row_waves);
-    else if (a.d <= 128) attend_f32_kernel<T, 128><<<blocks, 64 * kF32Waves, 0, stream>>>(a, c.row_waves);
-    else if (a.d <= 192) attend_f32_kernel<T, 192><<<blocks, 64 * kF32Waves, 0, stream>>>(a, c.row_waves);
-    else attend_f32_kernel<T, 256><<<blocks, 64 * kF32Waves, 0, stream>>>(a, c.row_waves);
+    if (a.d <= 64) attend_f32_kernel<T, 64><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 128) attend_f32_kernel<T, 128><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 192) attend_f32_kernel<T, 192><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else attend_f32_kernel<T, 256><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
 }
 
-static size_t part_bytes(const AttendArgs& a, const F32Cut& c)
+hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream)
 {
-    return c.split ? DYSPEC_PAGED_COUNTER_BYTES + (size_t)c.items * a.Hkv * 16 * c.row_waves * (a.d + 2) * sizeof(float) : 0;
-}
-
-size_t attend_workspace_bytes(const AttendBatch& b, int, int Hq, int Hkv, int d)
-{
-    AttendArgs a;
-    a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.d = d;
-    return part_bytes(a, cut_f32(b, a));
-}
-
-hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream)
-{
-    F32Cut c = cut_f32(b, a);
-    if (c.split && (!workspace || workspace_bytes < part_bytes(a, c))) {      // no room: one workgroup walks it all
-        c.items = 0;
-        for (int s = 0; s < a.n_seq; ++s) {
-            AttendSeq& q = a.seq[s];
-            q.parts = 1; q.item0 = c.items;
-            c.items += (int)(((long long)q.N * a.G + 16 * c.row_waves - 1) / (16 * c.row_waves));
-        }
-        c.split = false;
-    }
-    if (c.items == 0) return hipSuccess;
-    a.counters = static_cast<unsigned*>(workspace);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + DYSPEC_PAGED_COUNTER_BYTES);
-    if (dtype == DYSPEC_F32) launch_f32<float>(a, c, stream);
-    else launch_f32<__bf16>(a, c, stream);
+    if (dtype == DYSPEC_F32) launch_f32<float>(a, row_waves, items * a.Hkv, stream);
+    else launch_f32<__bf16>(a, row_waves, items * a.Hkv, stream);
     return hipGetLastError();
 }
-
-hipError_t prepare_attend() { return hipSuccess; }
 
 }  // namespace dyspec

@@ -116,6 +116,9 @@ hipError_t launch_kv_append(AppendArgs a, int dtype, bool wide, hipStream_t stre
 // eight rows at a time (all eight read before the first is written) needs no copy of the rows and no other thread.
 constexpr int kKeepThreads = 128, kKeepBatch = 8;
 
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+
 template <typename V>
 __global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs a)
 {
@@ -156,8 +159,8 @@ hipError_t launch_kv_keep(const KeepArgs& a, int n_layers, hipStream_t stream)
 {
     if (a.row0[a.n_seq] == 0) return hipSuccess;
     const dim3 grid((a.row_pieces + kKeepThreads - 1) / kKeepThreads, a.n_seq, 2 * n_layers);
-    if (a.piece_bytes == 16) kv_keep_kernel<uint4><<<grid, kKeepThreads, 0, stream>>>(a);
-    else kv_keep_kernel<uint2><<<grid, kKeepThreads, 0, stream>>>(a);
+    if (a.piece_bytes == 16) kv_keep_kernel<words4><<<grid, kKeepThreads, 0, stream>>>(a);
+    else kv_keep_kernel<words2><<<grid, kKeepThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

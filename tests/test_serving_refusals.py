@@ -90,7 +90,7 @@ def test_addresses(lib):
     assert prompt(lib, out=A) == BAD_ARG
     for bad in (dict(q=A + 4), dict(k=A + 4), dict(v=A + 2), dict(out=A + 0x10004), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(qs=1026), dict(ks=258)):
         assert prompt(lib, **bad) == BAD_ARG, bad
-    for bad in (dict(qs=1020), dict(ks=252), dict(vs=0), dict(vs=1 << 25)):
+    for bad in (dict(qs=1020), dict(ks=252), dict(vs=0), dict(vs=1 << 23)):
         assert prompt(lib, **bad) == BAD_SHAPE, bad
     for bad in (dict(q=A + 1), dict(k=A + 1), dict(k=None), dict(v=None), dict(freq=None), dict(freq=A + 2), dict(rel=A + 2), dict(q_out=None), dict(q=None),
                 dict(Hq=0), dict(q=A, q_out=A, qs=1032), dict(k_out=A, ks=264)):
