@@ -234,8 +234,11 @@ _dtypes: dict = {}
 
 
 def _dtype(name: str):
-    import torch
-    return _dtypes.setdefault(name, getattr(torch, name))
+    t = _dtypes.get(name)
+    if t is None:
+        import torch
+        t = _dtypes[name] = getattr(torch, name)
+    return t
 
 
 def _ptr(t, want: Optional[str] = None) -> int:
@@ -592,6 +595,8 @@ class PagedCache:
         if k.dim() not in (4, 5) or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v need one shape ([layers,] pages, rows, heads, head_dim) and dtype")
         n_pages, page, Hkv, d = k.shape[-4:]
+        if k.dim() == 5 and k.shape[0] == 0:
+            raise ValueError("a cache of no layer")
         for t in (k, v):
             if not t.is_cuda:
                 raise ValueError("device tensor required")
@@ -606,24 +611,20 @@ class PagedCache:
         columns = int(table.shape[1])
         c = _PagedKV(k.data_ptr(), v.data_ptr(), table.data_ptr(), int(n_pages), int(page), columns,
                      int(table.stride(0)) if table.shape[0] > 1 else columns, int(k.stride(-4)) if n_pages > 1 else int(page * Hkv * d))
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_ref", ctypes.byref(c))
-        object.__setattr__(self, "_heads", (int(Hkv), int(d)))
-        object.__setattr__(self, "_dtype", _code(k.dtype))
-
-    @property
-    def n_layers(self) -> int:
-        return int(self.k.shape[0]) if self.k.dim() == 5 else 1
+        layers = int(k.shape[0]) if k.dim() == 5 else 0
+        for name, value in dict(_c=c, _ref=ctypes.byref(c), _heads=(int(Hkv), int(d)), _code=_code(k.dtype), _torch_dtype=k.dtype,
+                                _device=k.get_device(), _rows=int(table.shape[0]), _layers=layers,
+                                _layer_stride=int(k.stride(0)) if layers > 1 else 0).items():
+            object.__setattr__(self, name, value)
 
     def layer(self, index: int) -> "PagedCache":
         return PagedCache(self.k[index], self.v[index], self.page_table)
 
 
 def _code(dtype) -> int:
-    code = {_dtype("float32"): F32, _dtype("bfloat16"): BF16}.get(dtype)
-    if code is None:
+    if dtype is not _dtype("bfloat16") and dtype is not _dtype("float32"):
         raise ValueError(f"float32 or bfloat16 expected, got {dtype}")
-    return code
+    return BF16 if dtype is _dtype("bfloat16") else F32
 
 
 class DeviceCall(PreparedCall):
@@ -635,117 +636,8 @@ class DeviceCall(PreparedCall):
         self._device = device
 
     def __call__(self):
-        if _torch.cuda.current_device() == self._device:
-            return super().__call__()
-        with _torch.cuda.device(self._device):
-            return super().__call__()
-
-
-def _token_rows(t, shape, dtype, device, what: str) -> int:
-    """Elements between the tokens of t [tokens, heads, d], heads dense."""
-    if t.shape != shape or t.dtype is not dtype or t.device != device:
-        raise ValueError(f"{what}: {tuple(shape)} of {dtype} on {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    n, heads, d = shape
-    s = t.stride()
-    if (d > 1 and s[2] != 1) or (heads > 1 and s[1] != d):
-        raise ValueError(f"{what}: a token's heads must be dense")
-    return s[0] if n > 1 else heads * d
-
-
-def _dense(t, shape, dtype, device, what: str) -> int:
-    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} on {device} expected")
-    return t.data_ptr()
-
-
-_on_stream = contextlib.nullcontext()
-
-
-def _stream_of(stream, device):
-    """(raw handle, context in which memory belongs to that stream) of the given stream or the device's current one."""
-    torch = _torch
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index), _on_stream
-    if stream.device != device:
-        raise ValueError("the stream is another device's")
-    return int(stream.cuda_stream), torch.cuda.stream(stream)
-
-
-def _hand_over(stream, *tensors) -> None:
-    """Memory that was given out for other streams is not to be reused while this one reads it."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
-
-
-_attend_scratch: dict = {}
-
-
-def _attend_workspace(device, raw: int, where, nbytes: int, prepared: bool):
-    """A paged_attn workspace, its head zero.  Calls of one stream run in order and share one; a prepared call, and a call that a
-    graph records, has its own, because whatever runs beside the graph may use the stream's."""
-    torch = _torch
-    with where:
-        capturing = torch.cuda.is_current_stream_capturing()
-        if prepared and capturing:
-            raise ValueError("prepare the call before the graph is recorded: its workspace has to be cleared first")
-        if not prepared and not capturing:
-            buf = _attend_scratch.get((device.index, raw))
-            if buf is not None and buf.numel() >= nbytes:
-                return buf
-        buf = torch.zeros(nbytes, dtype=torch.uint8, device=device)
-        if not prepared and not capturing:
-            _attend_scratch[(device.index, raw)] = buf
-        return buf
-
-
-def kv_append(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
-              out=None, k_out=None, stream=None):
-    """dyspec_kv_append: the new tokens' keys (rotated) and values go into their places in the pages; returns the rotated
-    queries (None without q).  k, v [sum N, Hkv, d] and q [sum N, Hq, d] may be slices of one projection's rows.
-    rel_pos: int32 positions relative to each sequence's context (a tree's depths), by default 0, 1, ...; inv_freq: fp32 [n],
-    the frequencies of the first n pairs of a head (None: nothing is rotated); out: the queries' place (may be q, where that is
-    dense); k_out: the rotated keys as dense rows as well."""
-    return kv_append_call(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_out, stream)()
-
-
-def kv_append_call(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
-                   out=None, k_out=None, stream=None) -> PreparedCall:
-    """kv_append's call, prepared: nothing is launched until the returned object is called."""
-    lib = _lib or load_library()
-    torch, total = _torch, batch.total_nodes
-    kc, (Hkv, d) = cache.k, cache._heads
-    device, dtype = kc.device, kc.dtype
-    if kc.dim() != 4 or cache.page_table.shape[0] < batch.n_seq:
-        raise ValueError("kv_append takes one layer's cache, with a table row per sequence")
-    shape = (total, Hkv, d)
-    ks, vs = _token_rows(k, shape, dtype, device, "k"), _token_rows(v, shape, dtype, device, "v")
-    raw, where = _stream_of(stream, device)
-    qp = qs = op = Hq = 0
-    if q is not None:
-        Hq = int(q.shape[1])
-        qs, qp = _token_rows(q, (total, Hq, d), dtype, device, "q"), q.data_ptr()
-        if out is None:
-            with where:
-                out = torch.empty((total, Hq, d), dtype=dtype, device=device)
-        op = _dense(out, (total, Hq, d), dtype, device, "out")
-    elif out is not None:
-        raise ValueError("out is the queries' place: q is missing")
-    kp = 0 if k_out is None else _dense(k_out, shape, dtype, device, "k_out")
-    rp = 0 if rel_pos is None else _dense(rel_pos, (total,), torch.int32, device, "rel_pos")
-    n_freq = fp = 0
-    if inv_freq is not None:
-        n_freq = inv_freq.numel()
-        fp = _dense(inv_freq, (n_freq,), torch.float32, device, "inv_freq")
-    if total == 0:
-        return _Nothing(out)
-    _hand_over(stream, q, k, v, out, k_out, rel_pos, inv_freq, kc, cache.v, cache.page_table)
-    cb = batch._c()
-    args = (qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, cache._ref, ctypes.byref(cb), rp, fp, n_freq, 1 if interleaved else 0,
-            Hq, Hkv, d, cache._dtype, op, kp, raw)
-    return DeviceCall(lib.dyspec_kv_append, args, (q, k, v, cache, cb, batch, rel_pos, inv_freq, out, k_out), "dyspec_kv_append", out,
-                      device.index)
+        _issue(self._fn, self._args, self._device, self._where)
+        return self.out
 
 
 class _Nothing(PreparedCall):
@@ -759,101 +651,263 @@ class _Nothing(PreparedCall):
         return self.out
 
 
+def _issue(fn, args, device: int, where: str) -> None:
+    if _torch._C._cuda_getDevice() == device:
+        st = fn(*args)
+    else:
+        with _torch.cuda.device(device):
+            st = fn(*args)
+    if st != 0:
+        raise DyspecError(st, where)
+
+
+def _token_rows(t, shape, dtype, device: int, what: str) -> int:
+    """Elements between the tokens of t [tokens, heads, d], heads dense."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        raise ValueError(f"{what}: {tuple(shape)} of {dtype} on device {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    s = t.stride()
+    n, heads, d = shape
+    if s[2] != 1 or s[1] != d:                 # (of a dimension of one the stride says nothing)
+        if (d > 1 and s[2] != 1) or (heads > 1 and s[1] != d):
+            raise ValueError(f"{what}: a token's heads must be dense")
+    return s[0] if n > 1 else heads * d
+
+
+def _dense(t, shape, dtype, device: int, what: str) -> int:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {tuple(shape)} of {dtype} on device {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _chunks(batch: Batch) -> dict:
+    """The batch's memo with what the calls below ask for every time: tokens, the C struct by reference."""
+    memo = batch._memo()
+    if "chunks" not in memo:
+        memo["chunks"] = (int(batch.node_offset[-1]), ctypes.byref(batch._c(memo)))
+    return memo
+
+
+def _stream_of(stream, device: int):
+    """(raw handle, context in which memory belongs to that stream) of a given stream."""
+    if stream.device.index != device:
+        raise ValueError("the stream is another device's")
+    return int(stream.cuda_stream), _torch.cuda.stream(stream)
+
+
+_current = contextlib.nullcontext()
+
+
+def _hand_over(stream, *tensors) -> None:
+    """Memory that was given out for other streams is not to be reused while this one reads it."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+
+
+_attend_scratch: dict = {}
+
+
+def _attend_workspace(device: int, raw: int, where, nbytes: int, prepared: bool):
+    """A paged_attn workspace, its head zero.  Calls of one stream run in order and share one; a prepared call, and a call that a
+    graph records, has its own, because whatever runs beside the graph may use the stream's."""
+    torch = _torch
+    with where:
+        capturing = torch._C._cuda_isCurrentStreamCapturing()
+        if not prepared and not capturing:
+            buf = _attend_scratch.get((device, raw))
+            if buf is not None and buf[1] >= nbytes:
+                return buf[0]
+        if prepared and capturing:
+            raise ValueError("prepare the call before the graph is recorded: its workspace has to be cleared first")
+        buf = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+        if not prepared and not capturing:
+            _attend_scratch[(device, raw)] = (buf, nbytes)
+        return buf
+
+
+def kv_append(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
+              out=None, k_out=None, stream=None):
+    """dyspec_kv_append: the new tokens' keys (rotated) and values go into their places in the pages; returns the rotated
+    queries (None without q).  k, v [sum N, Hkv, d] and q [sum N, Hq, d] may be slices of one projection's rows.
+    rel_pos: int32 positions relative to each sequence's context (a tree's depths), by default 0, 1, ...; inv_freq: fp32 [n],
+    the frequencies of the first n pairs of a head (None: nothing is rotated); out: the queries' place (may be q, where that is
+    dense); k_out: the rotated keys as dense rows as well."""
+    args, out = _append_args(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_out, stream)
+    if args is not None:
+        _issue(_lib.dyspec_kv_append, args, cache._device, "dyspec_kv_append")
+    return out
+
+
+def kv_append_call(k, v, batch: Batch, cache: PagedCache, q=None, rel_pos=None, inv_freq=None, interleaved: bool = False,
+                   out=None, k_out=None, stream=None) -> PreparedCall:
+    """kv_append's call, prepared: nothing is launched until the returned object is called."""
+    args, out = _append_args(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_out, stream)
+    if args is None:
+        return _Nothing(out)
+    keep = (k, v, batch._c(), cache, q, rel_pos, inv_freq, out, k_out)
+    return DeviceCall(_lib.dyspec_kv_append, args, keep, "dyspec_kv_append", out, cache._device)
+
+
+def _append_args(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_out, stream):
+    if _lib is None:
+        load_library()
+    torch = _torch
+    total, ref = _chunks(batch)["chunks"]
+    device, dtype, (Hkv, d) = cache._device, cache._torch_dtype, cache._heads
+    if cache._layers or cache._rows < batch.n_seq:
+        raise ValueError("kv_append takes one layer's cache, with a table row per sequence")
+    shape = (total, Hkv, d)
+    ks, vs = _token_rows(k, shape, dtype, device, "k"), _token_rows(v, shape, dtype, device, "v")
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    qp = qs = op = Hq = 0
+    if q is not None:
+        Hq = q.shape[1]
+        shape = (total, Hq, d)
+        qs, qp = _token_rows(q, shape, dtype, device, "q"), q.data_ptr()
+        if out is None:
+            with where:
+                out = torch.empty(shape, dtype=dtype, device=q.device)
+            op = out.data_ptr()
+        else:
+            op = _dense(out, shape, dtype, device, "out")
+    elif out is not None:
+        raise ValueError("out is the queries' place: q is missing")
+    kp = 0 if k_out is None else _dense(k_out, (total, Hkv, d), dtype, device, "k_out")
+    rp = 0 if rel_pos is None else _dense(rel_pos, (total,), torch.int32, device, "rel_pos")
+    n_freq = fp = 0
+    if inv_freq is not None:
+        n_freq = inv_freq.numel()
+        fp = _dense(inv_freq, (n_freq,), torch.float32, device, "inv_freq")
+    if total == 0:
+        return None, out
+    if stream is not None:
+        _hand_over(stream, q, k, v, out, k_out, rel_pos, inv_freq, cache.k, cache.v, cache.page_table)
+    return (qp, qs, k.data_ptr(), ks, v.data_ptr(), vs, cache._ref, ref, rp, fp, n_freq, 1 if interleaved else 0, Hq, Hkv, d,
+            cache._code, op, kp, raw), out
+
+
 def kv_keep(cache: PagedCache, batch: Batch, accepted_nodes, n_accepted, stream=None) -> None:
     """dyspec_kv_keep: after verify, the accepted path's rows move up behind the root's, in every layer of the cache.
     `batch` describes the trees as they were appended; accepted_nodes and n_accepted are verify's."""
-    lib = _lib or load_library()
-    torch, total = _torch, batch.total_nodes
-    k = cache.k
-    device, (Hkv, d) = k.device, cache._heads
-    if cache.page_table.shape[0] < batch.n_seq:
+    if _lib is None:
+        load_library()
+    torch = _torch
+    total, ref = _chunks(batch)["chunks"]
+    device, (Hkv, d), n_seq = cache._device, cache._heads, batch.n_seq
+    if cache._rows < n_seq:
         raise ValueError("a table row per sequence is needed")
     ap = _dense(accepted_nodes, (total,), torch.int32, device, "accepted_nodes")
-    np_ = _dense(n_accepted, (batch.n_seq,), torch.int32, device, "n_accepted")
+    np_ = _dense(n_accepted, (n_seq,), torch.int32, device, "n_accepted")
     if total == 0:
         return
-    raw, _ = _stream_of(stream, device)
-    _hand_over(stream, accepted_nodes, n_accepted, k, cache.v, cache.page_table)
-    cb = batch._c()
-    layers = cache.n_layers
-    DeviceCall(lib.dyspec_kv_keep, (cache._ref, layers, int(k.stride(0)) if layers > 1 else 0, ctypes.byref(cb), ap, np_, Hkv, d, cache._dtype, raw),
-               (), "dyspec_kv_keep", None, device.index)()
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(device)
+    else:
+        raw, _ = _stream_of(stream, device)
+        _hand_over(stream, accepted_nodes, n_accepted, cache.k, cache.v, cache.page_table)
+    _issue(_lib.dyspec_kv_keep, (cache._ref, cache._layers or 1, cache._layer_stride, ref, ap, np_, Hkv, d, cache._code, raw), device, "dyspec_kv_keep")
 
 
 def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None):
     """dyspec_paged_attn: the new tokens (appended before) attend to the pages: to their context and, causally or by an ancestor
     mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d]."""
-    return _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, False)()
+    args, out, _ = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, False)
+    if args is not None:
+        _issue(_lib.dyspec_paged_attn, args, cache._device, "dyspec_paged_attn")
+    return out
 
 
 def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None) -> PreparedCall:
     """paged_attn's call, prepared: nothing is launched until the returned object is called.  It has a workspace of its own."""
-    return _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, True)
+    args, out, ws = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, True)
+    if args is None:
+        return _Nothing(out)
+    return DeviceCall(_lib.dyspec_paged_attn, args, (q, batch._c(), cache, anc_mask, out, ws), "dyspec_paged_attn", out, cache._device)
 
 
-def _paged_attn(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared) -> PreparedCall:
-    lib = _lib or load_library()
+def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared):
+    if _lib is None:
+        load_library()
     torch = _torch
-    kc, (Hkv, d), code = cache.k, cache._heads, cache._dtype
-    device, dtype = kc.device, kc.dtype
-    memo = batch._memo()
-    total, Hq = int(batch.node_offset[-1]), int(q.shape[1])
-    if kc.dim() != 4 or cache.page_table.shape[0] < batch.n_seq:
+    memo = _chunks(batch)
+    total, ref = memo["chunks"]
+    device, dtype, (Hkv, d), code = cache._device, cache._torch_dtype, cache._heads, cache._code
+    if cache._layers or cache._rows < batch.n_seq:
         raise ValueError("paged_attn takes one layer's cache, with a table row per sequence")
-    qp = _dense(q, (total, Hq, d), dtype, device, "q")
+    Hq = q.shape[1]
+    shape = (total, Hq, d)
+    qp = _dense(q, shape, dtype, device, "q")
     mp = 0
     if anc_mask is not None:
         words = memo.get("chunk_words")
         if words is None:
             words = memo["chunk_words"] = max(1, -(-int(np.diff(batch.node_offset).max()) // 64))
         mp = _dense(anc_mask, (total, words), torch.int64, device, "anc_mask")
-    raw, where = _stream_of(stream, device)
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
     if out is None:
         with where:
             out = torch.empty_like(q)
-    op = _dense(out, q.shape, dtype, device, "out")
+        op = out.data_ptr()
+    else:
+        op = _dense(out, shape, dtype, device, "out")
     if total == 0:
-        return _Nothing(out)
-    cb = batch._c(memo)
-    ref = ctypes.byref(cb)
+        return None, out, None
     key = ("ws_paged", Hq, Hkv, d, code)
     nbytes = memo.get(key)
     if nbytes is None:
-        nbytes = memo[key] = int(lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code))
-    ws = _attend_workspace(device, raw, where, nbytes, prepared) if nbytes else None
-    _hand_over(stream, q, out, anc_mask, kc, cache.v, cache.page_table)
-    args = (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, op, ws.data_ptr() if nbytes else 0, nbytes, raw)
-    return DeviceCall(lib.dyspec_paged_attn, args, (q, cache, cb, batch, anc_mask, out, ws), "dyspec_paged_attn", out, device.index)
+        nbytes = memo[key] = int(_lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code))
+    ws, wp = None, 0
+    if nbytes:
+        ws = _attend_workspace(device, raw, where, nbytes, prepared)
+        wp = ws.data_ptr()
+    if stream is not None:
+        _hand_over(stream, q, out, anc_mask, cache.k, cache.v, cache.page_table)
+    return (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, op, wp, nbytes, raw), out, ws
 
 
 def prompt_attn(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None):
     """dyspec_prompt_attn: packed prompts attend to themselves, causally.  q [sum N, Hq, d], k, v [sum N, Hkv, d], which may be
     slices of one projection's rows; the batch's n_nodes are the prompts' lengths, its prefix_len zeros."""
-    return prompt_attn_call(q, k, v, batch, softmax_scale, out, stream)()
+    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream)
+    if args is not None:
+        _issue(_lib.dyspec_prompt_attn, args, device, "dyspec_prompt_attn")
+    return out
 
 
 def prompt_attn_call(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None) -> PreparedCall:
     """prompt_attn's call, prepared: nothing is launched until the returned object is called."""
-    lib = _lib or load_library()
-    torch, total = _torch, batch.total_nodes
-    device, dtype = q.device, q.dtype
-    if not q.is_cuda:
+    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream)
+    if args is None:
+        return _Nothing(out)
+    return DeviceCall(_lib.dyspec_prompt_attn, args, (q, k, v, batch._c(), out), "dyspec_prompt_attn", out, device)
+
+
+def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
+    if _lib is None:
+        load_library()
+    torch = _torch
+    total, ref = _chunks(batch)["chunks"]
+    device, dtype = q.get_device(), q.dtype
+    if device < 0:
         raise ValueError("device tensor required")
-    code, (Hq, d), Hkv = _code(dtype), q.shape[1:], int(k.shape[1])
-    Hq, d = int(Hq), int(d)
-    qs = _token_rows(q, (total, Hq, d), dtype, device, "q")
-    ks, vs = _token_rows(k, (total, Hkv, d), dtype, device, "k"), _token_rows(v, (total, Hkv, d), dtype, device, "v")
-    raw, where = _stream_of(stream, device)
+    code = _code(dtype)
+    _, Hq, d = q.shape
+    Hkv = k.shape[1]
+    shape, kv_shape = (total, Hq, d), (total, Hkv, d)
+    qs = _token_rows(q, shape, dtype, device, "q")
+    ks, vs = _token_rows(k, kv_shape, dtype, device, "k"), _token_rows(v, kv_shape, dtype, device, "v")
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
     if out is None:
         with where:
-            out = torch.empty((total, Hq, d), dtype=dtype, device=device)
-    op = _dense(out, (total, Hq, d), dtype, device, "out")
+            out = torch.empty(shape, dtype=dtype, device=q.device)
+        op = out.data_ptr()
+    else:
+        op = _dense(out, shape, dtype, device, "out")
     if total == 0:
-        return _Nothing(out)
-    _hand_over(stream, q, k, v, out)
-    cb = batch._c()
-    args = (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ctypes.byref(cb), Hq, Hkv, d, code, softmax_scale, op, raw)
-    return DeviceCall(lib.dyspec_prompt_attn, args, (q, k, v, cb, batch, out), "dyspec_prompt_attn", out, device.index)
+        return None, out, device
+    if stream is not None:
+        _hand_over(stream, q, k, v, out)
+    return (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ref, Hq, Hkv, d, code, softmax_scale, op, raw), out, device
 
 
 def probe_mfma_bf16(iterations: int, sink, stream=None, random_operands: bool = False) -> float:

@@ -441,8 +441,8 @@ static dyspec_status check_heads(int Hq, int Hkv, int d, int dtype)
 {
     if (Hkv < 1 || Hq < 0 || Hq % Hkv != 0) return DYSPEC_BAD_SHAPE;
     if ((dtype != DYSPEC_F32 && dtype != DYSPEC_BF16) || d < 4 || d > 256 || d % 4) return DYSPEC_UNSUPPORTED;
-    // a token's heads stay below 4 MB: eight rows of a page are addressed with 32-bit offsets
-    if ((long long)max(Hq, Hkv) * d > 1 << 20) return DYSPEC_BAD_SHAPE;
+    // a token's heads stay below 4 MB: eight rows of a page are addressed with 32-bit offsets; append divides by multiplication
+    if ((long long)max(Hq, Hkv) * d > 1 << 20 || max(Hq, Hkv) > 8192) return DYSPEC_BAD_SHAPE;
     return DYSPEC_OK;
 }
 
@@ -509,7 +509,7 @@ dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, i
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.page_stride = cache->page_stride;
     a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
     a.Hq = q ? n_q_heads : 0; a.Hkv = n_kv_heads; a.d = head_dim; a.half = n_freq; a.interleaved = interleaved != 0;
-    a.total = b.row0[b.n_seq]; a.tokens = 1; a.n_seq = b.n_seq;
+    a.total = b.row0[b.n_seq]; a.n_seq = b.n_seq;
     for (int s = 0; s < b.n_seq; ++s) { a.row0[s] = b.row0[s]; a.context[s] = b.context[s]; }
     a.row0[b.n_seq] = b.row0[b.n_seq];
     const int vec = 16 / elt;

@@ -4,8 +4,6 @@
 
 namespace dyspec {
 
-constexpr int kAppendTokens = 4;                 // tokens of a workgroup at most
-
 struct AppendArgs {
     const void *q, *k, *v;
     void *q_out, *k_out, *k_pages, *v_pages;     // k_out: nullptr or the rotated keys as dense rows
@@ -14,12 +12,14 @@ struct AppendArgs {
     long long q_stride, k_stride, v_stride, page_stride;         // elements
     int table_stride, page_shift, n_pages;
     int Hq, Hkv, d, half, interleaved;           // Hq 0: no queries
-    int total, tokens;                           // tokens of the call, of a workgroup
+    int total;                                   // tokens of the call
+    int per_head, units;                         // units of a head, of a token; of a workgroup (the launcher's)
+    uint32_t share, per_head_magic;              // x / per_head = hi(x * magic), per_head 1: x
     int n_seq;
     int row0[DYSPEC_MAX_SEQ + 1], context[DYSPEC_MAX_SEQ];
 };
 // `wide`: rows, strides and dims allow 16-byte pieces
-hipError_t launch_kv_append(AppendArgs a, int dtype, bool wide, hipStream_t stream);
+hipError_t launch_kv_append(const AppendArgs& a, int dtype, bool wide, hipStream_t stream);
 
 struct KeepArgs {
     char *k_pages, *v_pages;

@@ -9,104 +9,125 @@ namespace dyspec {
 //
 // Pair i of a head is turned by the angle pos * inv_freq[i].  The product of a position and an fp32 frequency is exact in 64
 // bits, and so is kept in turns to 2^-53 of its size; the fraction of a turn, in [-1/2, 1/2], is what goes to 32 bits, so far
-// positions lose nothing.  A workgroup computes the sines of its tokens once, for all heads, into LDS.
+// positions lose nothing.
 //
 // A unit is VEC pairs: two pieces of VEC elements, which one thread reads, turns and writes, so that a tensor may be rotated in
-// place.  Units past the rotated dims, and those of V, are copied.
-constexpr int kAppendThreads = 256;
+// place.  Units past the rotated dims, and those of V, are copied.  A workgroup has one token (with few tokens a share of one's
+// units).  A thread asks for its first unit before it looks anything up, so that the trips to memory for the page, the
+// frequencies and the rows overlap; the sines are computed once a workgroup, for all heads, into LDS.
+constexpr int kAppendThreads = 256, kAppendBatch = 2;
+static_assert(kAppendThreads >= 128, "a thread per pair of a head");
 
 template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Piece { T e[VEC]; };
 
 template <typename T, int VEC>
-__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a)
+__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs)
 {
-    extern __shared__ float2 turn[];                       // [tokens][half]: cos, sin
-    __shared__ long long place[kAppendTokens];             // element offset of a token's row in the pool, -1: no page
-    const int t0 = blockIdx.x * a.tokens, count = min(a.tokens, a.total - t0);
-    for (int x = threadIdx.x; x < count * max(a.half, 1); x += kAppendThreads) {
-        const int t = a.half > 0 ? x / a.half : x, i = x - t * a.half;
-        const int row = t0 + t;
-        int s = 0;
-        while (s + 1 < a.n_seq && row >= a.row0[s + 1]) ++s;
-        const int local = row - a.row0[s];
-        if (a.half > 0) {
-            const long long pos = (long long)a.context[s] + (a.rel_pos ? a.rel_pos[row] : local);
-            const double turns = (double)pos * (double)a.inv_freq[i] * 0.15915494309189533577;    // 1 / 2 pi
-            float sn, cs;
-            sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
-            turn[x] = make_float2(cs, sn);
-        }
-        if (i == 0) {
-            const int at = a.context[s] + local;
-            const unsigned page = (unsigned)a.table[(long long)s * a.table_stride + (at >> a.page_shift)];
-            place[t] = page < (unsigned)a.n_pages ? (long long)page * a.page_stride + (long long)(at & ((1 << a.page_shift) - 1)) * a.Hkv * a.d : -1;
-        }
-    }
-    __syncthreads();
+    const AppendArgs& a = *(const AppendArgs*)(__attribute__((address_space(4))) const AppendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    __shared__ float2 turn[128];                           // cos, sin
     typedef Piece<T, VEC> piece;
-    const int heads = a.Hq + 2 * a.Hkv, per_head = (a.d + 2 * VEC - 1) / (2 * VEC), turned = a.half / VEC;
-    for (int x = threadIdx.x; x < count * heads * per_head; x += kAppendThreads) {
-        const int u = x % per_head, y = x / per_head;
-        const int head = y % heads, t = y / heads;
-        const bool is_q = head < a.Hq, is_v = head >= a.Hq + a.Hkv;
-        const int hh = is_q ? head : is_v ? head - a.Hq - a.Hkv : head - a.Hq;
-        const T* const src = (is_q ? static_cast<const T*>(a.q) + (t0 + t) * a.q_stride
-                                   : is_v ? static_cast<const T*>(a.v) + (t0 + t) * a.v_stride
-                                          : static_cast<const T*>(a.k) + (t0 + t) * a.k_stride) + (long long)hh * a.d;
-        const bool turns = !is_v && u < turned;
-        const int at0 = turns && !a.interleaved ? u * VEC : 2 * u * VEC;
-        const int at1 = turns && !a.interleaved ? a.half + u * VEC : at0 + VEC;
-        piece p0 = *reinterpret_cast<const piece*>(src + at0), p1;
-        if (at1 < a.d) p1 = *reinterpret_cast<const piece*>(src + at1);
-        if (turns) {
-            const float2* const cs = turn + t * a.half + u * VEC;
-            if (a.interleaved) {
+    const int token = blockIdx.x, tid = threadIdx.x;
+    const int half = a.half, d = a.d, Hq = a.Hq, Hkv = a.Hkv;
+    const bool apart = !a.interleaved;
+    struct Unit { int head, at0, at1; piece p0, p1; };
+    auto fetch = [&](Unit& w, uint32_t x) __attribute__((always_inline)) {
+        w.head = a.per_head_magic ? (int)__umulhi(x, a.per_head_magic) : (int)x;
+        const int u = (int)x - w.head * a.per_head, h = w.head;
+        const bool turns = h < Hq + Hkv && u * VEC < half;
+        w.at0 = turns && apart ? u * VEC : 2 * u * VEC;
+        w.at1 = turns && apart ? half + u * VEC : w.at0 + VEC;
+        const T* const src = (h < Hq ? static_cast<const T*>(a.q) + token * a.q_stride + (long long)h * d
+                              : h < Hq + Hkv ? static_cast<const T*>(a.k) + token * a.k_stride + (long long)(h - Hq) * d
+                                             : static_cast<const T*>(a.v) + token * a.v_stride + (long long)(h - Hq - Hkv) * d);
+        w.p0 = *reinterpret_cast<const piece*>(src + w.at0);
+        if (w.at1 < d) w.p1 = *reinterpret_cast<const piece*>(src + w.at1);
+    };
+    long long row = -1;                                    // element offset of the token's row in the pool, -1: no page
+    auto finish = [&](Unit& w) __attribute__((always_inline)) {
+        const bool is_q = w.head < Hq, is_v = w.head >= Hq + Hkv;
+        if (!is_v && w.at0 < (apart ? half : 2 * half)) {
+            const float2* const cs = turn + (apart ? w.at0 : w.at0 / 2);
+            if (apart) {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {            // pair e: elements 2e and 2e + 1 of both pieces end to end
-                    T* const lo = 2 * e < VEC ? &p0.e[2 * e] : &p1.e[2 * e - VEC];
-                    T* const hi = 2 * e + 1 < VEC ? &p0.e[2 * e + 1] : &p1.e[2 * e + 1 - VEC];
-                    const float u0 = (float)*lo, u1 = (float)*hi;
-                    *lo = (T)(u0 * cs[e].x - u1 * cs[e].y);
-                    *hi = (T)(u0 * cs[e].y + u1 * cs[e].x);
+                for (int e = 0; e < VEC; ++e) {
+                    const float x = (float)w.p0.e[e], y = (float)w.p1.e[e];
+                    w.p0.e[e] = (T)(x * cs[e].x - y * cs[e].y);
+                    w.p1.e[e] = (T)(x * cs[e].y + y * cs[e].x);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float u0 = (float)p0.e[e], u1 = (float)p1.e[e];
-                    p0.e[e] = (T)(u0 * cs[e].x - u1 * cs[e].y);
-                    p1.e[e] = (T)(u0 * cs[e].y + u1 * cs[e].x);
+                for (int e = 0; e < VEC; ++e) {            // pair e: elements 2e and 2e + 1 of both pieces end to end
+                    T& lo = 2 * e < VEC ? w.p0.e[(2 * e) % VEC] : w.p1.e[(2 * e) % VEC];
+                    T& hi = 2 * e + 1 < VEC ? w.p0.e[(2 * e + 1) % VEC] : w.p1.e[(2 * e + 1) % VEC];
+                    const float x = (float)lo, y = (float)hi;
+                    lo = (T)(x * cs[e].x - y * cs[e].y);
+                    hi = (T)(x * cs[e].y + y * cs[e].x);
                 }
             }
         }
-        auto leave = [&](T* dst) {
-            *reinterpret_cast<piece*>(dst + at0) = p0;
-            if (at1 < a.d) *reinterpret_cast<piece*>(dst + at1) = p1;
+        auto leave = [&](T* dst) __attribute__((always_inline)) {
+            *reinterpret_cast<piece*>(dst + w.at0) = w.p0;
+            if (w.at1 < d) *reinterpret_cast<piece*>(dst + w.at1) = w.p1;
         };
         if (is_q) {
-            leave(static_cast<T*>(a.q_out) + ((long long)(t0 + t) * a.Hq + hh) * a.d);
+            leave(static_cast<T*>(a.q_out) + ((long long)token * Hq + w.head) * d);
         } else {
-            if (place[t] >= 0) leave(static_cast<T*>(is_v ? a.v_pages : a.k_pages) + place[t] + (long long)hh * a.d);
-            if (!is_v && a.k_out) leave(static_cast<T*>(a.k_out) + ((long long)(t0 + t) * a.Hkv + hh) * a.d);
+            const int h = is_v ? w.head - Hq - Hkv : w.head - Hq;
+            if (row >= 0) leave(static_cast<T*>(is_v ? a.v_pages : a.k_pages) + row + (long long)h * d);
+            if (!is_v && a.k_out) leave(static_cast<T*>(a.k_out) + ((long long)token * Hkv + h) * d);
         }
+    };
+    const uint32_t end = min((uint32_t)a.units, (blockIdx.y + 1) * a.share);
+    uint32_t x = blockIdx.y * a.share + tid;
+    Unit first;
+    const bool some = x < end;
+    if (some) fetch(first, x);
+    // ---- the token's sequence (lanes ask one each), its place, its angles
+    const int lane = tid & 63;
+    const int s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(token >= (lane < a.n_seq ? a.row0[lane] : 0x7fffffff))) - 1;
+    const int C = a.context[s], local = token - a.row0[s], at = C + local;
+    const unsigned page = (unsigned)a.table[(long long)s * a.table_stride + (at >> a.page_shift)];
+    if (tid < half) {
+        const long long pos = (long long)C + (a.rel_pos ? a.rel_pos[token] : local);
+        const double turns = (double)pos * (double)a.inv_freq[tid] * 0.15915494309189533577;      // 1 / 2 pi
+        float sn, cs;
+        sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
+        turn[tid] = make_float2(cs, sn);
+    }
+    if (page < (unsigned)a.n_pages) row = (long long)page * a.page_stride + (long long)(at & ((1 << a.page_shift) - 1)) * Hkv * d;
+    __syncthreads();
+    if (some) finish(first);
+    for (x += kAppendThreads; x < end; x += kAppendBatch * kAppendThreads) {
+        Unit w[kAppendBatch];
+#pragma unroll
+        for (int y = 0; y < kAppendBatch; ++y)
+            if (x + y * kAppendThreads < end) fetch(w[y], x + y * kAppendThreads);
+#pragma unroll
+        for (int y = 0; y < kAppendBatch; ++y)
+            if (x + y * kAppendThreads < end) finish(w[y]);
     }
 }
 
-template <typename T>
-static void launch_append(const AppendArgs& a, bool wide, int blocks, hipStream_t stream)
+template <typename T, int VEC>
+static hipError_t launch_append(AppendArgs a, hipStream_t stream)
 {
-    const size_t lds = (size_t)a.tokens * a.half * sizeof(float2);
-    if (wide) kv_append_kernel<T, 16 / (int)sizeof(T)><<<blocks, kAppendThreads, lds, stream>>>(a);
-    else kv_append_kernel<T, 1><<<blocks, kAppendThreads, lds, stream>>>(a);
+    a.per_head = (a.d + 2 * VEC - 1) / (2 * VEC);
+    a.units = a.per_head * (a.Hq + 2 * a.Hkv);
+    // few tokens: up to a workgroup per 256 units, so that about two workgroups a CU share the work
+    const uint32_t cuts = max(1u, min(512u / (uint32_t)a.total, (uint32_t)(a.units + kAppendThreads - 1) / kAppendThreads));
+    a.share = ((a.units + cuts - 1) / cuts + kAppendThreads - 1) / kAppendThreads * kAppendThreads;
+    // x / n as hi(x * magic), exact while x * n < 2^32: at most 24576 heads of 128 units
+    a.per_head_magic = a.per_head == 1 ? 0u : (uint32_t)((1ull << 32) / a.per_head + 1);
+    const dim3 grid(a.total, (a.units + a.share - 1) / a.share);
+    kv_append_kernel<T, VEC><<<grid, kAppendThreads, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
-hipError_t launch_kv_append(AppendArgs a, int dtype, bool wide, hipStream_t stream)
+hipError_t launch_kv_append(const AppendArgs& a, int dtype, bool wide, hipStream_t stream)
 {
     if (a.total == 0) return hipSuccess;
-    a.tokens = a.total <= 1024 ? 1 : kAppendTokens;
-    const int blocks = (a.total + a.tokens - 1) / a.tokens;
-    if (dtype == DYSPEC_F32) launch_append<float>(a, wide, blocks, stream);
-    else launch_append<__bf16>(a, wide, blocks, stream);
-    return hipGetLastError();
+    if (dtype == DYSPEC_F32) return wide ? launch_append<float, 4>(a, stream) : launch_append<float, 1>(a, stream);
+    return wide ? launch_append<__bf16, 8>(a, stream) : launch_append<__bf16, 1>(a, stream);
 }
 
 // ---- keep
@@ -114,44 +135,51 @@ hipError_t launch_kv_append(AppendArgs a, int dtype, bool wide, hipStream_t stre
 // Row C + 1 + i of a sequence takes row C + accepted[i].  A path's rows ascend and the root is row 0, so accepted[i] > i: a row
 // is only ever read from its own place or from behind every place written before, and a thread that moves its 16-byte column
 // eight rows at a time (all eight read before the first is written) needs no copy of the rows and no other thread.
+// Lane l of a wave looks up the l-th move of the eight, so that the list, the page numbers and the rows are three trips to memory.
 constexpr int kKeepThreads = 128, kKeepBatch = 8;
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 
 template <typename V>
-__global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs a)
+__global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs)
 {
-    const int s = blockIdx.y, N = a.row0[s + 1] - a.row0[s], C = a.context[s];
-    const int n = min(a.n_accepted[s], N - 1);
-    const int col = blockIdx.x * kKeepThreads + threadIdx.x;
-    if (col >= a.row_pieces || n <= 0) return;
-    const int layer = blockIdx.z >> 1;
-    char* const pool = (blockIdx.z & 1 ? a.v_pages : a.k_pages) + layer * a.layer_bytes + (long long)col * (int)sizeof(V);
+    const KeepArgs& a = *(const KeepArgs*)(__attribute__((address_space(4))) const KeepArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    const int s = blockIdx.y, first = a.row0[s], N = a.row0[s + 1] - first, C = a.context[s];
+    if (N < 2) return;
+    const int lane = threadIdx.x & 63, col = blockIdx.x * kKeepThreads + threadIdx.x;
+    const bool mine = col < a.row_pieces;
+    char* const pool = (blockIdx.z & 1 ? a.v_pages : a.k_pages) + (blockIdx.z >> 1) * a.layer_bytes + (long long)col * (int)sizeof(V);
     const int* const table = a.table + (long long)s * a.table_stride;
-    auto offset = [&](int at) -> long long {
-        const unsigned page = (unsigned)table[at >> a.page_shift];
-        return page < (unsigned)a.n_pages ? (long long)page * a.page_bytes + (long long)(at & ((1 << a.page_shift) - 1)) * a.row_bytes : -1;
-    };
+    const int page_mask = (1 << a.page_shift) - 1;
+    auto listed = [&](int i0) { return a.accepted[first + min(i0 + (lane & (kKeepBatch - 1)), N - 2)]; };
+    int from = listed(0);                                          // (with the count: it does not wait for that)
+    const int n = min(a.n_accepted[s], N - 1);
     for (int i0 = 0; i0 < n; i0 += kKeepBatch) {
+        const int i = i0 + (lane & (kKeepBatch - 1));
+        long long src = -1, dst = -1;                              // byte offsets of this lane's move
+        if (i < n && from > i + 1 && from < N) {                   // (from == i + 1: in place already)
+            const unsigned p = (unsigned)table[(C + from) >> a.page_shift], q = (unsigned)table[(C + 1 + i) >> a.page_shift];
+            if (p < (unsigned)a.n_pages && q < (unsigned)a.n_pages) {
+                src = p * a.page_bytes + ((C + from) & page_mask) * a.row_bytes;
+                dst = q * a.page_bytes + ((C + 1 + i) & page_mask) * a.row_bytes;
+            }
+        }
+        if (i0 + kKeepBatch < n) from = listed(i0 + kKeepBatch);
+        auto of_lane = [](long long x, int l) {
+            return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) | (unsigned)__builtin_amdgcn_readlane((int)x, l));
+        };
         V v[kKeepBatch];
         long long to[kKeepBatch];
 #pragma unroll
         for (int x = 0; x < kKeepBatch; ++x) {
-            const int i = min(i0 + x, n - 1);
-            const int from = a.accepted[a.row0[s] + i];
-            to[x] = -1;
-            if (i0 + x < n && from > i + 1 && from < N) {          // from == i + 1: in place already
-                const long long src = offset(C + from);
-                if (src >= 0) {
-                    to[x] = offset(C + 1 + i);
-                    v[x] = *reinterpret_cast<const V*>(pool + src);
-                }
-            }
+            const long long at = of_lane(src, x);
+            to[x] = of_lane(dst, x);
+            if (at >= 0 && mine) v[x] = *reinterpret_cast<const V*>(pool + at);
         }
 #pragma unroll
         for (int x = 0; x < kKeepBatch; ++x)
-            if (to[x] >= 0) *reinterpret_cast<V*>(pool + to[x]) = v[x];
+            if (to[x] >= 0 && mine) *reinterpret_cast<V*>(pool + to[x]) = v[x];
     }
 }
 
