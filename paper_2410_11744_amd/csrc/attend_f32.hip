@@ -18,13 +18,14 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kF32Waves = 4;
 
-template <typename T, int DP>
-__global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, int row_waves)
+template <typename T, int DP, bool Paged>
+__global__ __launch_bounds__(64 * kF32Waves, DP <= 128 ? 2 : 1) void attend_f32_kernel(AttendArgs, int row_waves)
 {
     const AttendArgs& a = attend_args_here();
     typedef typename Four<T>::raw raw;
     constexpr int NS = DP / 16, NB = DP / 64;
-    constexpr int KB = DP <= 128 ? 32 : 16, N16 = KB / 16;         // keys of a step
+    constexpr int KB = DP <= 128 ? 32 : 16, N16 = KB / 16, RUNS = KB / 8;      // keys of a step; runs of eight keys lie each within a page
+    constexpr int kAhead = 64 / RUNS;                                          // steps whose page numbers the lanes hold
     __shared__ float merge_area[kF32Waves - 1][64 * (16 * NB + 2)];
     __shared__ int flag;
 
@@ -32,10 +33,10 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
     const int R = 16 * row_waves, key_waves = kF32Waves / row_waves;
-    const int wq = wave % row_waves, wk = wave / row_waves;
+    const int wq = wave & (row_waves - 1), wk = row_waves == 1 ? wave : 0;
     const AttendItem it = attend_item(a, blockIdx.x, R);
     const AttendSeq& s = it.s;
-    const int rows = a.G * s.N, r0 = it.block * R;
+    const int d = a.d, rows = a.G * s.N, r0 = it.block * R;
     const int r = r0 + 16 * wq + n, rc = min(r, rows - 1);
     const int j = div_G(a, rc), h = it.kvh * a.G + (rc - j * a.G);
     const int end = s.C + div_G(a, min(r0 + R, rows) - 1) + 1;     // keys that some row of the block may see
@@ -43,17 +44,20 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, 
     if (it.part >= n_parts) return;
     const int k_begin = s.parts > 1 ? it.part * s.share : 0, k_end = s.parts > 1 ? min(end, k_begin + s.share) : end;
     const int last = k_end - 1;
+    const int full = a.mask ? s.C : s.C + div_G(a, min(r0 + 16 * wq, rows - 1)) + 1;       // keys before this one are every row's of the wave
     const int size = (int)sizeof(T);
-    const char* const kp = a.k + (long long)it.kvh * a.d * size;
-    const char* const vp = a.v + (long long)it.kvh * a.d * size;
+    const long long k_stride = a.k_stride, v_stride = a.v_stride, page_bytes = a.page_bytes;
+    const char* const kp = a.k + (long long)it.kvh * d * size;
+    const char* const vp = a.v + (long long)it.kvh * d * size;
+    const float c2 = a.c2;
 
     // Q: dims 16s + 4g .. of query n; a piece past head_dim is zero here and in K
     float4 q[NS];
-    const char* const qrow = a.q + (long long)(s.row0 + j) * a.q_stride + (long long)h * a.d * size;
+    const char* const qrow = a.q + (long long)(s.row0 + j) * a.q_stride + (long long)h * d * size;
 #pragma unroll
     for (int x = 0; x < NS; ++x) {
         const int dim = 16 * x + 4 * g;
-        q[x] = dim < a.d ? Four<T>::wide(*reinterpret_cast<const raw*>(qrow + dim * size)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        q[x] = dim < d ? Four<T>::wide(*reinterpret_cast<const raw*>(qrow + dim * size)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     floatx4 acc[NB][4];
 #pragma unroll
@@ -62,84 +66,99 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, 
         for (int c = 0; c < 4; ++c) acc[b][c] = floatx4{ 0.0f, 0.0f, 0.0f, 0.0f };
     float m = kLowest, l = 0.0f;
 
-    // 16 keys from key16 on are two runs of eight rows, each within a page; rows past the last key repeat it
-    auto runs = [&](int key16, long long stride, int (&first)[2], long long (&off)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            first[u] = min(key16 + 8 * u, last) & ~7;
-            off[u] = key_offset(a, s, first[u], stride);
+    // page numbers of this wave's steps i0 .. i0 + kAhead - 1: lane RUNS (i - i0) + u has run u's
+    const int first_key = k_begin + KB * wk, key_step = KB * key_waves;
+    const int page_shift = a.page_shift, page_mask = (1 << page_shift) - 1;
+    auto fetch_pages = [=, &a](int i0) __attribute__((always_inline)) -> uint32_t {
+        const int key = min(first_key + key_step * (i0 + lane / RUNS) + 8 * (lane % RUNS), last);
+        return min((uint32_t)a.table[(long long)s.id * a.table_stride + (key >> page_shift)], (uint32_t)a.n_pages - 1u);
+    };
+    uint32_t pages = 0u;
+    if constexpr (Paged) pages = fetch_pages(0);
+    // Row of key key0 + off (of run u_lo where low, else of the next one) of step i; keys past the last one repeat it.
+    auto row_of = [=](const char* base, long long stride, uint32_t window, int i, int key0, int off, int u_lo, bool low) __attribute__((always_inline)) -> const char* {
+        const int key = min(key0 + off, last);
+        if constexpr (Paged) {
+            const uint32_t p0 = (uint32_t)__builtin_amdgcn_readlane((int)window, RUNS * (i & (kAhead - 1)) + u_lo);
+            const uint32_t p1 = (uint32_t)__builtin_amdgcn_readlane((int)window, RUNS * (i & (kAhead - 1)) + u_lo + 1);
+            const long long b0 = (long long)p0 * page_bytes, b1 = (long long)p1 * page_bytes;
+            return base + (low ? b0 : b1) + (key & page_mask) * stride;
+        } else {
+            return base + (s.row0 + key) * stride;
         }
     };
-    auto load_k = [&](int key0, raw (&kr)[N16][NS]) {
+    auto load_k = [=](raw (&kr)[N16][NS], uint32_t window, int i, int key0) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < N16; ++b) {
-            int first[2];
-            long long off[2];
-            runs(key0 + 16 * b, a.k_stride, first, off);
-            const int key = min(key0 + 16 * b + n, last);
-            const char* const row = kp + (n < 8 ? off[0] + (key - first[0]) * a.k_stride : off[1] + (key - first[1]) * a.k_stride);
+            const char* const row = row_of(kp, k_stride, window, i, key0, 16 * b + n, 2 * b, n < 8);
 #pragma unroll
             for (int x = 0; x < NS; ++x) {
                 const int dim = 16 * x + 4 * g;
-                kr[b][x] = *reinterpret_cast<const raw*>(row + (dim < a.d ? dim : 0) * size);
+                kr[b][x] = *reinterpret_cast<const raw*>(row + (dim < d ? dim : 0) * size);
             }
         }
     };
     raw kr[N16][NS];
-    int key0 = k_begin + KB * wk;
-    if (key0 < k_end) load_k(key0, kr);
-    for (; key0 < k_end; key0 += KB * key_waves) {
-        // V: dims 64b + 4n .. of keys 4g + i
+    int key0 = first_key;
+    if (key0 < k_end) load_k(kr, pages, 0, key0);
+    for (int i = 0; key0 < k_end; ++i, key0 += key_step) {
+        // V: dims 64b + 4n .. of keys 4g + x
         raw vr[N16][4][NB];
-#pragma unroll
-        for (int b = 0; b < N16; ++b) {
-            int first[2];
-            long long off[2];
-            runs(key0 + 16 * b, a.v_stride, first, off);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = min(key0 + 16 * b + 4 * g + i, last);
-                const char* const row = vp + (g < 2 ? off[0] + (key - first[0]) * a.v_stride : off[1] + (key - first[1]) * a.v_stride);
-#pragma unroll
-                for (int x = 0; x < NB; ++x) {
-                    const int dim = 64 * x + 4 * n;
-                    vr[b][i][x] = *reinterpret_cast<const raw*>(row + (dim < a.d ? dim : 0) * size);
-                }
-            }
-        }
-        floatx4 S[N16];
-#pragma unroll
-        for (int b = 0; b < N16; ++b) {
-            S[b] = floatx4{ 0.0f, 0.0f, 0.0f, 0.0f };
-#pragma unroll
-            for (int x = 0; x < NS; ++x) {
-                float4 k = Four<T>::wide(kr[b][x]);
-                if (DP > a.d && 16 * x + 4 * g >= a.d) k = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x, q[x].x, S[b], 0, 0, 0);
-                S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.y, q[x].y, S[b], 0, 0, 0);
-                S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.z, q[x].z, S[b], 0, 0, 0);
-                S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w, q[x].w, S[b], 0, 0, 0);
-            }
-        }
-        const int next = key0 + KB * key_waves;
-        if (next < k_end) load_k(next, kr);
-        // scores of keys a row does not see: -inf, whatever K holds there
-        uint32_t seen = seen_bits(a, s, j, key0);
-        if (k_end - key0 < KB) seen &= (1u << (k_end - key0)) - 1u;
-        float up = m;
 #pragma unroll
         for (int b = 0; b < N16; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!((seen >> (16 * b + 4 * g + i)) & 1u)) S[b][i] = -INFINITY;
-                up = fmaxf(up, S[b][i]);
+            for (int x = 0; x < 4; ++x) {
+                const char* const row = row_of(vp, v_stride, pages, i, key0, 16 * b + 4 * g + x, 2 * b, g < 2);
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+                    const int dim = 64 * y + 4 * n;
+                    vr[b][x][y] = *reinterpret_cast<const raw*>(row + (dim < d ? dim : 0) * size);
+                }
             }
+        floatx4 S[N16];                                            // (the blocks' chains in turn: a dependent MFMA waits for its accumulator)
+#pragma unroll
+        for (int b = 0; b < N16; ++b) S[b] = floatx4{ 0.0f, 0.0f, 0.0f, 0.0f };
+#pragma unroll
+        for (int x = 0; x < NS; ++x) {
+            float4 k[N16];
+#pragma unroll
+            for (int b = 0; b < N16; ++b) {
+                k[b] = Four<T>::wide(kr[b][x]);
+                if (16 * x + 16 > d && 16 * x + 4 * g >= d) k[b] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int b = 0; b < N16; ++b) S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b].x, q[x].x, S[b], 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < N16; ++b) S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b].y, q[x].y, S[b], 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < N16; ++b) S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b].z, q[x].z, S[b], 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < N16; ++b) S[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[b].w, q[x].w, S[b], 0, 0, 0);
+        }
+        if (key0 + key_step < k_end) {
+            if constexpr (Paged)
+                if (((i + 1) & (kAhead - 1)) == 0) pages = fetch_pages(i + 1);
+            load_k(kr, pages, i + 1, key0 + key_step);
+        }
+        // scores of keys a row does not see: -inf, whatever K holds there
+        if (key0 + KB > full || key0 + KB > k_end) {
+            uint32_t seen = seen_bits(a, s, j, key0);
+            if (k_end - key0 < KB) seen &= (1u << (k_end - key0)) - 1u;
+#pragma unroll
+            for (int b = 0; b < N16; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (!((seen >> (16 * b + 4 * g + x)) & 1u)) S[b][x] = -INFINITY;
+        }
+        float up = m;
+#pragma unroll
+        for (int b = 0; b < N16; ++b) up = fmaxf(fmaxf(fmaxf(S[b][0], S[b][1]), fmaxf(S[b][2], S[b][3])), up);
         up = fmaxf(up, __shfl_xor(up, 16, kWave));
         up = fmaxf(up, __shfl_xor(up, 32, kWave));
-        const float f = exp2f((m - up) * a.c2);
-        m = up;
-        l *= f;
-        if (__any(f != 1.0f)) {
+        if (__any(up != m)) {
+            const float f = __builtin_amdgcn_exp2f((m - up) * c2);
+            m = up;
+            l *= f;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -148,16 +167,16 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, 
 #pragma unroll
         for (int b = 0; b < N16; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = S[b][i] == -INFINITY ? 0.0f : exp2f((S[b][i] - m) * a.c2);
+            for (int x = 0; x < 4; ++x) {
+                const float p = S[b][x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((S[b][x] - m) * c2);
                 l += p;
 #pragma unroll
-                for (int x = 0; x < NB; ++x) {
-                    const float4 v = Four<T>::wide(vr[b][i][x]);
-                    acc[x][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x, p, acc[x][0], 0, 0, 0);
-                    acc[x][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.y, p, acc[x][1], 0, 0, 0);
-                    acc[x][2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.z, p, acc[x][2], 0, 0, 0);
-                    acc[x][3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w, p, acc[x][3], 0, 0, 0);
+                for (int y = 0; y < NB; ++y) {
+                    const float4 v = Four<T>::wide(vr[b][x][y]);
+                    acc[y][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x, p, acc[y][0], 0, 0, 0);
+                    acc[y][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.y, p, acc[y][1], 0, 0, 0);
+                    acc[y][2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.z, p, acc[y][2], 0, 0, 0);
+                    acc[y][3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.w, p, acc[y][3], 0, 0, 0);
                 }
             }
     }
@@ -238,19 +257,23 @@ __global__ __launch_bounds__(64 * kF32Waves) void attend_f32_kernel(AttendArgs, 
     if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<T, kSlotF32, 0>(a, it, n_parts, R, 64 * kF32Waves);
 }
 
-template <typename T>
+template <typename T, bool Paged>
 static void launch_f32(const AttendArgs& a, int row_waves, int blocks, hipStream_t stream)
 {
-    if (a.d <= 64) attend_f32_kernel<T, 64><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else if (a.d <= 128) attend_f32_kernel<T, 128><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else if (a.d <= 192) attend_f32_kernel<T, 192><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else attend_f32_kernel<T, 256><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    if (a.d <= 64) attend_f32_kernel<T, 64, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 128) attend_f32_kernel<T, 128, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 192) attend_f32_kernel<T, 192, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else attend_f32_kernel<T, 256, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
 }
 
 hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream)
 {
-    if (dtype == DYSPEC_F32) launch_f32<float>(a, row_waves, items * a.Hkv, stream);
-    else launch_f32<__bf16>(a, row_waves, items * a.Hkv, stream);
+    const int blocks = items * a.Hkv;
+    if (dtype == DYSPEC_F32) {
+        if (a.table) launch_f32<float, true>(a, row_waves, blocks, stream); else launch_f32<float, false>(a, row_waves, blocks, stream);
+    } else {
+        if (a.table) launch_f32<__bf16, true>(a, row_waves, blocks, stream); else launch_f32<__bf16, false>(a, row_waves, blocks, stream);
+    }
     return hipGetLastError();
 }
 
