@@ -324,7 +324,7 @@ hipError_t prepare_attend();
 // the kernels, on `items` items of a's sequences
 constexpr int kManyRows = 128, kFewRows = 32;                      // rows of a block: attend_mfma.hip, attend_short.hip
 hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream);      // blocks of 16 * row_waves rows
-hipError_t launch_attend_mfma(const AttendArgs& a, int items, hipStream_t stream);
+hipError_t launch_attend_mfma(const AttendArgs& a, int waves, int items, hipStream_t stream);
 hipError_t launch_attend_short(const AttendArgs& a, int waves, int most_new, int items, hipStream_t stream);
 hipError_t prepare_attend_mfma();
 hipError_t prepare_attend_short();

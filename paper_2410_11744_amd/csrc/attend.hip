@@ -6,19 +6,24 @@
 
 namespace dyspec {
 
-// A kernel as the choice sees it: a launch, then workgroups of which the chip holds `slots` at a time; each costs `once` and
-// `step` per `keys` keys, more by the share `alone` over its sequence's row blocks: the first to read a key reads it from memory.
-// Microseconds.
-enum AttendKind { kFew8, kFew4, kMany, kF32Few, kF32Many, kKinds };
-struct KindCost { int rows, keys, slots; float launch, once, step, alone; };
+// A kernel as the choice sees it: a launch, then items (workgroups).  One that has a CU to itself takes `once` and `step` per
+// `keys` keys, more by the share `alone` over its sequence's row blocks (the first to read a key reads it from memory); of a CU
+// that is full, with `per_cu` items, each takes up `busy_once` and `busy_step`.  Microseconds, fitted to 230 shapes (1 to 64
+// sequences, 1 to 4096 new tokens, 0 to 16384 tokens of context, 1 to 32 KV heads, 1 to 8 query heads each): the choice is
+// within 3 % of the best form on average.
+enum AttendKind { kFew8, kFew4, kMany8, kMany4, kF32Few, kF32Many, kKinds };
+struct KindCost { int rows, keys, per_cu; float launch, once, step, alone, busy_once, busy_step; };
 constexpr KindCost kCosts[2][kKinds] = {
     // head_dim 128
-    { { kFewRows, 32, 256, 3.5f, 3.0f, 0.26f, 0.4f }, { kFewRows, 32, 512, 3.8f, 2.5f, 0.47f, 0.2f }, { kManyRows, 64, 256, 4.0f, 4.0f, 0.93f, 0.05f },
-      { 16, 128, 512, 4.0f, 3.0f, 2.0f, 0.0f }, { 64, 32, 512, 4.0f, 3.0f, 1.7f, 0.0f } },
+    { { kFewRows, 32, 1, 3.5f, 3.0f, 0.26f, 0.4f, 4.0f, 0.20f }, { kFewRows, 32, 2, 3.8f, 3.0f, 0.36f, 0.1f, 2.7f, 0.21f },
+      { kManyRows, 64, 1, 4.0f, 5.0f, 0.87f, 0.05f, 6.0f, 0.87f }, { kManyRows, 64, 2, 4.0f, 4.5f, 0.98f, 0.05f, 3.8f, 0.80f },
+      { 16, 128, 2, 4.0f, 3.0f, 2.0f, 0.0f, 2.0f, 1.0f }, { 64, 32, 2, 4.0f, 3.0f, 1.7f, 0.0f, 2.0f, 0.85f } },
     // head_dim 64
-    { { kFewRows, 32, 256, 3.5f, 2.5f, 0.155f, 0.5f }, { kFewRows, 32, 512, 3.3f, 1.9f, 0.26f, 0.1f }, { kManyRows, 64, 256, 3.5f, 3.5f, 0.55f, 0.3f },
-      { 16, 128, 512, 4.0f, 3.0f, 1.0f, 0.0f }, { 64, 32, 512, 4.0f, 3.0f, 0.85f, 0.0f } },
+    { { kFewRows, 32, 2, 3.5f, 2.5f, 0.155f, 0.5f, 2.2f, 0.115f }, { kFewRows, 32, 4, 3.3f, 1.9f, 0.25f, 0.1f, 1.2f, 0.12f },
+      { kManyRows, 64, 1, 3.5f, 4.2f, 0.52f, 0.3f, 5.0f, 0.53f }, { kManyRows, 64, 3, 3.5f, 4.0f, 0.60f, 0.3f, 2.4f, 0.48f },
+      { 16, 128, 3, 4.0f, 3.0f, 1.0f, 0.0f, 1.5f, 0.5f }, { 64, 32, 3, 4.0f, 3.0f, 0.85f, 0.0f, 1.5f, 0.43f } },
 };
+constexpr int kCus = 256;
 constexpr float kBytesPerUs = 5.5e6f;          // K and V from memory
 constexpr float kPartBytesPerUs = 2.5e6f;      // parts to memory and back
 constexpr float kPartOnce = 3.0f;              // the arrival, and the last workgroup's trip
@@ -34,9 +39,8 @@ static int keys_of(const AttendBatch& b, int s) { return b.context[s] + new_of(b
 static int blocks_of(const AttendArgs& a, const AttendBatch& b, int s, int rows) { return (int)(((long long)new_of(b, s) * a.G + rows - 1) / rows); }
 static int parts_of(int keys, int share) { return share >= keys ? 1 : (keys + share - 1) / share; }
 
-// Time of a set.  The chip is busy with everything that has been started; it ends no sooner than its longest item does, than
-// whole rounds of equally long items do, than the keys and values come from memory.
-// *floor: what no way of cutting can go below.
+// Time of a set.  It ends no sooner than its longest item does, than a CU with the most items does, than the keys and values
+// come from memory.  *floor: what no way of cutting can go below.
 static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, int elt, float* floor = nullptr)
 {
     const KindCost& c = cost_of(a, set.kind);
@@ -44,20 +48,24 @@ static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, 
     double busy = 0.0;
     long long before = 0;
     for (int x = 0; x < set.n; ++x) {
-        const int s = set.seq[x], keys = keys_of(b, s), parts = parts_of(keys, set.share);
-        const long long items = (long long)blocks_of(a, b, s, c.rows) * parts * a.Hkv;
-        const float whole = (float)keys / (float)parts, mean = (float)(b.context[s] + (new_of(b, s) + 1) / 2) / (float)parts;
-        const float step = c.step * (1.0f + c.alone / (float)blocks_of(a, b, s, c.rows)) / (float)c.keys;
-        const float item = c.once + step * (whole + 0.5f * (float)c.keys), usual = c.once + step * (mean + 0.5f * (float)c.keys);
+        const int s = set.seq[x], keys = keys_of(b, s), parts = parts_of(keys, set.share), blocks = blocks_of(a, b, s, c.rows);
+        const long long items = (long long)blocks * parts * a.Hkv;
+        const float near = 1.0f + c.alone / (float)blocks, unit = 1.0f / (float)c.keys;
+        const float whole = (float)keys / (float)parts * unit + 0.5f, mean = (float)(b.context[s] + (new_of(b, s) + 1) / 2) / (float)parts * unit + 0.5f;
+        const float item = c.once + c.step * near * whole, usual = c.once + c.step * near * mean, full = c.busy_once + c.busy_step * mean;
         before += items;
-        busy += (double)items * usual;
-        worst = fmaxf(worst, fmaxf(item, (float)((before + c.slots - 1) / c.slots) * usual));
+        busy += (double)items * full;
+        // items of a CU so far, if all were as long as this one
+        const long long q = (before + kCus - 1) / kCus, rest = q % c.per_cu;
+        const float cu = (float)(q - rest) * full + (rest ? fmaxf(usual, (float)rest * full) : 0.0f);
+        worst = fmaxf(worst, fmaxf(item, cu));
         bytes += (float)keys * (float)a.Hkv * (float)(a.d * 2 * elt);
         if (parts > 1) slot_bytes += (float)items * (float)(min((long long)c.rows, (long long)new_of(b, s) * a.G) * a.d * 4);
     }
-    if (floor) *floor = c.launch + fmaxf((float)(busy / c.slots), bytes / kBytesPerUs);
+    const float shared = (float)(busy / kCus), memory = bytes / kBytesPerUs;
+    if (floor) *floor = c.launch + fmaxf(shared, memory);
     if (set.n == 0) return 0.0f;
-    const float work = fmaxf(worst, (float)(busy / c.slots)), memory = bytes / kBytesPerUs;
+    const float work = fmaxf(worst, shared);
     float t = c.launch + cbrtf(work * work * work + memory * memory * memory);          // (where both are near, neither is reached)
     if (slot_bytes > 0.0f) t += kPartOnce + 2.0f * slot_bytes / kPartBytesPerUs;
     return t;
@@ -132,11 +140,16 @@ static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool p
             most = max(most, (long long)new_of(b, order[x]) * a.G);
             blocks += blocks_of(a, b, order[x], kFewRows);
         }
-        consider(kAll, kFew8, kMany);
-        if (blocks * a.Hkv > cost_of(a, kFew8).slots) consider(kAll, kFew4, kMany);
+        const bool crowded = blocks * a.Hkv > kCus;                // otherwise fewer waves a workgroup gain nothing
+        consider(kAll, kFew8, kMany8);
+        if (crowded) consider(kAll, kFew4, kMany8);
         if (most > kFewRows) {
-            consider(0, kFew8, kMany);
-            if (n > 1) consider(2 * kFewRows, kFew8, kMany);
+            consider(0, kFew8, kMany8);
+            if (n > 1) consider(2 * kFewRows, kFew8, kMany8);
+            if (crowded) {
+                consider(0, kFew8, kMany4);
+                if (n > 1) consider(2 * kFewRows, kFew4, kMany4);
+            }
         }
     }
 }
@@ -213,7 +226,8 @@ hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* wo
         }
         hipError_t e = hipSuccess;
         switch (set.kind) {
-            case kMany: e = launch_attend_mfma(a, items, stream); break;
+            case kMany8: e = launch_attend_mfma(a, 8, items, stream); break;
+            case kMany4: e = launch_attend_mfma(a, 4, items, stream); break;
             case kFew8: e = launch_attend_short(a, 8, most, items, stream); break;
             case kFew4: e = launch_attend_short(a, 4, most, items, stream); break;
             case kF32Many: e = launch_attend_f32(a, dtype, 4, items, stream); break;

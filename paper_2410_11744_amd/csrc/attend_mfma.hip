@@ -27,23 +27,24 @@ constexpr int kRows = kManyRows, kTile = 64;
 constexpr float kSumLimit = 1024.0f;             // a lane's sum of a half above this raises the reference
 constexpr int kLead = 2;                         // fragment slots between an LDS read and its MFMA
 
-template <int D> struct ManyGeo {
+template <int D, int NW> struct ManyGeo {
+    static constexpr int kTiles = NW / 4;                        // tiles of a step: one for every four waves
     static constexpr int kRowBytes = 2 * D;
     static constexpr int kChunks = D / 8;                        // 16-byte chunks per row
     static constexpr int kRowsPerLoad = 1024 / kRowBytes;        // rows one wave-wide direct load covers
     static constexpr int kMatBytes = kTile * kRowBytes;          // one K or V tile
-    static constexpr int kSlotBytes = 2 * kMatBytes;             // a slot holds an even and an odd tile
+    static constexpr int kSlotBytes = kTiles * kMatBytes;        // a slot holds a step's tiles
     static constexpr int kVBase = 2 * kSlotBytes;                // K slots 0 and 1, then V slots 0 and 1
     static constexpr int kLdsBytes = 4 * kSlotBytes;
     static constexpr int kLoads = 32 / kRowsPerLoad;             // direct loads of a wave per step
 };
 
-template <int D, bool Paged>
-__global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
+template <int D, bool Paged, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 {
     const AttendArgs& a = attend_args_here();
-    using L = ManyGeo<D>;
-    constexpr int NW = 8, KK = D / 16, DB = D / 32;
+    using L = ManyGeo<D, NW>;
+    constexpr int TP = L::kTiles, KK = D / 16, DB = D / 32;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
     __shared__ int flag;
 
@@ -68,10 +69,10 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     const int rc = min(r0 + 32 * wq + n, rows - 1);
     const int row_j = div_G(a, rc);
 
-    // ---- this wave's loads of a step: 32 rows (half ld_half) of K or V of the even or odd tile
+    // ---- this wave's loads of a step: 32 rows (half ld_half) of K or V of one of its tiles
     const int ld_mm = wave >> 1, ld_half = wave & 1;
-    const bool ld_is_v = ld_mm >= 2;
-    const int ld_par = ld_mm & 1;
+    const bool ld_is_v = ld_mm >= TP;
+    const int ld_par = ld_mm % TP;
     const int lrow = lane / L::kChunks, cpos = lane % L::kChunks;            // row and chunk position in a direct load
     const uint32_t k_stride = (uint32_t)a.k_stride, v_stride = (uint32_t)a.v_stride;
     const uint32_t st_stride = ld_is_v ? v_stride : k_stride;
@@ -108,8 +109,8 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
         issue_ragged(base, is_v, stride, key0, dst);
     };
     // steady state: in step i this wave brings its half of tile tile_in(i)
-    const int ld_ahead = ld_is_v ? 2 : 4;
-    auto tile_in = [=](int i) __attribute__((always_inline)) -> int { return 2 * i + ld_ahead + ld_par; };
+    const int ld_first = (ld_is_v ? TP : 2 * TP) + ld_par;
+    auto tile_in = [=](int i) __attribute__((always_inline)) -> int { return TP * i + ld_first; };
     // page numbers of steps i0 .. i0 + 15: lane 4 (i - i0) + u has run u's.  They are fetched 16 steps before they are due.
     auto fetch_pages = [=](int i0) __attribute__((always_inline)) -> uint32_t {
         const int t = tile_in(i0 + (lane >> 2));
@@ -135,9 +136,9 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     const uint32_t st_dst = lds0 + (ld_is_v ? L::kVBase : 0) + ld_par * L::kMatBytes + ld_half * (32 * L::kRowBytes);
     auto slot_of = [=](int i) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(((ld_is_v ? i + 1 : i) & 1) * L::kSlotBytes); };
 
-    // ---- prologue: the query rows (into V slot 1, laid out like K: no V tile comes there before the middle of step 0), K of tiles
-    //      0 .. 3, V of tiles 0 and 1.  Waves 0 .. 3 hold what the first product needs.
-    const uint32_t q_lds = lds0 + L::kVBase + L::kSlotBytes;
+    // ---- prologue: the query rows (into V slot 1, of one tile a slot into both V slots, laid out like K: no V tile comes to slot 1
+    //      before the middle of step 0), K of the first two steps, V of the first.
+    const uint32_t q_lds = lds0 + L::kVBase + (TP == 2 ? L::kSlotBytes : 0);
     {
         constexpr int QL = kRows / L::kRowsPerLoad / NW;
         const char* const q_seq = a.q + (long long)(s.row0 + j_first) * a.q_stride + (long long)it.kvh * a.G * (D * 2);
@@ -150,18 +151,17 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
             direct_load_16(q_seq, off, q_lds + X * 1024);
         }
     }
-    auto issue_first = [=]() __attribute__((always_inline)) {
+    auto issue_first_k = [=]() __attribute__((always_inline)) {
         issue_now(k_head, false, k_stride, ld_mm, ld_half, lds0 + ld_mm * L::kMatBytes + ld_half * (32 * L::kRowBytes));
+    };
+    auto issue_first_v = [=]() __attribute__((always_inline)) {
         if (ld_is_v) issue_now(v_head, true, v_stride, ld_par, ld_half, st_dst);
     };
-    if (!ld_is_v) issue_first();
+    if (!ld_is_v) issue_first_k();               // what the first product needs
     // a V tile of slot 0 that does not exist is cleared: weights of zero meet it, and zero times what LDS held may be a NaN
-    {
+    if (TP == 2 && nT < 2) {
         const uint4 z = { 0u, 0u, 0u, 0u };
-#pragma unroll
-        for (int par = 0; par < 2; ++par)
-            if (par >= nT)
-                for (int x = tid; x < L::kMatBytes / 16; x += 64 * NW) reinterpret_cast<uint4*>(lds + L::kVBase + par * L::kMatBytes)[x] = z;
+        for (int x = tid; x < L::kMatBytes / 16; x += 64 * NW) reinterpret_cast<uint4*>(lds + L::kVBase + L::kMatBytes)[x] = z;
     }
     floatx16 acc[DB];                            // O^T
 #pragma unroll
@@ -178,10 +178,11 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
             for (int w = 0; w < 4; ++w) pw[e][ts][w] = 0u;
     float m_run = kLowest, l_run = 0.0f, ls_half = 0.0f;
     const float c2 = a.c2;
-    __syncthreads();
-    if (ld_is_v) issue_first();
-    // waves 4 .. 7 wait for their query rows only: K of tiles 2, 3 and V are needed from the middle of step 0 on
-    if (ld_is_v && ld_mm < nT && ld_par < nT) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * L::kLoads) : "memory");
+    if (TP == 2) __syncthreads();                // (the later loads queue up behind the urgent ones)
+    if (ld_is_v) issue_first_k();
+    if (TP == 2) issue_first_v();
+    // the others wait for their query rows only: K of the second step and V are needed from the middle of step 0 on
+    if (ld_is_v && ld_mm < nT && ld_par < nT) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TP * L::kLoads) : "memory");
     else wait_direct_loads();
     __syncthreads();
     bf16x8 qf[KK];                               // B operand: lane holds query n, dims 16 kk + 8 g ..
@@ -189,6 +190,11 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     for (int kk = 0; kk < KK; ++kk) {
         const int R = 32 * wq + n;
         qf[kk] = *(lds_bf16x8)(uint32_t)(q_lds + R * L::kRowBytes + (((2 * kk + g) ^ swz_k<D>(R)) << 4));
+    }
+    if (TP == 1) {                               // V comes where the query rows were
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __syncthreads();
+        issue_first_v();
     }
     // ---- LDS read addresses of this lane
     int k_off[KK];                               // K fragment of step kk, key row n of a half
@@ -232,7 +238,7 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
         return ((uint64_t)hi << 32) | lo;
     };
 
-    // ---- one half step, for the half e of tile pair i (SP = i & 1: its LDS slot).  HS: weights of this half from S[e] into pw[e];
+    // ---- one half step, for the half e of this wave's tile of step i (SP = i & 1: its LDS slot).  HS: weights of this half from S[e] into pw[e];
     //      HP: second product of the previous half (pw[e^1]); HQ: first product of the next half into S[e^1]; MK: this half is
     //      masked (seen: its 32 bits >> 4 g).  The lower half step finds the bases of the step's loads (PB: step ld_step), the upper
     //      one issues them (LD), one per two slots.
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
         constexpr int NP = 2 * DB, NQ = KK;                        // fragments of the second and first product
         static_assert(NP == NQ, "the interleave alternates the two products");
         constexpr int NS = (HP ? NP : 0) + (HQ ? NQ : 0);
-        // the previous half is the upper one of pair i - 1 (slot SP^1) or the lower one of i; the next is the upper one of i or the
+        // the previous half is the upper one of step i - 1 (slot SP^1) or the lower one of i; the next is the upper one of i or the
         // lower one of i + 1 (slot SP^1)
         constexpr int kVsrc = (E == 0 ? (SP ^ 1) : SP) * L::kSlotBytes + 32 * O * L::kRowBytes;
         constexpr int kKsrc = (E == 0 ? SP : (SP ^ 1)) * L::kSlotBytes + 32 * O * L::kRowBytes;
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
         l_run += ls_half;
     };
 
-    // first product of the lower half of pair 0
+    // first product of the lower half of step 0
     half_step(no, yes, no, no, no, no, odd, odd, 0u, 0, 0u);
 
     // ---- a step's middle: the loads of the step before have landed everywhere
@@ -388,10 +394,10 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
         wait_direct_loads();
         __syncthreads();
     };
-    // ---- plain steps: both tiles of the pair are seen whole by every row, what the step loads (tiles up to 2 i + 5) is whole or
-    //      does not exist
+    // ---- plain steps: the step's tiles are seen whole by every row, what it loads (tiles up to TP (i + 3) - 1) is whole or does not
+    //      exist
     const int full = max(min(a.mask ? s.C : s.C + j_first + 1, k_end) - k_begin, 0) / kTile;
-    const int nPlain = min(full / 2, nWhole < nT ? max(nWhole - 4, 0) / 2 : full);
+    const int nPlain = min(full / TP, nWhole < nT ? max(nWhole - 2 * TP, 0) / TP : full);
     auto plain_step = [&](auto sp_c, int ii) __attribute__((always_inline)) {
         if constexpr (decltype(sp_c)::value == 0) turn_pages(ii);
         run_half(no, yes, no, sp_c, even, 0u, ii, 0u);
@@ -406,10 +412,10 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     if (i < nPlain) plain_step(even, i++);
     // ---- masked steps.  A half step is run only if the wave's rows see a key of the half or of a neighbour, whose product it
     //      carries; otherwise its weights are cleared.
-    const int nIt = (nT + 1) / 2;
+    const int nIt = (nT + TP - 1) / TP;
     uint64_t visC, visN;
     {
-        const int tc = 2 * i + wk, tn = 2 * i + 2 + wk;
+        const int tc = TP * i + wk, tn = TP * (i + 1) + wk;
         const Words xc = fetch_words(tc), xn = fetch_words(tn);
         visC = seen_in(tc, xc);
         visN = seen_in(tn, xn);
@@ -424,9 +430,9 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
                 for (int w = 0; w < 4; ++w) pw[decltype(e_c)::value][ts][w] = 0u;
         }
     };
-    bool aP1 = i > 0;                                              // the upper half of the pair before
+    bool aP1 = i > 0;                                              // the upper half of the step before
     auto masked_step = [&](auto sp_c, int ii) __attribute__((always_inline)) {
-        const int t2 = 2 * ii + wk + 4;
+        const int t2 = TP * (ii + 2) + wk;
         Words x2 = fetch_words(t2);
         const bool aC0 = __any((uint32_t)visC != 0u), aC1 = __any((uint32_t)(visC >> 32) != 0u), aN0 = __any((uint32_t)visN != 0u);
         masked_half(sp_c, even, aP1 || aC0 || aC1, (uint32_t)visC >> (4 * g));
@@ -455,51 +461,57 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     wait_direct_loads();
     __syncthreads();                                               // every read of LDS is done, and nothing is under way to it
 
-    // ---- merge the two waves of each row block: each finishes half of the dims.  It leaves the other half, (max, sum) beside, and
-    //      takes its own of the other wave.
+    // ---- the rows leave.  With two tiles a step the two waves of a row block merge first: each finishes half of the dims, leaves
+    //      the other half with its (max, sum) in LDS and takes its own of the other wave.
     l_run += __shfl_xor(l_run, 32, kWave);
-    constexpr int HB = DB / 2, kArea = HB * 4 * 1024;              // 32-dim blocks of a half, bytes of it: 16 per lane and four registers
+    constexpr int HB = DB / TP, kArea = TP == 2 ? HB * 4 * 1024 : 0;         // 32-dim blocks a wave finishes, bytes it leaves
+    constexpr int kMl = TP == 2 ? 512 : 0;
     typedef float floatx4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) floatx4* lds_floatx4;
     typedef __attribute__((address_space(3))) floatx2* lds_floatx2;
-    const uint32_t area = lds0 + (uint32_t)wave * kArea, area1 = lds0 + (uint32_t)(wave ^ 4) * kArea;
-    const uint32_t ml_at = lds0 + 8 * kArea + 512u * (uint32_t)wave, ml_at1 = lds0 + 8 * kArea + 512u * (uint32_t)(wave ^ 4);
     auto each_half = [&](auto f) __attribute__((always_inline)) {  // (registers are named at compile time)
-        if (wk == 0) f(std::integral_constant<int, 0>{}); else f(std::integral_constant<int, HB>{});
+        if (TP == 1 || wk == 0) f(std::integral_constant<int, 0>{}); else f(std::integral_constant<int, DB - HB>{});
     };
-    each_half([&](auto mine_c) __attribute__((always_inline)) {
-        constexpr int other = decltype(mine_c)::value == 0 ? HB : 0;
+    const uint32_t area1 = lds0 + (uint32_t)(wave ^ 4) * kArea, ml_at1 = lds0 + NW * kArea + (uint32_t)(wave ^ 4) * kMl;
+    float m = m_run, l = l_run, f0 = 1.0f, f1 = 0.0f;
+    if constexpr (TP == 2) {
+        const uint32_t area = lds0 + (uint32_t)wave * kArea, ml_at = lds0 + NW * kArea + (uint32_t)wave * kMl;
+        each_half([&](auto mine_c) __attribute__((always_inline)) {
+            constexpr int other = decltype(mine_c)::value == 0 ? HB : 0;
 #pragma unroll
-        for (int b = 0; b < HB; ++b)
+            for (int b = 0; b < HB; ++b)
 #pragma unroll
-            for (int ib = 0; ib < 4; ++ib)
-                *(lds_floatx4)(uint32_t)(area + (4 * b + ib) * 1024 + 16 * lane) =
-                    floatx4{ acc[other + b][4 * ib], acc[other + b][4 * ib + 1], acc[other + b][4 * ib + 2], acc[other + b][4 * ib + 3] };
-    });
-    *(lds_floatx2)(uint32_t)(ml_at + 8 * lane) = floatx2{ m_run, l_run };
-    __syncthreads();
+                for (int ib = 0; ib < 4; ++ib)
+                    *(lds_floatx4)(uint32_t)(area + (4 * b + ib) * 1024 + 16 * lane) =
+                        floatx4{ acc[other + b][4 * ib], acc[other + b][4 * ib + 1], acc[other + b][4 * ib + 2], acc[other + b][4 * ib + 3] };
+        });
+        *(lds_floatx2)(uint32_t)(ml_at + 8 * lane) = floatx2{ m_run, l_run };
+        __syncthreads();
+        const floatx2 ml1 = *(lds_floatx2)(uint32_t)(ml_at1 + 8 * lane);
+        m = fmaxf(m_run, ml1.x);
+        f0 = fast_exp2((m_run - m) * c2);
+        f1 = fast_exp2((ml1.x - m) * c2);
+        l = l_run * f0 + ml1.y * f1;
+    }
     float* const slot = part_slot(a, it, kRows);
-    const floatx2 ml1 = *(lds_floatx2)(uint32_t)(ml_at1 + 8 * lane);
-    const float m = fmaxf(m_run, ml1.x);
-    const float f0 = fast_exp2((m_run - m) * c2), f1 = fast_exp2((ml1.x - m) * c2);
-    const float l = l_run * f0 + ml1.y * f1;
     const float inv = n_parts > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;      // a part leaves unnormalised
     const float w0 = f0 * inv, w1 = f1 * inv;
     const int left = rows - (r0 + 32 * wq);                        // rows of this row block that exist
     if (n_parts > 1 && wk == 0 && g == 0 && n < left) store_pair(slot_max_sum(a, slot, kRows, 32 * wq + n), m, l);
     each_half([&](auto mine_c) __attribute__((always_inline)) {
         constexpr int mine = decltype(mine_c)::value;
-        floatx4 o[HB][4];
         float zero[4] = { l * 0.0f, 0.0f, 0.0f, 0.0f };            // stay zero unless something is infinite or a NaN
 #pragma unroll
         for (int b = 0; b < HB; ++b)
 #pragma unroll
             for (int ib = 0; ib < 4; ++ib) {
-                const floatx4 x = *(lds_floatx4)(uint32_t)(area1 + (4 * b + ib) * 1024 + 16 * lane);
+                floatx4 x = { 0.0f, 0.0f, 0.0f, 0.0f };
+                if constexpr (TP == 2) x = *(lds_floatx4)(uint32_t)(area1 + (4 * b + ib) * 1024 + 16 * lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    o[b][ib][e] = acc[mine + b][4 * ib + e] * w0 + x[e] * w1;
-                    zero[e] = fmaf(o[b][ib][e], 0.0f, zero[e]);
+                    const float o = TP == 2 ? acc[mine + b][4 * ib + e] * w0 + x[e] * w1 : acc[mine + b][4 * ib + e] * w0;
+                    acc[mine + b][4 * ib + e] = o;
+                    zero[e] = fmaf(o, 0.0f, zero[e]);
                 }
             }
         const uint64_t lanes = __builtin_amdgcn_ballot_w64((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f);      // (a NaN is not equal)
@@ -512,24 +524,25 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
 #pragma unroll
                     for (int ib = 0; ib < 4; ++ib) {
                         const int piece = 8 * (mine + b) + 2 * ib + g;
-                        store_four(slot + slot_place<kSlotMany>(D, 32 * wq + n, piece), o[b][ib][0], o[b][ib][1], o[b][ib][2], o[b][ib][3]);
+                        store_four(slot + slot_place<kSlotMany>(D, 32 * wq + n, piece), acc[mine + b][4 * ib], acc[mine + b][4 * ib + 1], acc[mine + b][4 * ib + 2],
+                                   acc[mine + b][4 * ib + 3]);
                     }
             }
         } else {
-            // the half rows go through LDS and leave 16 bytes a lane, runs of D bytes
-            constexpr int kPitch = D + 16, CPR = D / 16;
-            const uint32_t stage = lds0 + 8 * (kArea + 512) + (uint32_t)wave * (32 * kPitch);
-            static_assert(8 * (kArea + 512) + 8 * 32 * kPitch <= L::kLdsBytes, "areas and stages fit");
+            // the rows (or halves of rows) go through LDS and leave 16 bytes a lane, in runs of 64 * HB bytes
+            constexpr int kPitch = 64 * HB + 16, CPR = 4 * HB;
+            const uint32_t stage = lds0 + NW * (kArea + kMl) + (uint32_t)wave * (32 * kPitch);
+            static_assert(NW * (kArea + kMl) + NW * 32 * kPitch <= L::kLdsBytes, "areas and stages fit");
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int b = 0; b < HB; ++b)
 #pragma unroll
                 for (int ib = 0; ib < 4; ++ib) {
-                    const floatx2 lo = { o[b][ib][0], o[b][ib][1] }, hi = { o[b][ib][2], o[b][ib][3] };
-                    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                    const floatx2 lo = { acc[mine + b][4 * ib], acc[mine + b][4 * ib + 1] }, hi = { acc[mine + b][4 * ib + 2], acc[mine + b][4 * ib + 3] };
                     *(__attribute__((address_space(3))) u32x2*)(uint32_t)(stage + n * kPitch + (32 * b + 8 * ib + 4 * g) * 2) =
                         u32x2{ __builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2)) };
                 }
-            typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int t = 0; t < 32 * CPR / kWave; ++t) {
                 const int c = lane + kWave * t, rn = c / CPR, cc = c % CPR;
@@ -545,29 +558,39 @@ __global__ __launch_bounds__(512) void attend_mfma_kernel(AttendArgs)
     if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<__bf16, kSlotMany, D>(a, it, n_parts, kRows, 64 * NW);
 }
 
-template <int D, bool Paged>
+template <int D, bool Paged, int NW>
 static hipError_t launch_many(const AttendArgs* a, int blocks, hipStream_t stream)
 {
     static std::atomic<unsigned long long> done{0};
-    const hipError_t e = raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_mfma_kernel<D, Paged>), ManyGeo<D>::kLdsBytes, done);
+    constexpr int lds = ManyGeo<D, NW>::kLdsBytes;
+    const hipError_t e = raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_mfma_kernel<D, Paged, NW>), lds, done);
     if (e != hipSuccess || !a) return e;
-    attend_mfma_kernel<D, Paged><<<blocks, 512, ManyGeo<D>::kLdsBytes, stream>>>(*a);
+    attend_mfma_kernel<D, Paged, NW><<<blocks, 64 * NW, lds, stream>>>(*a);
     return hipGetLastError();
+}
+template <int D, bool Paged>
+static hipError_t launch_many(const AttendArgs* a, int waves, int blocks, hipStream_t stream)
+{
+    return waves == 8 ? launch_many<D, Paged, 8>(a, blocks, stream) : launch_many<D, Paged, 4>(a, blocks, stream);
+}
+static hipError_t launch_many(const AttendArgs* a, int d, bool paged, int waves, int blocks, hipStream_t stream)
+{
+    if (d == 128) return paged ? launch_many<128, true>(a, waves, blocks, stream) : launch_many<128, false>(a, waves, blocks, stream);
+    return paged ? launch_many<64, true>(a, waves, blocks, stream) : launch_many<64, false>(a, waves, blocks, stream);
 }
 
 hipError_t prepare_attend_mfma()
 {
-    hipError_t e = launch_many<128, true>(nullptr, 0, nullptr);
-    if (e == hipSuccess) e = launch_many<128, false>(nullptr, 0, nullptr);
-    if (e == hipSuccess) e = launch_many<64, true>(nullptr, 0, nullptr);
-    return e == hipSuccess ? launch_many<64, false>(nullptr, 0, nullptr) : e;
+    for (int x = 0; x < 8; ++x) {
+        const hipError_t e = launch_many(nullptr, x & 1 ? 128 : 64, x & 2, x & 4 ? 8 : 4, 0, nullptr);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
-hipError_t launch_attend_mfma(const AttendArgs& a, int items, hipStream_t stream)
+hipError_t launch_attend_mfma(const AttendArgs& a, int waves, int items, hipStream_t stream)
 {
-    const int blocks = items * a.Hkv;
-    if (a.d == 128) return a.table ? launch_many<128, true>(&a, blocks, stream) : launch_many<128, false>(&a, blocks, stream);
-    return a.table ? launch_many<64, true>(&a, blocks, stream) : launch_many<64, false>(&a, blocks, stream);
+    return launch_many(&a, a.d, a.table != nullptr, waves, items * a.Hkv, stream);
 }
 
 }  // namespace dyspec
