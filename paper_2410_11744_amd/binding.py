@@ -711,6 +711,9 @@ def _attend_workspace(device: int, raw: int, where, nbytes: int, prepared: bool)
     """A paged_attn workspace, its head zero.  Calls of one stream run in order and share one; a prepared call, and a call that a
     graph records, has its own, because whatever runs beside the graph may use the stream's."""
     torch = _torch
+    if torch._C._cuda_getDevice() != device:
+        with torch.cuda.device(device):
+            return _attend_workspace(device, raw, where, nbytes, prepared)
     with where:
         capturing = torch._C._cuda_isCurrentStreamCapturing()
         if not prepared and not capturing:

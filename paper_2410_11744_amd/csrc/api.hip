@@ -125,7 +125,7 @@ dyspec_status dyspec_init(void)
 {
     void* scratch_address = nullptr;
     if (prepare_tree_attn() != hipSuccess || prepare_build_tree() != hipSuccess || prepare_build_threshold() != hipSuccess || prepare_verify() != hipSuccess ||
-        prepare_reorder() != hipSuccess || prepare_attend() != hipSuccess ||
+        prepare_reorder() != hipSuccess || prepare_attend() != hipSuccess || prepare_kv_cache() != hipSuccess ||
         static_scratch_address(&scratch_address) != hipSuccess)
         return DYSPEC_HIP_ERROR;
     return DYSPEC_OK;
@@ -437,12 +437,14 @@ static dyspec_status check_chunks(const dyspec_batch* b, bool context, int max_n
     return DYSPEC_OK;
 }
 
+constexpr int kMostHeads = 8192, kMostRow = 1 << 20;
+
 static dyspec_status check_heads(int Hq, int Hkv, int d, int dtype)
 {
     if (Hkv < 1 || Hq < 0 || Hq % Hkv != 0) return DYSPEC_BAD_SHAPE;
     if ((dtype != DYSPEC_F32 && dtype != DYSPEC_BF16) || d < 4 || d > 256 || d % 4) return DYSPEC_UNSUPPORTED;
     // a token's heads stay below 4 MB: eight rows of a page are addressed with 32-bit offsets; append divides by multiplication
-    if ((long long)max(Hq, Hkv) * d > 1 << 20 || max(Hq, Hkv) > 8192) return DYSPEC_BAD_SHAPE;
+    if (max(Hq, Hkv) > kMostHeads || max(Hq, Hkv) * d > kMostRow) return DYSPEC_BAD_SHAPE;
     return DYSPEC_OK;
 }
 
@@ -491,7 +493,8 @@ dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, i
 {
     AttendBatch b;
     dyspec_status st = check_chunks(batch, true, DYSPEC_MAX_CHUNK, &b);
-    if (st == DYSPEC_OK) st = check_heads(n_kv_heads > 0 ? (n_q_heads + n_kv_heads - 1) / n_kv_heads * n_kv_heads : 1, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK) st = check_heads(n_kv_heads, n_kv_heads, head_dim, dtype);
+    if (st == DYSPEC_OK && (n_q_heads > kMostHeads || (int64_t)n_q_heads * head_dim > kMostRow)) st = DYSPEC_BAD_SHAPE;
     if (st == DYSPEC_OK) st = check_cache(cache, b, n_kv_heads, head_dim, dtype);
     if (st != DYSPEC_OK) return st;
     if (!k || !v || n_q_heads < 0 || (n_q_heads > 0) != (q != nullptr) || (q && !q_out)) return DYSPEC_BAD_ARG;
@@ -550,9 +553,14 @@ size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_
     return attend_workspace_bytes(b, dtype, n_q_heads, n_kv_heads, head_dim);
 }
 
-dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch, const uint64_t* anc_mask,
-                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, float softmax_scale,
-                                void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+static dyspec_status launched(hipError_t e, const AttendForm* form)
+{
+    return e == hipSuccess ? DYSPEC_OK : form && e == hipErrorInvalidValue ? DYSPEC_UNSUPPORTED : DYSPEC_HIP_ERROR;
+}
+
+static dyspec_status paged_attn_common(const AttendForm* form, const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
+                                       const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                       float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     AttendBatch b;
     dyspec_status st = check_chunks(batch, true, anc_mask ? DYSPEC_MAX_NODES : DYSPEC_MAX_CHUNK, &b);
@@ -576,13 +584,20 @@ dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, con
         a.mask = reinterpret_cast<const uint32_t*>(anc_mask);
         a.mask_words = 2 * ((most + 63) / 64);
     }
-    return launch_attend(a, b, dtype, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess
-               ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+    return launched(launch_attend(a, b, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
 }
 
-dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
-                                 const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
-                                 float softmax_scale, void* out, void* hip_stream)
+dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch, const uint64_t* anc_mask,
+                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, float softmax_scale,
+                                void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    return paged_attn_common(nullptr, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
+                             workspace_bytes, hip_stream);
+}
+
+static dyspec_status prompt_attn_common(const AttendForm* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                        int64_t v_stride, const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                        int32_t dtype, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     AttendBatch b;
     dyspec_status st = check_chunks(batch, false, DYSPEC_MAX_CHUNK, &b);
@@ -598,7 +613,36 @@ dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k,
     AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim, softmax_scale);
     a.q = static_cast<const char*>(q); a.k = static_cast<const char*>(k); a.v = static_cast<const char*>(v); a.out = static_cast<char*>(out);
     a.q_stride = q_stride * elt; a.k_stride = k_stride * elt; a.v_stride = v_stride * elt; a.out_stride = q_row * elt;
-    return launch_attend(a, b, dtype, nullptr, 0, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+    return launched(launch_attend(a, b, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
+}
+
+dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                 const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                 float softmax_scale, void* out, void* hip_stream)
+{
+    return prompt_attn_common(nullptr, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out,
+                              nullptr, 0, hip_stream);
+}
+
+// dyspec_paged_attn and dyspec_prompt_attn (with a workspace) launched in a given form: form[0] the kernel, form[1] keys per part (attend.h);
+// DYSPEC_UNSUPPORTED where there is no such form.  Exported, but no part of the interface: tests run cases through kernels that
+// their sizes would not choose.
+dyspec_status dyspec_paged_attn_in_form(const int32_t* form, const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
+                                        const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                        float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!form) return DYSPEC_BAD_ARG;
+    const AttendForm f = { form[0], form[1] };
+    return paged_attn_common(&f, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace, workspace_bytes, hip_stream);
+}
+dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                         int64_t v_stride, const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                         int32_t dtype, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!form) return DYSPEC_BAD_ARG;
+    const AttendForm f = { form[0], form[1] };
+    return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
+                              workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

@@ -317,8 +317,11 @@ __device__ __forceinline__ void leave_exact_rows(const AttendArgs& a, const Atte
 // ---- launches
 struct AttendBatch { int n_seq; int row0[DYSPEC_MAX_SEQ + 1]; int context[DYSPEC_MAX_SEQ]; };
 size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d);
-// `a` without its sequences, which are dealt to the kernels and cut into items (attend.hip)
-hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
+// `a` without its sequences, which are dealt to the kernels and cut into items (attend.hip), or, with a form (tests), all given to
+// one kernel (0 .. 5: few rows, 8 and 4 waves; many rows, 8 and 4 waves; fp32, blocks of 16 and 64 rows), walks cut into shares of
+// that many keys (0: not); hipErrorInvalidValue where there is no such form
+struct AttendForm { int kernel, share; };
+hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream);
 hipError_t prepare_attend();
 
 // the kernels, on `items` items of a's sequences
@@ -328,5 +331,6 @@ hipError_t launch_attend_mfma(const AttendArgs& a, int waves, int items, hipStre
 hipError_t launch_attend_short(const AttendArgs& a, int waves, int most_new, int items, hipStream_t stream);
 hipError_t prepare_attend_mfma();
 hipError_t prepare_attend_short();
+hipError_t prepare_attend_f32();
 
 }  // namespace dyspec

@@ -102,6 +102,28 @@ static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, b
 
 struct Plan { int n; Set set[2]; };
 
+static bool on_bf16_cores(const AttendArgs& a, int dtype)
+{
+    auto pieces = [](const void* p, long long stride) { return reinterpret_cast<size_t>(p) % 16 == 0 && stride % 16 == 0; };
+    return dtype == DYSPEC_BF16 && (a.d == 64 || a.d == 128) && pieces(a.q, a.q_stride) && pieces(a.k, a.k_stride) && pieces(a.v, a.v_stride) &&
+           pieces(a.out, a.out_stride);
+}
+
+// The plan of a form that was asked for: all sequences with one kernel.
+static bool plan_given(const AttendArgs& a, const AttendBatch& b, int dtype, const AttendForm& form, Plan& plan)
+{
+    if (form.kernel < 0 || form.kernel >= kKinds || form.share < 0 || form.share % kUnit) return false;
+    if (form.kernel < kF32Few && !on_bf16_cores(a, dtype)) return false;
+    plan.n = 1;
+    Set& set = plan.set[0];
+    set.kind = (AttendKind)form.kernel;
+    set.share = form.share ? form.share : DYSPEC_MAX_CONTEXT;
+    set.n = 0;
+    for (int s = 0; s < b.n_seq; ++s)
+        if (new_of(b, s) > 0) set.seq[set.n++] = s;
+    return form.share == 0 || counters_of(a, b, set) * (long long)sizeof(unsigned) <= DYSPEC_PAGED_COUNTER_BYTES;
+}
+
 static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool parts, Plan& plan)
 {
     int order[DYSPEC_MAX_SEQ], n = 0;
@@ -111,9 +133,7 @@ static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool p
         for (; at > 0 && keys_of(b, order[at - 1]) < keys_of(b, s); --at) order[at] = order[at - 1];
         order[at] = s;
     }
-    auto pieces = [](const void* p, long long stride) { return reinterpret_cast<size_t>(p) % 16 == 0 && stride % 16 == 0; };
-    const bool bf16 = dtype == DYSPEC_BF16 && (a.d == 64 || a.d == 128) && pieces(a.q, a.q_stride) && pieces(a.k, a.k_stride) &&
-                      pieces(a.v, a.v_stride) && pieces(a.out, a.out_stride);
+    const bool bf16 = on_bf16_cores(a, dtype);
     const int elt = dtype == DYSPEC_BF16 ? 2 : 4;
     // sequences of at most `rows` rows to `few`, the others to `many`; kept if that is the fastest so far
     float best = 0.0f;
@@ -196,19 +216,21 @@ size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, 
     return bytes ? DYSPEC_PAGED_COUNTER_BYTES + bytes : 0;
 }
 
-hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream)
+hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream)
 {
     Plan plan;
     for (int parts = workspace != nullptr; parts >= 0; --parts) {
-        plan_of(a, b, dtype, parts != 0, plan);
+        if (form && !plan_given(a, b, dtype, *form, plan)) return hipErrorInvalidValue;
+        if (!form) plan_of(a, b, dtype, parts != 0, plan);
         size_t need = DYSPEC_PAGED_COUNTER_BYTES;
-        for (int x = 0; x < plan.n && parts; ++x) {
+        for (int x = 0; x < plan.n && (parts || form); ++x) {
             int groups, most;
             long long slots;
             fill(a, b, plan.set[x], &groups, &slots, &most);
             need += (size_t)slots * slot_bytes(a, plan.set[x].kind);
         }
-        if (!parts || need <= workspace_bytes || need == DYSPEC_PAGED_COUNTER_BYTES) break;      // no room: every walk in one piece
+        if (form && need > DYSPEC_PAGED_COUNTER_BYTES && (!workspace || need > workspace_bytes)) return hipErrorInvalidValue;
+        if (!parts || form || need <= workspace_bytes || need == DYSPEC_PAGED_COUNTER_BYTES) break;      // no room: every walk in one piece
     }
     char* slots_at = static_cast<char*>(workspace) + DYSPEC_PAGED_COUNTER_BYTES;
     unsigned* counters = static_cast<unsigned*>(workspace);
@@ -240,8 +262,9 @@ hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, void* wo
 
 hipError_t prepare_attend()
 {
-    const hipError_t e = prepare_attend_mfma();
-    return e == hipSuccess ? prepare_attend_short() : e;
+    hipError_t e = prepare_attend_mfma();
+    if (e == hipSuccess) e = prepare_attend_short();
+    return e == hipSuccess ? prepare_attend_f32() : e;
 }
 
 }  // namespace dyspec

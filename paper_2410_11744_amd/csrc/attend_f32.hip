@@ -277,4 +277,10 @@ hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int 
     return hipGetLastError();
 }
 
+hipError_t prepare_attend_f32()                                    // (asking loads the code)
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, reinterpret_cast<const void*>(&attend_f32_kernel<float, 64, true>));
+}
+
 }  // namespace dyspec

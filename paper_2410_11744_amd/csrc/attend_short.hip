@@ -277,6 +277,7 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
     typedef float floatx4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) floatx4* lds_floatx4;
     typedef __attribute__((address_space(3))) floatx2* lds_floatx2;
+    if (r0 + n < rows)
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll

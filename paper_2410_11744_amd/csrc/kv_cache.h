@@ -31,5 +31,6 @@ struct KeepArgs {
     int row0[DYSPEC_MAX_SEQ + 1], context[DYSPEC_MAX_SEQ];
 };
 hipError_t launch_kv_keep(const KeepArgs& a, int n_layers, hipStream_t stream);
+hipError_t prepare_kv_cache();
 
 }  // namespace dyspec

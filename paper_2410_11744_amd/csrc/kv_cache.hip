@@ -192,4 +192,10 @@ hipError_t launch_kv_keep(const KeepArgs& a, int n_layers, hipStream_t stream)
     return hipGetLastError();
 }
 
+hipError_t prepare_kv_cache()                                      // (asking loads the code)
+{
+    hipFuncAttributes at;
+    return hipFuncGetAttributes(&at, reinterpret_cast<const void*>(&kv_keep_kernel<words4>));
+}
+
 }  // namespace dyspec

@@ -187,3 +187,45 @@ def test_rows_that_are_no_sixteen_bytes_apart(dy):
         want, bound = attend_plain(*(x[a:a + n].double().cpu().numpy() for x in (q, k, v)), visible_rows(n, 0), 0.1, 2.0 ** -8, 2.0 ** -8)
         compare(out[a:a + n].double().cpu().numpy(), want, bound, "strided")
         compare(same[a:a + n].double().cpu().numpy(), want, bound, "dense")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("tree", [False, True], ids=["causal", "tree"])
+def test_a_full_batch_of_sequences_of_every_kind(dy, dtype, d, tree):
+    """64 sequences: without a new token, with one, with a few, with hundreds; without a context, with thousands."""
+    rng = np.random.default_rng(17)
+    new = [int(x) for x in rng.choice([0, 1, 1, 1, 2, 7, 33, 150, 260], 64)]
+    context = [int(x) for x in rng.choice([0, 1, 15, 64, 200, 1000, 2500], 64)]
+    c = Paged(new, context, 4, 2, d, dtype, 16, 23, mask=random_mask(new, 6)[0] if tree else None)
+    out = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev)
+    c.check(out)
+
+
+@pytest.mark.parametrize("dtype,new,context", [(BF16, (1,), (150_001,)), (BF16, (70,), (60_003,)), (BF16, (300, 1), (33_000, 90_000)), (F32, (1, 3), (50_000, 7))])
+def test_long_contexts(dy, dtype, new, context):
+    c = Paged(new, context, 2, 1, 64 if dtype is F32 else 128, dtype, 256, 29)
+    c.check(dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale))
+
+
+def test_a_long_prompt(dy):
+    """20001 tokens: rows from all over it against the plain form."""
+    n, g = 20001, torch.Generator().manual_seed(31)
+    q, k, v = (torch.randn((n, 2, 128), generator=g).to(BF16) for _ in range(3))
+    out = dy.prompt_attn(q.cuda(), k.cuda(), v.cuda(), dy.Batch.from_sizes([n]), 0.1).double().cpu().numpy()
+    rows = np.unique(np.concatenate([np.arange(70), np.random.default_rng(1).integers(0, n, 60), np.arange(n - 70, n)]))
+    seen = np.arange(n)[None] <= rows[:, None]
+    want, bound = attend_plain(q[rows].double().numpy(), k.double().numpy(), v.double().numpy(), seen, 0.1, 2.0 ** -8, 2.0 ** -8)
+    compare(out[rows], want, bound, "rows")
+
+
+@pytest.mark.parametrize("dtype,d,new", [(BF16, 128, 300), (BF16, 128, 20), (BF16, 64, 200), (F32, 64, 100)])
+def test_a_row_that_is_no_number_leaves_the_others_alone(dy, dtype, d, new):
+    c = Paged((new, 3), (100, 40), 4, 2, d, dtype, 16, 41)
+    c.q[new // 2, 1, 7] = math.nan
+    c.q[new // 3, 2] = math.inf
+    out = dy.paged_attn(c.q.cuda(), c.batch, c.cache, c.scale)
+    assert torch.isnan(out[new // 2, 1]).all() and torch.isnan(out[new // 3, 2]).all()
+    c.q[new // 2, 1], c.q[new // 3, 2] = 0, 0
+    out[new // 2, 1] = dy.paged_attn(c.q.cuda(), c.batch, c.cache, c.scale)[new // 2, 1]
+    out[new // 3, 2] = dy.paged_attn(c.q.cuda(), c.batch, c.cache, c.scale)[new // 3, 2]
+    c.check(out)
