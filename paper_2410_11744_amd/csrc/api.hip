@@ -484,6 +484,12 @@ static AttendArgs attend_args(int Hq, int Hkv, int d, float scale)
     return a;
 }
 
+static void sequences(Sequences<DYSPEC_MAX_SEQ>& seq, const AttendBatch& b)
+{
+    for (int s = 0; s < b.n_seq; ++s) { seq.row0[s] = b.row0[s]; seq.context[s] = b.context[s]; }
+    seq.row0[b.n_seq] = b.row0[b.n_seq];
+}
+
 static bool scale_ok(float x) { return x > 0.0f && x <= 3.4e38f; }
 
 dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -506,19 +512,19 @@ dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, i
     if (!aligned(q, elt) || !aligned(k, elt) || !aligned(v, elt) || !aligned(q_out, elt) || !aligned(k_out, elt) || !aligned(rel_pos, 4) || !aligned(inv_freq, 4))
         return DYSPEC_BAD_ARG;
     if ((q && q == q_out && q_stride != q_row) || (k == k_out && k_stride != kv_row)) return DYSPEC_BAD_ARG;      // in place: dense only
-    AppendArgs a;
+    AppendHead a;
+    Sequences<DYSPEC_MAX_SEQ> seq;
     a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_out = k_out; a.k_pages = cache->k; a.v_pages = cache->v;
     a.table = cache->page_table; a.rel_pos = rel_pos; a.inv_freq = inv_freq;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.page_stride = cache->page_stride;
     a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
     a.Hq = q ? n_q_heads : 0; a.Hkv = n_kv_heads; a.d = head_dim; a.half = n_freq; a.interleaved = interleaved != 0;
-    a.total = b.row0[b.n_seq]; a.n_seq = b.n_seq;
-    for (int s = 0; s < b.n_seq; ++s) { a.row0[s] = b.row0[s]; a.context[s] = b.context[s]; }
-    a.row0[b.n_seq] = b.row0[b.n_seq];
+    a.n_seq = b.n_seq;
+    sequences(seq, b);
     const int vec = 16 / elt;
     const bool wide = head_dim % vec == 0 && n_freq % vec == 0 && aligned(k, 16) && aligned(v, 16) && aligned(k_out, 16) && k_stride % vec == 0 &&
                       v_stride % vec == 0 && (!q || (aligned(q, 16) && aligned(q_out, 16) && q_stride % vec == 0));
-    return launch_kv_append(a, dtype, wide, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+    return launch_kv_append(a, seq, dtype, wide, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
 dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int64_t layer_stride, const dyspec_batch* batch,
@@ -533,7 +539,8 @@ dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int
     if (!accepted_nodes || !n_accepted || !aligned(accepted_nodes, 4) || !aligned(n_accepted, 4)) return DYSPEC_BAD_ARG;
     const int elt = dtype == DYSPEC_F32 ? 4 : 2;
     if (n_layers < 1 || n_layers > 32767 || layer_stride < 0 || layer_stride > ((int64_t)1 << 44) || (layer_stride * elt) % 16) return DYSPEC_BAD_SHAPE;
-    KeepArgs a;
+    KeepHead a;
+    Sequences<DYSPEC_MAX_SEQ> seq;
     a.k_pages = static_cast<char*>(cache->k); a.v_pages = static_cast<char*>(cache->v);
     a.table = cache->page_table; a.accepted = accepted_nodes; a.n_accepted = n_accepted;
     a.layer_bytes = layer_stride * elt; a.page_bytes = cache->page_stride * elt; a.row_bytes = (long long)n_kv_heads * head_dim * elt;
@@ -541,9 +548,8 @@ dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int
     a.row_pieces = (int)(a.row_bytes / a.piece_bytes);
     a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
     a.n_seq = b.n_seq;
-    for (int s = 0; s < b.n_seq; ++s) { a.row0[s] = b.row0[s]; a.context[s] = b.context[s]; }
-    a.row0[b.n_seq] = b.row0[b.n_seq];
-    return launch_kv_keep(a, n_layers, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+    sequences(seq, b);
+    return launch_kv_keep(a, seq, n_layers, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
 size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype)

@@ -3,7 +3,19 @@
 // decode step's few hundred KB the trips to it.
 #include "kv_cache.h"
 
+#include "launch.h"
+
 namespace dyspec {
+
+template <typename Args> __device__ __forceinline__ const Args& args_here()      // (read where they are: a copy would go to scratch memory)
+{
+    return *(const Args*)(__attribute__((address_space(4))) const Args*)__builtin_amdgcn_kernarg_segment_ptr();
+}
+template <int S> static void fill(Sequences<S>& to, const Sequences<DYSPEC_MAX_SEQ>& from, int n_seq)
+{
+    for (int s = 0; s < n_seq; ++s) { to.row0[s] = from.row0[s]; to.context[s] = from.context[s]; }
+    to.row0[n_seq] = from.row0[n_seq];
+}
 
 // ---- append
 //
@@ -20,10 +32,10 @@ static_assert(kAppendThreads >= 128, "a thread per pair of a head");
 
 template <typename T, int VEC> struct alignas(VEC * sizeof(T)) Piece { T e[VEC]; };
 
-template <typename T, int VEC>
-__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs)
+template <typename T, int VEC, int S>
+__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs<S>)
 {
-    const AppendArgs& a = *(const AppendArgs*)(__attribute__((address_space(4))) const AppendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    const AppendArgs<S>& a = args_here<AppendArgs<S>>();
     __shared__ float2 turn[128];                           // cos, sin
     typedef Piece<T, VEC> piece;
     const int token = blockIdx.x, tid = threadIdx.x;
@@ -84,8 +96,8 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs)
     if (some) fetch(first, x);
     // ---- the token's sequence (lanes ask one each), its place, its angles
     const int lane = tid & 63;
-    const int s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(token >= (lane < a.n_seq ? a.row0[lane] : 0x7fffffff))) - 1;
-    const int C = a.context[s], local = token - a.row0[s], at = C + local;
+    const int s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(token >= (lane < a.n_seq ? a.seq.row0[lane] : 0x7fffffff))) - 1;
+    const int C = a.seq.context[s], local = token - a.seq.row0[s], at = C + local;
     const unsigned page = (unsigned)a.table[(long long)s * a.table_stride + (at >> a.page_shift)];
     if (tid < half) {
         const long long pos = (long long)C + (a.rel_pos ? a.rel_pos[token] : local);
@@ -108,26 +120,34 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs)
     }
 }
 
-template <typename T, int VEC>
-static hipError_t launch_append(AppendArgs a, hipStream_t stream)
+template <typename T, int VEC, int S>
+static hipError_t launch_append(const AppendHead& head, const Sequences<DYSPEC_MAX_SEQ>& seq, hipStream_t stream)
 {
+    static Kernel kernel(reinterpret_cast<const void*>(&kv_append_kernel<T, VEC, S>));
+    AppendArgs<S> a;
+    static_cast<AppendHead&>(a) = head;
+    fill(a.seq, seq, head.n_seq);
+    const uint32_t total = (uint32_t)seq.row0[head.n_seq];
     a.per_head = (a.d + 2 * VEC - 1) / (2 * VEC);
     a.units = a.per_head * (a.Hq + 2 * a.Hkv);
     // few tokens: up to a workgroup per 256 units, so that about two workgroups a CU share the work
-    const uint32_t cuts = max(1u, min(512u / (uint32_t)a.total, (uint32_t)(a.units + kAppendThreads - 1) / kAppendThreads));
+    const uint32_t cuts = max(1u, min(512u / total, (uint32_t)(a.units + kAppendThreads - 1) / kAppendThreads));
     a.share = ((a.units + cuts - 1) / cuts + kAppendThreads - 1) / kAppendThreads * kAppendThreads;
     // x / n as hi(x * magic), exact while x * n < 2^32: at most 24576 heads of 128 units
     a.per_head_magic = a.per_head == 1 ? 0u : (uint32_t)((1ull << 32) / a.per_head + 1);
-    const dim3 grid(a.total, (a.units + a.share - 1) / a.share);
-    kv_append_kernel<T, VEC><<<grid, kAppendThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    return kernel.launch(dim3(total, (a.units + a.share - 1) / a.share), kAppendThreads, 0, stream, a);
+}
+template <typename T, int VEC>
+static hipError_t launch_append(const AppendHead& head, const Sequences<DYSPEC_MAX_SEQ>& seq, hipStream_t stream)
+{
+    return head.n_seq <= kFewSeq ? launch_append<T, VEC, kFewSeq>(head, seq, stream) : launch_append<T, VEC, DYSPEC_MAX_SEQ>(head, seq, stream);
 }
 
-hipError_t launch_kv_append(const AppendArgs& a, int dtype, bool wide, hipStream_t stream)
+hipError_t launch_kv_append(const AppendHead& a, const Sequences<DYSPEC_MAX_SEQ>& seq, int dtype, bool wide, hipStream_t stream)
 {
-    if (a.total == 0) return hipSuccess;
-    if (dtype == DYSPEC_F32) return wide ? launch_append<float, 4>(a, stream) : launch_append<float, 1>(a, stream);
-    return wide ? launch_append<__bf16, 8>(a, stream) : launch_append<__bf16, 1>(a, stream);
+    if (seq.row0[a.n_seq] == 0) return hipSuccess;
+    if (dtype == DYSPEC_F32) return wide ? launch_append<float, 4>(a, seq, stream) : launch_append<float, 1>(a, seq, stream);
+    return wide ? launch_append<__bf16, 8>(a, seq, stream) : launch_append<__bf16, 1>(a, seq, stream);
 }
 
 // ---- keep
@@ -141,11 +161,11 @@ constexpr int kKeepThreads = 128, kKeepBatch = 8;
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 
-template <typename V>
-__global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs)
+template <typename V, int S>
+__global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs<S>)
 {
-    const KeepArgs& a = *(const KeepArgs*)(__attribute__((address_space(4))) const KeepArgs*)__builtin_amdgcn_kernarg_segment_ptr();
-    const int s = blockIdx.y, first = a.row0[s], N = a.row0[s + 1] - first, C = a.context[s];
+    const KeepArgs<S>& a = args_here<KeepArgs<S>>();
+    const int s = blockIdx.y, first = a.seq.row0[s], N = a.seq.row0[s + 1] - first, C = a.seq.context[s];
     if (N < 2) return;
     const int lane = threadIdx.x & 63, col = blockIdx.x * kKeepThreads + threadIdx.x;
     const bool mine = col < a.row_pieces;
@@ -183,19 +203,31 @@ __global__ __launch_bounds__(kKeepThreads) void kv_keep_kernel(KeepArgs)
     }
 }
 
-hipError_t launch_kv_keep(const KeepArgs& a, int n_layers, hipStream_t stream)
+template <typename V, int S>
+static hipError_t launch_keep(const KeepHead& head, const Sequences<DYSPEC_MAX_SEQ>& seq, int n_layers, hipStream_t stream)
 {
-    if (a.row0[a.n_seq] == 0) return hipSuccess;
-    const dim3 grid((a.row_pieces + kKeepThreads - 1) / kKeepThreads, a.n_seq, 2 * n_layers);
-    if (a.piece_bytes == 16) kv_keep_kernel<words4><<<grid, kKeepThreads, 0, stream>>>(a);
-    else kv_keep_kernel<words2><<<grid, kKeepThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    static Kernel kernel(reinterpret_cast<const void*>(&kv_keep_kernel<V, S>));
+    KeepArgs<S> a;
+    static_cast<KeepHead&>(a) = head;
+    fill(a.seq, seq, head.n_seq);
+    return kernel.launch(dim3((a.row_pieces + kKeepThreads - 1) / kKeepThreads, a.n_seq, 2 * n_layers), kKeepThreads, 0, stream, a);
+}
+template <typename V>
+static hipError_t launch_keep(const KeepHead& head, const Sequences<DYSPEC_MAX_SEQ>& seq, int n_layers, hipStream_t stream)
+{
+    return head.n_seq <= kFewSeq ? launch_keep<V, kFewSeq>(head, seq, n_layers, stream) : launch_keep<V, DYSPEC_MAX_SEQ>(head, seq, n_layers, stream);
+}
+
+hipError_t launch_kv_keep(const KeepHead& a, const Sequences<DYSPEC_MAX_SEQ>& seq, int n_layers, hipStream_t stream)
+{
+    if (seq.row0[a.n_seq] == 0) return hipSuccess;
+    return a.piece_bytes == 16 ? launch_keep<words4>(a, seq, n_layers, stream) : launch_keep<words2>(a, seq, n_layers, stream);
 }
 
 hipError_t prepare_kv_cache()                                      // (asking loads the code)
 {
-    hipFuncAttributes at;
-    return hipFuncGetAttributes(&at, reinterpret_cast<const void*>(&kv_keep_kernel<words4>));
+    hipFunction_t f;
+    return Kernel(reinterpret_cast<const void*>(&kv_keep_kernel<words4, kFewSeq>)).find(&f);
 }
 
 }  // namespace dyspec
