@@ -630,7 +630,8 @@ dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k,
                               nullptr, 0, hip_stream);
 }
 
-// dyspec_paged_attn and dyspec_prompt_attn (with a workspace) launched in a given form: form[0] the kernel, form[1] keys per part (attend.h);
+// dyspec_paged_attn and dyspec_prompt_attn (with a workspace) launched in a given form: form[0] the kernel, form[1] keys per part,
+// form[2] row blocks whose walks stay whole (attend.h);
 // DYSPEC_UNSUPPORTED where there is no such form.  Exported, but no part of the interface: tests run cases through kernels that
 // their sizes would not choose.
 dyspec_status dyspec_paged_attn_in_form(const int32_t* form, const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
@@ -638,7 +639,7 @@ dyspec_status dyspec_paged_attn_in_form(const int32_t* form, const void* q, cons
                                         float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     if (!form) return DYSPEC_BAD_ARG;
-    const AttendForm f = { form[0], form[1] };
+    const AttendForm f = { form[0], form[1], form[2] };
     return paged_attn_common(&f, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace, workspace_bytes, hip_stream);
 }
 dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
@@ -646,7 +647,7 @@ dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int
                                          int32_t dtype, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     if (!form) return DYSPEC_BAD_ARG;
-    const AttendForm f = { form[0], form[1] };
+    const AttendForm f = { form[0], form[1], form[2] };
     return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
                               workspace_bytes, hip_stream);
 }

@@ -13,11 +13,12 @@ namespace dyspec {
 
 constexpr float kLowest = -3.402823466e38f;      // running maximum before the first key
 
-// One sequence of a launch.  Its row blocks (of the kernel's R rows) times `parts` are consecutive items; a workgroup takes one
-// item of one KV head.  Blocks come last row first: under a causal mask the long walks start first.
+// One sequence of a launch, or some row blocks of one.  Its row blocks (of the kernel's R rows) times `parts` are consecutive items;
+// a workgroup takes one item of one KV head.  Blocks come last row first: under a causal mask the long walks start first.
 struct AttendSeq {
     int item0;        // first item
-    int group0;       // first row block, counted over the launch
+    int end_block;    // the first item's row block is the one before this
+    int group0;       // the sequence's first row block, counted over the launch
     int id;           // row of the page table
     int row0;         // first token in q, k, v, out, mask
     int N, C;         // new tokens, tokens before them
@@ -40,7 +41,7 @@ struct AttendArgs {
     int Hq, Hkv, G, d;
     uint32_t g_magic;              // r / G = hi(r * g_magic), G = 1: r
     float c2;                      // softmax scale * log2(e): weights are exp2(c2 * score)
-    int n_seq;
+    int n_seq;                     // entries of the table
     AttendSeq seq[DYSPEC_MAX_SEQ];
 };
 
@@ -52,27 +53,26 @@ __device__ __forceinline__ const AttendArgs& attend_args_here()
 }
 
 // A workgroup's place: block of rows, part of the walk.
-struct AttendItem { AttendSeq s; int kvh, block, part, local; };      // local: the item's number in its sequence
+struct AttendItem { AttendSeq s; int kvh, block, part, local; };      // local: the item's number in its entry
 
 typedef __attribute__((address_space(4))) const int* scalar_ints;
 
-__device__ __forceinline__ AttendItem attend_item(const AttendArgs& a, int index, int rows_per_block)
+__device__ __forceinline__ AttendItem attend_item(const AttendArgs& a, int index)
 {
     AttendItem it;
     const int item = index / a.Hkv;
     it.kvh = index - item * a.Hkv;
     it.s = a.seq[0];
-    if (a.n_seq > 1) {                                     // sequences that start at or before this item
+    if (a.n_seq > 1) {                                     // entries that start at or before this item
         const int lane = threadIdx.x & 63;
         const int at = lane < a.n_seq ? a.seq[lane].item0 : 0x7fffffff;
         it.s = a.seq[__builtin_popcountll(__builtin_amdgcn_ballot_w64(item >= at)) - 1];
     }
     const int local = item - it.s.item0;
     it.local = local;
-    const int blocks = (a.G * it.s.N + rows_per_block - 1) / rows_per_block;
     const int lb = it.s.parts > 1 ? local / it.s.parts : local;
     it.part = local - lb * it.s.parts;
-    it.block = blocks - 1 - lb;
+    it.block = it.s.end_block - 1 - lb;
     return it;
 }
 
@@ -319,8 +319,8 @@ struct AttendBatch { int n_seq; int row0[DYSPEC_MAX_SEQ + 1]; int context[DYSPEC
 size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d);
 // `a` without its sequences, which are dealt to the kernels and cut into items (attend.hip), or, with a form (tests), all given to
 // one kernel (0 .. 5: few rows, 8 and 4 waves; many rows, 8 and 4 waves; fp32, blocks of 16 and 64 rows), walks cut into shares of
-// that many keys (0: not); hipErrorInvalidValue where there is no such form
-struct AttendForm { int kernel, share; };
+// that many keys (0: not) but for those of the first `whole` row blocks; hipErrorInvalidValue where there is no such form
+struct AttendForm { int kernel, share, whole; };
 hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream);
 hipError_t prepare_attend();
 

@@ -10,7 +10,7 @@ namespace dyspec {
 // `keys` keys, more by the share `alone` over its sequence's row blocks (the first to read a key reads it from memory); of a CU
 // that is full, with `per_cu` items, each takes up `busy_once` and `busy_step`.  Microseconds, fitted to 230 shapes (1 to 64
 // sequences, 1 to 4096 new tokens, 0 to 16384 tokens of context, 1 to 32 KV heads, 1 to 8 query heads each): the choice is
-// within 3 % of the best form on average.
+// 1.7 % (head_dim 128) and 3.6 % (64) from the best form on average.
 enum AttendKind { kFew8, kFew4, kMany8, kMany4, kF32Few, kF32Many, kKinds };
 struct KindCost { int rows, keys, per_cu; float launch, once, step, alone, busy_once, busy_step; };
 constexpr KindCost kCosts[2][kKinds] = {
@@ -27,45 +27,70 @@ constexpr int kCus = 256;
 constexpr float kBytesPerUs = 5.5e6f;          // K and V from memory
 constexpr float kPartBytesPerUs = 2.5e6f;      // parts to memory and back
 constexpr float kPartOnce = 3.0f;              // the arrival, and the last workgroup's trip
+constexpr float kTail = 0.6f;                  // of the rounds of what is cut beside whole walks: it fills up the CUs that those leave
 constexpr int kUnit = 128;                     // a share is a multiple of this many keys
 
 static const KindCost& cost_of(const AttendArgs& a, AttendKind k) { return kCosts[a.d <= 64][k]; }
 
-// A set of sequences (indices, longest walks first) for one kernel, walks cut into shares of at most `share` keys.
-struct Set { AttendKind kind; int n, share; int seq[DYSPEC_MAX_SEQ]; };
+// A set of sequences (indices, longest walks first) for one kernel.  Walks are cut into shares of at most `share` keys, but for
+// those of the first `whole` row blocks in the order of the launch, which leave no parts: the blocks of long prompts beside single
+// tokens with long contexts (pieces of prompts of 700 and 331 tokens beside five that decode: 110 -> 87 us), or the first rounds
+// of workgroups, where what is left after them is shared out (40 row blocks of 8 heads over 4700 tokens: 115 -> 109 us).
+struct Set { AttendKind kind; int n, share, whole; int seq[DYSPEC_MAX_SEQ]; };
 
 static int new_of(const AttendBatch& b, int s) { return b.row0[s + 1] - b.row0[s]; }
 static int keys_of(const AttendBatch& b, int s) { return b.context[s] + new_of(b, s); }
 static int blocks_of(const AttendArgs& a, const AttendBatch& b, int s, int rows) { return (int)(((long long)new_of(b, s) * a.G + rows - 1) / rows); }
 static int parts_of(int keys, int share) { return share >= keys ? 1 : (keys + share - 1) / share; }
 
+// Row blocks end - blocks .. end - 1 of a sequence: new tokens `from` .. `to` - 1.
+struct Piece { int s, end, blocks, parts, from, to; };
+
+// The set's pieces in the order of the launch: a sequence each, or two where `whole` ends inside one.
+template <typename F> static void each_piece(const AttendArgs& a, const AttendBatch& b, const Set& set, F f)
+{
+    const int rows = cost_of(a, set.kind).rows;
+    long long left = set.whole;
+    for (int x = 0; x < set.n; ++x) {
+        const int s = set.seq[x], N = new_of(b, s), blocks = blocks_of(a, b, s, rows), uncut = (int)min(left, (long long)blocks), cut = blocks - uncut;
+        left -= uncut;
+        const int border = cut ? min(N, (int)(((long long)cut * rows + a.G - 1) / a.G)) : 0;      // tokens of the blocks that are cut
+        if (uncut) f(Piece{ s, blocks, uncut, 1, border, N });
+        if (cut) f(Piece{ s, cut, cut, parts_of(b.context[s] + border, set.share), 0, border });
+    }
+}
+
 // Time of a set.  It ends no sooner than its longest item does, than a CU with the most items does, than the keys and values
 // come from memory.  *floor: what no way of cutting can go below.
 static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, int elt, float* floor = nullptr)
 {
     const KindCost& c = cost_of(a, set.kind);
-    float worst = 0.0f, bytes = 0.0f, slot_bytes = 0.0f;
-    double busy = 0.0;
-    long long before = 0;
-    for (int x = 0; x < set.n; ++x) {
-        const int s = set.seq[x], keys = keys_of(b, s), parts = parts_of(keys, set.share), blocks = blocks_of(a, b, s, c.rows);
-        const long long items = (long long)blocks * parts * a.Hkv;
-        const float near = 1.0f + c.alone / (float)blocks, unit = 1.0f / (float)c.keys;
-        const float whole = (float)keys / (float)parts * unit + 0.5f, mean = (float)(b.context[s] + (new_of(b, s) + 1) / 2) / (float)parts * unit + 0.5f;
+    float longest = 0.0f, worst = 0.0f, bytes = 0.0f, slot_bytes = 0.0f;
+    double busy = 0.0, head = 0.0;                 // a CU's share of the items, of those before `whole`
+    long long before = 0, blocks_before = 0;
+    each_piece(a, b, set, [&](const Piece& p) {
+        if (blocks_before == set.whole) { head = busy; before = 0; worst = 0.0f; }
+        blocks_before += p.blocks;
+        const int keys = b.context[p.s] + p.to;
+        const long long items = (long long)p.blocks * p.parts * a.Hkv;
+        const float near = 1.0f + c.alone / (float)p.blocks, unit = 1.0f / (float)c.keys;
+        const float whole = (float)keys / (float)p.parts * unit + 0.5f;
+        const float mean = (float)(b.context[p.s] + (p.from + p.to + 1) / 2) / (float)p.parts * unit + 0.5f;
         const float item = c.once + c.step * near * whole, usual = c.once + c.step * near * mean, full = c.busy_once + c.busy_step * mean;
         before += items;
-        busy += (double)items * full;
+        busy += (double)items * full / kCus;
         // items of a CU so far, if all were as long as this one
         const long long q = (before + kCus - 1) / kCus, rest = q % c.per_cu;
         const float cu = (float)(q - rest) * full + (rest ? fmaxf(usual, (float)rest * full) : 0.0f);
+        longest = fmaxf(longest, item);
         worst = fmaxf(worst, fmaxf(item, cu));
-        bytes += (float)keys * (float)a.Hkv * (float)(a.d * 2 * elt);
-        if (parts > 1) slot_bytes += (float)items * (float)(min((long long)c.rows, (long long)new_of(b, s) * a.G) * a.d * 4);
-    }
-    const float shared = (float)(busy / kCus), memory = bytes / kBytesPerUs;
+        if (p.to == new_of(b, p.s)) bytes += (float)keys * (float)a.Hkv * (float)(a.d * 2 * elt);
+        if (p.parts > 1) slot_bytes += (float)items * (float)(min((long long)c.rows, (long long)p.to * a.G) * a.d * 4);
+    });
+    const float shared = (float)busy, memory = bytes / kBytesPerUs;
     if (floor) *floor = c.launch + fmaxf(shared, memory);
     if (set.n == 0) return 0.0f;
-    const float work = fmaxf(worst, shared);
+    const float work = fmaxf(longest, (float)head + fmaxf(head > 0.0 ? kTail * worst : worst, (float)(busy - head)));
     float t = c.launch + cbrtf(work * work * work + memory * memory * memory);          // (where both are near, neither is reached)
     if (slot_bytes > 0.0f) t += kPartOnce + 2.0f * slot_bytes / kPartBytesPerUs;
     return t;
@@ -82,21 +107,51 @@ static long long counters_of(const AttendArgs& a, const AttendBatch& b, const Se
 static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, bool parts)
 {
     set.share = DYSPEC_MAX_CONTEXT;
+    set.whole = 0;
     float floor, best = time_of(a, b, set, elt, &floor);
     if (!parts || set.n == 0 || counters_of(a, b, set) * (long long)sizeof(unsigned) > DYSPEC_PAGED_COUNTER_BYTES / 2) return best;
     if (best < 1.15f * floor) return best;
-    int best_share = set.share;
-    const int longest = keys_of(b, set.seq[0]);
-    constexpr int kTries[] = { 2, 3, 4, 6, 8, 12, 16, 24, 32 };
-    for (int p : kTries) {
-        const int share = ((longest + p - 1) / p + kUnit - 1) / kUnit * kUnit;
-        set.share = share;
-        const float t = time_of(a, b, set, elt);
-        if (t < 0.97f * best) { best = t; best_share = share; }
-        else if (t > 1.3f * best) break;
-        if (share == kUnit) break;
+    Set found = set;
+    auto tries = [&](int longest, long long whole) {
+        constexpr int kTries[] = { 2, 3, 4, 6, 8, 12, 16, 24, 32 };
+        for (int p : kTries) {
+            set.share = ((longest + p - 1) / p + kUnit - 1) / kUnit * kUnit;
+            set.whole = (int)whole;
+            const float t = time_of(a, b, set, elt);
+            if (t < 0.97f * best) { best = t; found = set; }
+            else if (t > 1.3f * best) break;
+            if (set.share == kUnit) break;
+        }
+    };
+    tries(keys_of(b, set.seq[0]), 0);
+    if (cost_of(a, set.kind).rows != kManyRows) { set = found; return best; }
+    // long walks of single blocks beside sequences of many: those whole and first, these cut
+    const int rows = cost_of(a, set.kind).rows;
+    const Set before = set;
+    long long whole = 0;
+    int n = 0, longest_single = 0;
+    for (int single = 0; single < 2; ++single) {
+        for (int x = 0; x < before.n; ++x) {
+            const int blocks = blocks_of(a, b, before.seq[x], rows);
+            if ((blocks == 1) != (single == 1)) continue;
+            set.seq[n++] = before.seq[x];
+            if (!single) whole += blocks;
+        }
+        if (!single && (n == 0 || n == before.n)) break;
+        if (!single) longest_single = n;
     }
-    set.share = best_share;
+    if (longest_single) tries(keys_of(b, set.seq[longest_single]), whole);
+    // what is left after some rounds of a workgroup a CU cut
+    set = before;
+    const long long rounds = counters_of(a, b, set) / kCus;
+    for (long long r = rounds; r >= 1 && r > rounds - 3 && set.n < DYSPEC_MAX_SEQ; --r) {      // (a table entry more)
+        whole = r * kCus / a.Hkv;
+        int x = 0;                                         // the sequence in which they end, its longest walk after them
+        long long upto = blocks_of(a, b, set.seq[0], rows);
+        while (x < set.n - 1 && upto <= whole) upto += blocks_of(a, b, set.seq[++x], rows);
+        if (upto > whole) tries(b.context[set.seq[x]] + (int)min((long long)new_of(b, set.seq[x]), ((upto - whole) * rows + a.G - 1) / a.G), whole);
+    }
+    set = found;
     return best;
 }
 
@@ -112,15 +167,17 @@ static bool on_bf16_cores(const AttendArgs& a, int dtype)
 // The plan of a form that was asked for: all sequences with one kernel.
 static bool plan_given(const AttendArgs& a, const AttendBatch& b, int dtype, const AttendForm& form, Plan& plan)
 {
-    if (form.kernel < 0 || form.kernel >= kKinds || form.share < 0 || form.share % kUnit) return false;
+    if (form.kernel < 0 || form.kernel >= kKinds || form.share < 0 || form.share % kUnit || form.whole < 0) return false;
     if (form.kernel < kF32Few && !on_bf16_cores(a, dtype)) return false;
     plan.n = 1;
     Set& set = plan.set[0];
     set.kind = (AttendKind)form.kernel;
     set.share = form.share ? form.share : DYSPEC_MAX_CONTEXT;
+    set.whole = form.whole;
     set.n = 0;
     for (int s = 0; s < b.n_seq; ++s)
         if (new_of(b, s) > 0) set.seq[set.n++] = s;
+    if (form.whole && set.n == DYSPEC_MAX_SEQ) return false;
     return form.share == 0 || counters_of(a, b, set) * (long long)sizeof(unsigned) <= DYSPEC_PAGED_COUNTER_BYTES;
 }
 
@@ -176,25 +233,26 @@ static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool p
 
 static size_t slot_bytes(const AttendArgs& a, AttendKind k) { return (size_t)a.Hkv * slot_floats(a.d, cost_of(a, k).rows) * sizeof(float); }
 
-// The set's sequences in a's table; returns items, and the row blocks and slots they take.
+// The set's pieces in a's table; returns items, and the row blocks and slots they take.
 static int fill(AttendArgs& a, const AttendBatch& b, const Set& set, int* groups, long long* slots, int* most_new)
 {
-    int items = 0;
+    int items = 0, n = 0;
     *groups = 0; *slots = 0; *most_new = 0;
-    a.n_seq = set.n;
-    for (int x = 0; x < set.n; ++x) {
-        const int s = set.seq[x], keys = keys_of(b, s), blocks = blocks_of(a, b, s, cost_of(a, set.kind).rows);
-        AttendSeq& q = a.seq[x];
+    each_piece(a, b, set, [&](const Piece& p) {
+        const int s = p.s, keys = b.context[s] + p.to;
+        AttendSeq& q = a.seq[n];
         q.id = s; q.row0 = b.row0[s]; q.N = new_of(b, s); q.C = b.context[s];
-        q.item0 = items; q.group0 = *groups; q.slot0 = (int)*slots;
-        q.parts = parts_of(keys, set.share);
-        q.share = q.parts == 1 ? keys : ((keys + q.parts - 1) / q.parts + kUnit - 1) / kUnit * kUnit;
+        q.item0 = items; q.end_block = p.end; q.slot0 = (int)*slots;
+        q.share = p.parts == 1 ? keys : ((keys + p.parts - 1) / p.parts + kUnit - 1) / kUnit * kUnit;
         q.parts = parts_of(keys, q.share);
-        items += blocks * q.parts;
-        *groups += blocks;
-        if (q.parts > 1) *slots += (long long)blocks * q.parts;
+        items += p.blocks * q.parts;
+        q.group0 = *groups - (p.end - p.blocks);
+        *groups += p.blocks;
+        if (q.parts > 1) *slots += (long long)p.blocks * q.parts;
         *most_new = max(*most_new, q.N);
-    }
+        ++n;
+    });
+    a.n_seq = n;
     return items;
 }
 

@@ -1,4 +1,4 @@
-"""Every kernel behind dyspec_paged_attn and dyspec_prompt_attn, with walks in one piece and in parts, on cases whose sizes would
+"""Every kernel behind dyspec_paged_attn and dyspec_prompt_attn, with walks in one piece, in parts and some of each, on cases whose sizes would
 choose another: masks, empty rows, unseen infinities and NaN, ragged ends (tests/serving.py: formulas and bounds)."""
 import ctypes
 import math
@@ -12,7 +12,7 @@ from serving import HALF, Paged, attend_plain, compare, random_mask, visible_row
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
-FORMS = [(k, share) for k in range(6) for share in (0, 128, 384)]
+FORMS = [(k, share, whole) for k in range(6) for share, whole in ((0, 0), (128, 0), (384, 0), (128, 3))]
 
 
 def with_forms(*shapes):
@@ -39,7 +39,7 @@ def workspace():
 
 def in_form(dy, form, c):
     lib, ws, out = dy.load_library(), workspace(), torch.full_like(c.q_dev, 7.0)
-    f = (ctypes.c_int32 * 2)(*form)
+    f = (ctypes.c_int32 * 3)(*form)
     mask = None if c.mask_dev is None else ctypes.c_void_p(c.mask_dev.data_ptr())
     p = lambda t: ctypes.c_void_p(t.data_ptr())
     st = lib.dyspec_paged_attn_in_form(f, p(c.q_dev), c.cache._ref, ctypes.byref(c.batch._c()), mask, c.Hq, c.Hkv, c.d, c.cache._code,
@@ -107,7 +107,7 @@ def test_prompts(dy, form, dtype, Hq, Hkv, d):
     q, k, v = (t.cuda() for t in host)
     lib, ws, out = dy.load_library(), workspace(), torch.full_like(q, 7.0)
     b = dy.Batch.from_sizes(new)
-    f, p = (ctypes.c_int32 * 2)(*form), lambda t: ctypes.c_void_p(t.data_ptr())
+    f, p = (ctypes.c_int32 * 3)(*form), lambda t: ctypes.c_void_p(t.data_ptr())
     I = ctypes.c_int64
     st = lib.dyspec_prompt_attn_in_form(f, p(q), I(Hq * d), p(k), I(Hkv * d), p(v), I(Hkv * d), ctypes.byref(b._c()), Hq, Hkv, d, dy.F32 if dtype is F32 else dy.BF16,
                                         ctypes.c_float(0.1), p(out), p(ws), ctypes.c_size_t(ws.numel()), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
@@ -123,5 +123,5 @@ def test_prompts(dy, form, dtype, Hq, Hkv, d):
 
 def test_forms_that_there_are_not(dy):
     c = Paged((5,), (300,), 4, 2, 64, F32, 16, 2)
-    for form in ((0, 0), (3, 0), (6, 0), (-1, 0), (4, 100), (4, -128)):
+    for form in ((0, 0, 0), (3, 0, 0), (6, 0, 0), (-1, 0, 0), (4, 100, 0), (4, -128, 0), (4, 128, -1)):
         assert in_form(dy, form, c)[0] == -3, form

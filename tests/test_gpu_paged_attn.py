@@ -207,6 +207,15 @@ def test_long_contexts(dy, dtype, new, context):
     c.check(dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale))
 
 
+@pytest.mark.parametrize("new,context,Hq,Hkv,d", [((500, 1, 2), (400, 2000, 1500), 64, 8, 128), ((1, 1000), (3000, 100), 32, 32, 64),
+                                                  ((544,), (1000,), 64, 8, 128)], ids=str)
+def test_whole_walks_beside_walks_in_parts(dy, new, context, Hq, Hkv, d):
+    """More row blocks than CUs: single tokens' long walks are cut beside them, or what is left after a round of workgroups."""
+    c = Paged(new, context, Hq, Hkv, d, BF16, 16, 37, mask=random_mask(new, 8)[0])
+    assert dy.load_library().dyspec_paged_attn_workspace_bytes(c.batch._c(), Hq, Hkv, d, dy.BF16) > 0
+    c.check(dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev))
+
+
 def test_a_long_prompt(dy):
     """20001 tokens: rows from all over it against the plain form."""
     n, g = 20001, torch.Generator().manual_seed(31)
