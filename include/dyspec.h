@@ -362,8 +362,9 @@ dyspec_status dyspec_verify_bf16(const void* draft_logits, const void* target_lo
 #define DYSPEC_MAX_CHUNK (1 << 20)          /* new tokens per sequence                                  */
 #define DYSPEC_MAX_CONTEXT (1 << 30)        /* tokens of a sequence, new ones included                  */
 #define DYSPEC_PAGED_COUNTER_BYTES 16384    /* head of a dyspec_paged_attn workspace                    */
-/* Up to 8192 heads and 2^20 elements a token; (n_q_heads / n_kv_heads)^2 times a sequence's new tokens, and
- * the batch's tokens times n_q_heads / 4, below 2^32 (DYSPEC_BAD_SHAPE beyond). */
+/* Up to 8192 heads and 2^20 elements a token; (n_q_heads / n_kv_heads)^2 times a sequence's new tokens below
+ * 2^32; up to 2^23 new tokens in a batch, and up to 2^27 of them times n_q_heads for attention
+ * (DYSPEC_BAD_SHAPE beyond). */
 
 /* One layer's pool.  Page p's rows are k + p * page_stride + row * n_kv_heads * head_dim (elements), dense
  * in the page; pages may lie apart (K and V pages in turns: page_stride of two pages). */

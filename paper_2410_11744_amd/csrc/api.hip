@@ -420,6 +420,10 @@ dyspec_status dyspec_verify_bf16(const void* draft_logits, const void* target_lo
 
 // ---- the paged cache and prompts
 
+// A launch has less than 2^32 threads along its grid: kv_append a workgroup of 256 a token, the attention kernels 256 on 16 rows or
+// 512 on 32, and up to one more for each sequence and KV head.
+constexpr int kMostTokens = 1 << 23;
+
 // New tokens and context of every sequence (a batch whose sequences may have no new tokens).
 static dyspec_status check_chunks(const dyspec_batch* b, bool context, int max_new, AttendBatch* ab)
 {
@@ -434,10 +438,11 @@ static dyspec_status check_chunks(const dyspec_batch* b, bool context, int max_n
         ab->context[s] = (int)c;
     }
     ab->row0[b->n_seq] = b->node_offset[b->n_seq];
-    return DYSPEC_OK;
+    return ab->row0[b->n_seq] <= kMostTokens ? DYSPEC_OK : DYSPEC_BAD_SHAPE;
 }
 
 constexpr int kMostHeads = 8192, kMostRow = 1 << 20;
+constexpr long long kMostRows = 1LL << 27;
 
 static dyspec_status check_heads(int Hq, int Hkv, int d, int dtype)
 {
@@ -453,7 +458,7 @@ static bool rows_ok(const AttendBatch& b, int Hq, int G)
 {
     int most = 0;
     for (int s = 0; s < b.n_seq; ++s) most = max(most, b.row0[s + 1] - b.row0[s]);
-    return (long long)most * G * G <= 0xffffffffLL && (long long)b.row0[b.n_seq] * Hq <= 1LL << 34;
+    return (long long)most * G * G <= 0xffffffffLL && (long long)b.row0[b.n_seq] * Hq <= kMostRows;
 }
 
 static int log2_of(int x) { int s = 0; while ((1 << s) < x) ++s; return s; }

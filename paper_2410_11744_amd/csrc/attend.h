@@ -150,7 +150,7 @@ __device__ __forceinline__ char* out_row(const AttendArgs& a, const AttendSeq& s
 // A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
 // matrix product.  Such keys may hold anything (a later token that overflowed), so a row that comes out with a NaN is done again
 // by this: keys one at a time, those the row does not see left out, weights against the reference m that the row has.  One wave,
-// lane i holds dims 4i..; a NaN of the row's own keys comes out as one again.
+// lane i holds dims 4i..; a NaN of the row's own keys comes out as one again (and ends the walk where it is in all dims).
 template <typename T>
 __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& s, int kvh, int r, int k_begin, int k_end, float m, float4& o, float& l)
 {
@@ -172,6 +172,7 @@ __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& 
         const float p = exp2f((dot - m) * a.c2);
         l += p;
         o.x += p * v.x; o.y += p * v.y; o.z += p * v.z; o.w += p * v.w;
+        if (__all(o.x != o.x && o.y != o.y && o.z != o.z && o.w != o.w)) return;      // nothing else comes of it
     }
 }
 

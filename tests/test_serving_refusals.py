@@ -63,6 +63,13 @@ def test_batches(lib):
         for b in (too_long, falling, late, negative, far, binding.Batch.from_sizes([1] * 65)._c()):
             assert call(lib, b=b) == BAD_SHAPE, call.__name__
     assert prompt(lib, b=batch((3, 1), (0, 4))) == BAD_SHAPE                 # a prompt has nothing before it
+    # 2^23 + 1 new tokens in all; 2^23 with 17 heads, more than 2^27 rows
+    many = binding.Batch(np.array([min(i << 20, (1 << 23) + 1) for i in range(10)], np.int32), np.zeros(9, np.int32), np.zeros(10, np.int64))._c()
+    wide = dict(max_pages=1 << 17, stride=1 << 17)
+    assert append(lib, c=cache(**wide), b=many) == keep(lib, c=cache(**wide), b=many) == attn(lib, c=cache(**wide), b=many) == prompt(lib, b=many) == BAD_SHAPE
+    rows = binding.Batch(np.array([i << 20 for i in range(9)] + [(1 << 23)], np.int32), np.zeros(9, np.int32), np.zeros(10, np.int64))._c()
+    assert attn(lib, c=cache(page_stride=16 * 17 * 64, **wide), b=rows, Hq=17, Hkv=17, d=64) == BAD_SHAPE
+    assert prompt(lib, b=rows, Hq=17, Hkv=17, d=64, qs=17 * 64, ks=17 * 64, vs=17 * 64) == BAD_SHAPE
     # under a mask, trees of up to 2048 rows
     wide = cache(max_pages=200, stride=200)
     assert attn(lib, c=wide, b=batch((2049,), (0,)), mask=A) == BAD_SHAPE
