@@ -769,7 +769,7 @@ def _append_args(k, v, batch, cache, q, rel_pos, inv_freq, interleaved, out, k_o
         qs, qp = _token_rows(q, shape, dtype, device, "q"), q.data_ptr()
         if out is None:
             with where:
-                out = torch.empty(shape, dtype=dtype, device=q.device)
+                out = q.new_empty(shape)
             op = out.data_ptr()
         else:
             op = _dense(out, shape, dtype, device, "out")
@@ -888,7 +888,6 @@ def prompt_attn_call(q, k, v, batch: Batch, softmax_scale: float, out=None, stre
 def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
     if _lib is None:
         load_library()
-    torch = _torch
     total, ref = _chunks(batch)["chunks"]
     device, dtype = q.get_device(), q.dtype
     if device < 0:
@@ -899,10 +898,10 @@ def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
     shape, kv_shape = (total, Hq, d), (total, Hkv, d)
     qs = _token_rows(q, shape, dtype, device, "q")
     ks, vs = _token_rows(k, kv_shape, dtype, device, "k"), _token_rows(v, kv_shape, dtype, device, "v")
-    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    raw, where = (_torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
     if out is None:
         with where:
-            out = torch.empty(shape, dtype=dtype, device=q.device)
+            out = q.new_empty(shape)
         op = out.data_ptr()
     else:
         op = _dense(out, shape, dtype, device, "out")

@@ -41,7 +41,7 @@ template <int D, int NW> struct ManyGeo {
     static constexpr int kMatBytes = kTile * kRowBytes;          // one K or V tile
     static constexpr int kSlotBytes = kTiles * kMatBytes;        // a slot holds a step's tiles
     static constexpr int kVBase = 2 * kSlotBytes;                // K slots 0 and 1, then V slots 0 and 1
-    static constexpr int kLdsBytes = 4 * kSlotBytes;
+    static constexpr int kLdsBytes = 4 * kSlotBytes + (kTiles == 1 ? kMatBytes : 0);      // (two workgroups of the latter fill a CU's 160 KB)
     static constexpr int kLoads = 32 / kRowsPerLoad;             // direct loads of a wave per step
 };
 
@@ -52,7 +52,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     using L = ManyGeo<D, NW>;
     constexpr int TP = L::kTiles, KK = D / 16, DB = D / 32;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
-    __shared__ int flag;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -142,9 +141,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     const uint32_t st_dst = lds0 + (ld_is_v ? L::kVBase : 0) + ld_par * L::kMatBytes + ld_half * (32 * L::kRowBytes);
     auto slot_of = [=](int i) __attribute__((always_inline)) -> uint32_t { return (uint32_t)(((ld_is_v ? i + 1 : i) & 1) * L::kSlotBytes); };
 
-    // ---- prologue: the query rows (into V slot 1, of one tile a slot into both V slots, laid out like K: no V tile comes to slot 1
-    //      before the middle of step 0), K of the first two steps, V of the first.
-    const uint32_t q_lds = lds0 + L::kVBase + (TP == 2 ? L::kSlotBytes : 0);
+    // ---- prologue: the query rows (into V slot 1, of one tile a slot also into the place behind it, laid out like K: no V tile
+    //      comes to slot 1 before the middle of step 0), K of the first two steps, V of the first.
+    const uint32_t q_lds = lds0 + L::kVBase + L::kSlotBytes;
     {
         constexpr int QL = kRows / L::kRowsPerLoad / NW;
         const char* const q_seq = a.q + (long long)(s.row0 + j_first) * a.q_stride + (long long)it.kvh * a.G * (D * 2);
@@ -184,11 +183,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
             for (int w = 0; w < 4; ++w) pw[e][ts][w] = 0u;
     float m_run = kLowest, l_run = 0.0f, ls_half = 0.0f;
     const float c2 = a.c2;
-    if (TP == 2) __syncthreads();                // (the later loads queue up behind the urgent ones)
+    __syncthreads();                             // (the later loads queue up behind the urgent ones)
     if (ld_is_v) issue_first_k();
-    if (TP == 2) issue_first_v();
+    issue_first_v();
     // the others wait for their query rows only: K of the second step and V are needed from the middle of step 0 on
-    if (ld_is_v && ld_mm < nT && ld_par < nT) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(TP * L::kLoads) : "memory");
+    if (ld_is_v && ld_mm < nT && ld_par < nT) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * L::kLoads) : "memory");
     else wait_direct_loads();
     __syncthreads();
     bf16x8 qf[KK];                               // B operand: lane holds query n, dims 16 kk + 8 g ..
@@ -196,11 +195,6 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     for (int kk = 0; kk < KK; ++kk) {
         const int R = 32 * wq + n;
         qf[kk] = *(lds_bf16x8)(uint32_t)(q_lds + R * L::kRowBytes + (((2 * kk + g) ^ swz_k<D>(R)) << 4));
-    }
-    if (TP == 1) {                               // V comes where the query rows were
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __syncthreads();
-        issue_first_v();
     }
     // ---- LDS read addresses of this lane
     int k_off[KK];                               // K fragment of step kk, key row n of a half
@@ -561,7 +555,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         leave_exact_rows<__bf16, kSlotMany>(a, it, bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, k_begin, k_end, n_parts, slot,
                                        [=](int row) { return __shfl(m, row - 32 * wq, kWave); });
     });
-    if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<__bf16, kSlotMany, D>(a, it, n_parts, kRows, 64 * NW);
+    if (n_parts > 1 && arrive_last(a, it, n_parts, reinterpret_cast<int*>(lds))) merge_parts<__bf16, kSlotMany, D>(a, it, n_parts, kRows, 64 * NW);
 }
 
 template <int D, bool Paged, int NW>
