@@ -18,10 +18,10 @@
 // of eight rows that lie each within a page: their addresses are uniform over the wave and are made by the scalar unit from page
 // numbers which 64 lanes hold for 16 steps ahead.  So pages cost the vector and matrix units nothing.
 //
-// What bounds it: the power the card may draw.  In the loop the matrix cores are busy 61 % of the cycles, LDS 32 %, and the clock
-// goes down to 1.6 GHz; reading operands earlier, other wave priorities or orders of the loop's instructions change nothing.
-// Measured, 64 query heads on 8: a causal prompt of 8192 tokens 0.92 to 0.98 ms, 1.12 to 1.19 PFLOP/s (a matrix product of 8192
-// cubed, by the library: 1.34); a tree of 512 rows over 4096 tokens in pages of 16: 70 to 73 us, 0.94 to 0.98 PFLOP/s.
+// What bounds it: the power the card may draw.  Over a prompt of 8192 tokens the matrix cores are busy 70 % of the cycles, LDS 36 %,
+// and the clock goes down to 1.5 GHz; reading operands earlier, other wave priorities or orders of the loop's instructions change
+// nothing.  Measured, 64 query heads on 8: that prompt 0.92 to 0.98 ms, 1.12 to 1.19 PFLOP/s (a matrix product of 8192 cubed, by the
+// library: 1.34); a tree of 512 rows over 4096 tokens in pages of 16: 70 to 73 us, 0.94 to 0.98 PFLOP/s.
 #include <atomic>
 
 #include "attend.h"
