@@ -495,7 +495,7 @@ static void sequences(Sequences<DYSPEC_MAX_SEQ>& seq, const AttendBatch& b)
     seq.row0[b.n_seq] = b.row0[b.n_seq];
 }
 
-static bool scale_ok(float x) { return x > 0.0f && x <= 3.4e38f; }
+static bool scale_ok(float x) { return x > 0.0f && x <= 2.3e38f; }      // (times log2 e it is finite still)
 
 dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const dyspec_paged_kv* cache, const dyspec_batch* batch, const int32_t* rel_pos, const float* inv_freq,

@@ -80,7 +80,7 @@ def test_batches(lib):
 def test_heads_and_types(lib):
     for call in (attn, prompt):
         assert call(lib, Hq=7) == BAD_SHAPE and call(lib, Hkv=0) == BAD_SHAPE and call(lib, Hq=0) == BAD_SHAPE and call(lib, Hq=-8) == BAD_SHAPE
-        for scale in (0.0, -1.0, float("nan"), float("inf")):
+        for scale in (0.0, -1.0, float("nan"), float("inf"), 3e38):
             assert call(lib, scale=scale) == BAD_ARG
     for call in (attn, prompt, append, keep):
         for d in (0, 2, 66, 260, -4):
