@@ -4,7 +4,7 @@
 // CU) the two waves of a row block take 64-key tiles in turn, even and odd, and merge (max, sum, rows) through LDS at the end: a
 // lone workgroup goes through its keys sooner.  With four (two workgroups a CU) a wave takes every tile: more row blocks than CUs
 // are dealt more evenly, and one workgroup computes while the other starts or ends (packed prompts of 1 to 1300 tokens, 32 heads:
-// 78 us with eight, 59 with four; one tree of 512 rows over 4096 tokens, as many row blocks as CUs: 74 with eight, 85 with four).
+// 78 us with eight, 58 with four; one tree of 512 rows over 4096 tokens, as many row blocks as CUs: 74 with eight, 85 with four).
 // Per 32-key half tile a wave computes S^T = K Q^T (a lane then holds one query and 16 keys), the weights, and O^T += V^T P^T,
 // whose B operand is already where the weights are.
 //
@@ -73,6 +73,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     const int nWhole = (k_end - k_begin) / kTile;
     const int rc = min(r0 + 32 * wq + n, rows - 1);
     const int row_j = div_G(a, rc);
+
+    // Bytes from the block's first token's first head (of this KV head) to row x of the block.  All factors are below 2^24.
+    const int row_first = r0 - j_first * a.G;
+    auto row_offset = [=](int x, uint32_t stride) __attribute__((always_inline)) -> uint32_t {
+        const int y = row_first + x, j = div_G(a, y);
+        return __umul24((uint32_t)j, stride) + (uint32_t)(y - (int)__umul24((uint32_t)j, (uint32_t)a.G)) * (D * 2);
+    };
 
     // ---- this wave's loads of a step: 32 rows (half ld_half) of K or V of one of its tiles
     const int ld_mm = wave >> 1, ld_half = wave & 1;
@@ -151,9 +158,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         for (int x = 0; x < QL; ++x) {
             const int X = wave * QL + x;
             const int R = X * L::kRowsPerLoad + lrow;
-            const int r = min(r0 + R, rows - 1), j = div_G(a, r);
-            const uint32_t off = (uint32_t)(j - j_first) * (uint32_t)a.q_stride + (uint32_t)(r - j * a.G) * (D * 2) + 16u * (uint32_t)(cpos ^ swz_k<D>(R));
-            direct_load_16(q_seq, off, q_lds + X * 1024);
+            direct_load_16(q_seq, row_offset(min(R, rows - 1 - r0), (uint32_t)a.q_stride) + 16u * (uint32_t)(cpos ^ swz_k<D>(R)), q_lds + X * 1024);
         }
     }
     auto issue_first_k = [=]() __attribute__((always_inline)) {
@@ -533,6 +538,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
             constexpr int kPitch = 64 * HB + 16, CPR = 4 * HB;
             const uint32_t stage = lds0 + NW * (kArea + kMl) + (uint32_t)wave * (32 * kPitch);
             static_assert(NW * (kArea + kMl) + NW * 32 * kPitch <= L::kLdsBytes, "areas and stages fit");
+            char* const out_first = a.out + (long long)(s.row0 + j_first) * a.out_stride + (long long)it.kvh * a.G * (D * 2);
+            const uint32_t out_stride = (uint32_t)a.out_stride;
             typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
             typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -548,8 +555,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
                 const int c = lane + kWave * t, rn = c / CPR, cc = c % CPR;
                 if (rn >= left || ((bad >> rn) & 1u)) continue;
                 const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(uint32_t)(stage + rn * kPitch + cc * 16);
-                const int r = r0 + 32 * wq + rn, j = div_G(a, r);
-                __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out_row(a, s, j, it.kvh * a.G + (r - j * a.G), 2) + 64 * mine + cc * 16));
+                __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out_first + (row_offset(32 * wq + rn, out_stride) + 64 * mine + cc * 16)));
             }
         }
         leave_exact_rows<__bf16, kSlotMany>(a, it, bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, k_begin, k_end, n_parts, slot,
