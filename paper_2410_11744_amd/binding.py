@@ -722,7 +722,8 @@ def _attend_workspace(device: int, raw: int, where, nbytes: int, prepared: bool)
                 return buf[0]
         if prepared and capturing:
             raise ValueError("prepare the call before the graph is recorded: its workspace has to be cleared first")
-        buf = torch.zeros(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", device))
+        buf[:PAGED_COUNTER_BYTES].zero_()                       # (a graph does this at every replay)
         if not prepared and not capturing:
             _attend_scratch[(device, raw)] = (buf, nbytes)
         return buf
