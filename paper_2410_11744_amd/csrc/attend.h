@@ -148,8 +148,32 @@ __device__ __forceinline__ char* out_row(const AttendArgs& a, const AttendSeq& s
 // ---- a row that met a NaN
 //
 // A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
-// matrix product.  Such keys may hold anything (a later token that overflowed), so a row that comes out with a NaN is done again
-// by this: keys one at a time, those the row does not see left out, weights against the reference m that the row has.  One wave,
+// matrix product.  Such keys may hold anything (a later token that overflowed), so rows that come out with a NaN are looked at
+// again: if what their block read beside keys that all its rows see was all finite, the NaN is the row's own and stays.
+// (Otherwise a NaN at the start of a long context would send every row through the walk below, a thousand times slower.)
+
+// Whether the block's query rows (which lie where a V tile would be, at weights of zero, when a walk starts) and V of the walk's keys
+// that some row of it may not see are finite.  One wave, lane i reads dims 4i..
+template <typename T>
+__device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int r1, int k_begin, int k_end)
+{
+    typedef typename Four<T>::raw raw;
+    const int size = (int)sizeof(T), lane = threadIdx.x & 63, piece = 4 * lane < a.d ? lane : 0;
+    float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // stays zero unless something is infinite or a NaN
+    auto add = [&](float4 x) { z.x = fmaf(x.x, 0.0f, z.x); z.y = fmaf(x.y, 0.0f, z.y); z.z = fmaf(x.z, 0.0f, z.z); z.w = fmaf(x.w, 0.0f, z.w); };
+#pragma unroll 4
+    for (int r = r0; r < r1; ++r) {
+        const int j = div_G(a, r), h = kvh * a.G + (r - j * a.G);
+        add(Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * size)));
+    }
+    const long long head = (long long)kvh * a.d * size + 4 * piece * size;
+#pragma unroll 4
+    for (int key = max(k_begin, a.mask ? s.C : s.C + div_G(a, r0) + 1); key < k_end; ++key)
+        add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
+    return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
+}
+
+// The row again: keys one at a time, those it does not see left out, weights against the reference m that the row has.  One wave,
 // lane i holds dims 4i..; a NaN of the row's own keys comes out as one again (and ends the walk where it is in all dims).
 template <typename T>
 __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& s, int kvh, int r, int k_begin, int k_end, float m, float4& o, float& l)
@@ -162,16 +186,26 @@ __device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& 
     const float4 q = Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * (int)sizeof(T)));
     o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     l = 0.0f;
-    const long long head = (long long)kvh * a.d * (int)sizeof(T);
+    const long long head = (long long)kvh * a.d * (int)sizeof(T) + 4 * piece * (int)sizeof(T);
+    constexpr int kBatch = 4;                                  // keys per trip to memory
 #pragma unroll 1
-    for (int key = k_begin; key < k_end; ++key) {
-        if (!(__builtin_amdgcn_readfirstlane((int)seen_bits(a, s, j, key)) & 1)) continue;
-        const float4 k = Four<T>::wide(*reinterpret_cast<const raw*>(a.k + key_offset(a, s, key, a.k_stride) + head + 4 * piece * (int)sizeof(T)));
-        const float4 v = Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head + 4 * piece * (int)sizeof(T)));
-        const float dot = wave_sum(mine ? (q.x * k.x + q.y * k.y) + (q.z * k.z + q.w * k.w) : 0.0f);
-        const float p = exp2f((dot - m) * a.c2);
-        l += p;
-        o.x += p * v.x; o.y += p * v.y; o.z += p * v.z; o.w += p * v.w;
+    for (int key = k_begin; key < k_end; key += kBatch) {
+        const uint32_t seen = (uint32_t)__builtin_amdgcn_readfirstlane((int)seen_bits(a, s, j, key));
+        float4 k[kBatch], v[kBatch];
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+            const int at = min(key + x, k_end - 1);
+            k[x] = Four<T>::wide(*reinterpret_cast<const raw*>(a.k + key_offset(a, s, at, a.k_stride) + head));
+            v[x] = Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, at, a.v_stride) + head));
+        }
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+            if (key + x >= k_end || !((seen >> x) & 1u)) continue;
+            const float dot = wave_sum(mine ? (q.x * k[x].x + q.y * k[x].y) + (q.z * k[x].z + q.w * k[x].w) : 0.0f);
+            const float p = exp2f((dot - m) * a.c2);
+            l += p;
+            o.x += p * v[x].x; o.y += p * v[x].y; o.z += p * v[x].z; o.w += p * v[x].w;
+        }
         if (__all(o.x != o.x && o.y != o.y && o.z != o.z && o.w != o.w)) return;      // nothing else comes of it
     }
 }

@@ -227,6 +227,7 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 ? 2 : 1) void attend_f32_
                     if (64 * b + 16 * g + 4 * i < a.d) nan |= acc[b][c][i] != acc[b][c][i];
         uint64_t lanes = __builtin_amdgcn_ballot_w64(nan && r < rows);
         uint32_t bad = (uint32_t)((lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu);
+        if (bad && hidden_are_finite<T>(a, s, it.kvh, r0, min(r0 + R, rows), k_begin, k_end)) bad = 0u;
         const bool leave = r < rows && !((bad >> n) & 1u);
         if (n_parts > 1) {
             if (g == 0 && r < rows) store_pair(slot_max_sum(a, slot, R, 16 * wq + n), m, l);

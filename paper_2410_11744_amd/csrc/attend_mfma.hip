@@ -522,6 +522,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         const uint64_t lanes = __builtin_amdgcn_ballot_w64((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f);      // (a NaN is not equal)
         uint32_t bad = (uint32_t)(lanes | lanes >> 32);
         if (left < 32) bad &= left > 0 ? (1u << left) - 1u : 0u;
+        if (bad && hidden_are_finite<__bf16>(a, s, it.kvh, r0, min(r0 + kRows, rows), k_begin, k_end)) bad = 0u;
         if (n_parts > 1) {
             if (n < left && !((bad >> n) & 1u)) {
 #pragma unroll

@@ -326,6 +326,7 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
 #pragma unroll
         for (int x = 0; x < 64 / DP; ++x)
             if ((lanes >> (x * DP)) & ((1ull << DP) - 1ull)) here |= 1u << x;
+        if (here && hidden_are_finite<__bf16>(a, s, it.kvh, r0, min(r0 + kFewRows, rows), k_begin, k_end)) here = 0u;
         bad |= here << (t * (64 / DP));
         if (there && n_parts > 1 && dp == 0) store_pair(slot_max_sum(a, part, kFewRows, row), M, l);
         if (!there || ((here >> (lane / DP)) & 1u)) continue;

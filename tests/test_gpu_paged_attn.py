@@ -238,3 +238,25 @@ def test_a_row_that_is_no_number_leaves_the_others_alone(dy, dtype, d, new):
     out[new // 2, 1] = dy.paged_attn(c.q.cuda(), c.batch, c.cache, c.scale)[new // 2, 1]
     out[new // 3, 2] = dy.paged_attn(c.q.cuda(), c.batch, c.cache, c.scale)[new // 3, 2]
     c.check(out)
+
+
+@pytest.mark.parametrize("tree", [False, True], ids=["causal", "tree"])
+@pytest.mark.parametrize("dtype,d,new,context", [(BF16, 128, 300, 200), (BF16, 128, 20, 700), (BF16, 64, 1, 5000), (F32, 64, 100, 50), (BF16, 80, 9, 40)])
+def test_what_every_row_sees_stays_in_its_dims(dy, dtype, d, new, context, tree):
+    """A NaN and an infinity in V, and a NaN in K, of a context: in the rows' results where the formula has them, nowhere else."""
+    c = Paged((new, 2, 40), (context, context, 33), 4, 2, d, dtype, 16, 43, mask=random_mask((new, 2, 40), 3)[0] if tree else None)
+    p, r = c.place(0, 5)
+    c.v[p, r, 0, 3], c.v[p, r, 1, d - 1] = 0, 0              # what the other dims are held against
+    v_dev = c.v.clone()
+    v_dev[p, r, 0, 3], v_dev[p, r, 1, d - 1] = math.nan, math.inf
+    p, r = c.place(1, context - 1)
+    c.k[p, r, 1, 2] = math.nan
+    c.cache.k.copy_(c.k), c.cache.v.copy_(v_dev)
+    out = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev)
+    first, second = out[:new], out[new:new + 2]
+    assert torch.isnan(first[:, :2, 3]).all() and (first[:, 2:, d - 1] == math.inf).all()
+    assert torch.isnan(second[:, 2:]).all() and torch.isfinite(second[:, :2]).all()
+    c.cache.v.copy_(c.v)
+    clean = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev)
+    first[:, :2, 3], first[:, 2:, d - 1] = clean[:new, :2, 3], clean[:new, 2:, d - 1]
+    c.check(out, only=(0, 2))
