@@ -20,8 +20,8 @@
 //
 // What bounds it: the power the card may draw.  Over a prompt of 8192 tokens the matrix cores are busy 70 % of the cycles, LDS 36 %,
 // and the clock goes down to 1.5 GHz; reading operands earlier, other wave priorities or orders of the loop's instructions change
-// nothing.  Measured, 64 query heads on 8: that prompt 0.92 to 0.98 ms, 1.12 to 1.19 PFLOP/s (a matrix product of 8192 cubed, by the
-// library: 1.34); a tree of 512 rows over 4096 tokens in pages of 16: 70 to 73 us, 0.94 to 0.98 PFLOP/s.
+// nothing.  Measured, 64 query heads on 8: that prompt 0.92 to 1.04 ms, 1.06 to 1.19 PFLOP/s (a matrix product of 8192 cubed, by the
+// library: 1.34); a tree of 512 rows over 4096 tokens in pages of 16: 70 to 80 us, 0.86 to 0.98 PFLOP/s, by the clock that a card holds.
 #include <atomic>
 
 #include "attend.h"
