@@ -359,7 +359,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         const float alpha = fast_exp2((m_run - m_new) * c2);
         m_run = m_new;
         l_run *= alpha;
-        if (__any(alpha != 0.0f && alpha != 1.0f)) {               // alpha 0: nothing summed yet, or nothing that counts
+        if (__any(alpha != 1.0f)) {                                // (alpha 0 too: a far lower reference's sums are still in acc)
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
