@@ -419,7 +419,7 @@ __global__ __launch_bounds__(64 * 2 * (4 / QB)) void tree_attn_mfma_kernel(AttnA
             const float alpha = fast_exp2((m_run[qb] - m_new) * c2);
             m_run[qb] = m_new;
             l_run[qb] *= alpha;
-            if (__any(alpha != 0.0f && alpha != 1.0f)) {       // alpha 0: accumulators still 0
+            if (__any(alpha != 1.0f)) {                        // (alpha 0 too: a far lower reference's sums are still in acc)
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
