@@ -149,11 +149,12 @@ __device__ __forceinline__ char* out_row(const AttendArgs& a, const AttendSeq& s
 //
 // A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
 // matrix product.  Such keys may hold anything (a later token that overflowed), so rows that come out with a NaN are looked at
-// again: if what their block read beside keys that all its rows see was all finite, the NaN is the row's own and stays.
+// again: if what their block took at a weight of zero was all finite, the NaN is the row's own and stays.
 // (Otherwise a NaN at the start of a long context would send every row through the walk below, a thousand times slower.)
 
 // Whether the block's query rows (which lie where a V tile would be, at weights of zero, when a walk starts) and V of the walk's keys
-// that some row of it may not see are finite.  One wave, lane i reads dims 4i..
+// that meet a weight of zero are finite: those that some row of the block may not see, and the last one, which is repeated behind the
+// end of a block of keys.  One wave, lane i reads dims 4i..
 template <typename T>
 __device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int r1, int k_begin, int k_end)
 {
@@ -168,7 +169,7 @@ __device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const Att
     }
     const long long head = (long long)kvh * a.d * size + 4 * piece * size;
 #pragma unroll 4
-    for (int key = max(k_begin, a.mask ? s.C : s.C + div_G(a, r0) + 1); key < k_end; ++key)
+    for (int key = max(k_begin, min(a.mask ? s.C : s.C + div_G(a, r0) + 1, k_end - 1)); key < k_end; ++key)
         add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
     return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
 }

@@ -1,5 +1,5 @@
-"""Attention over pages and of prompts where one key decides: its score lies far above all before it.  Every kernel, whole and in
-parts (test_gpu_attend_forms.py), against the plain form in 64 bits (tests/serving.py: formulas and bounds)."""
+"""Attention over pages and of prompts where one key decides: a score far above all others, an infinity that the last token sees.  Every kernel,
+whole and in parts (test_gpu_attend_forms.py), against the plain form in 64 bits (tests/serving.py: formulas and bounds)."""
 import ctypes
 import math
 
@@ -9,7 +9,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from serving import HALF, Paged, attend_plain, compare, random_mask, visible_rows
-from test_gpu_attend_forms import check, in_form, weight_half, with_forms, workspace
+from test_gpu_attend_forms import FORMS, check, in_form, weight_half, with_forms, workspace
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -78,3 +78,63 @@ def test_a_prompts_key_far_above_those_before_it(dy, form, dtype, Hq, Hkv, d):
         want, bound = attend_plain(*(t[at:at + n].double().numpy() for t in (q, k, v)), visible_rows(n, 0), 0.1, weight_half(form, dtype), HALF[dtype])
         compare(out[at:at + n], want, bound, f"prompt {s}")
         at += n
+
+
+# ---- infinities that the last token sees
+
+FORMS_OF_EACH = with_forms((BF16, 128), (BF16, 64), (F32, 64), (F32, 192)) + [(form, BF16, 80) for form in FORMS if form[0] >= 4]
+
+
+@pytest.mark.parametrize("form,dtype,d", FORMS_OF_EACH, ids=str)
+def test_an_infinity_in_the_newest_value(dy, form, dtype, d):
+    """One token each, causal: its own value's infinities come out as they are whether its place ends a block of keys or not, a second
+    sequence (which has none) as if they were not there."""
+    for context in (0, 30, 31, 63, 99, 127, 200, 511):
+        print("form", form, dtype, d, context, flush=True)
+        c = Paged((1, 1), (context, 77), 4, 2, d, dtype, 16, 45)
+        p, r = c.place(0, context)
+        c.v[p, r, 0, 3], c.v[p, r, 1, d - 1] = 0, 0               # what the other dims are held against
+        v = c.v.clone()
+        v[p, r, 0, 3], v[p, r, 1, d - 1] = math.inf, -math.inf
+        c.cache.v.copy_(v)
+        st, out = in_form(dy, form, c)
+        assert st == 0
+        assert (out[0, :2, 3] == math.inf).all() and (out[0, 2:, d - 1] == -math.inf).all()
+        c.cache.v.copy_(c.v)
+        st, clean = in_form(dy, form, c)
+        out[0, :2, 3], out[0, 2:, d - 1] = clean[0, :2, 3], clean[0, 2:, d - 1]
+        check(c, out, form)
+
+
+@pytest.mark.parametrize("form,dtype,d", with_forms((BF16, 128), (BF16, 64), (F32, 64)), ids=str)
+def test_an_infinity_in_a_prompts_last_value(dy, form, dtype, d):
+    """The same of a prompt, whose last row block may hold the last token alone (65 tokens of two heads)."""
+    for n in (1, 33, 64, 65, 129, 450):
+        print("form", form, dtype, d, n, flush=True)
+        g = torch.Generator().manual_seed(3)
+        q, k, v = (torch.randn((n, h, d), generator=g).to(dtype) for h in (4, 2, 2))
+        v[n - 1, 0, 3], v[n - 1, 1, d - 1] = 0, 0
+        bad = v.clone()
+        bad[n - 1, 0, 3], bad[n - 1, 1, d - 1] = math.inf, -math.inf
+        out = prompt_in_form(dy, form, q.cuda(), k.cuda(), bad.cuda(), (n,), 0.1).double().cpu().numpy()
+        assert (out[n - 1, :2, 3] == math.inf).all() and (out[n - 1, 2:, d - 1] == -math.inf).all()
+        want, bound = attend_plain(*(x.double().numpy() for x in (q, k, v)), visible_rows(n, 0), 0.1, weight_half(form, dtype), HALF[dtype])
+        out[n - 1, :2, 3], out[n - 1, 2:, d - 1] = want[n - 1, :2, 3], want[n - 1, 2:, d - 1]
+        compare(out, want, bound, "the rest")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64), (BF16, 80)])
+def test_an_infinity_in_the_newest_value_of_each_of_many(dy, dtype, d):
+    """As the library chooses the kernels: 20 sequences of one token, contexts of any size."""
+    context = [int(x) for x in np.random.default_rng(8).integers(0, 900, 20)]
+    c = Paged([1] * 20, context, 4, 2, d, dtype, 16, 47)
+    v = c.v.clone()
+    for s in range(20):
+        p, r = c.place(s, context[s])
+        c.v[p, r, 1, 5], v[p, r, 1, 5] = 0, math.inf
+    c.cache.v.copy_(v)
+    out = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale)
+    assert (out[:, 2:, 5] == math.inf).all()
+    c.cache.v.copy_(c.v)
+    out[:, 2:, 5] = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale)[:, 2:, 5]
+    c.check(out)
