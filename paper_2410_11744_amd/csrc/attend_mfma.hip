@@ -357,13 +357,19 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
         const float m_new = fmaxf(m_run, mx);
         const float alpha = fast_exp2((m_run - m_new) * c2);
+        // A row without a sum so far starts at zero whatever acc holds: the first half's second product takes what lies in V's slot then,
+        // query rows, at weights of zero, and a row's NaN is nothing to other rows.
+        const bool fresh = m_run == kLowest;
         m_run = m_new;
         l_run *= alpha;
-        if (__any(alpha != 1.0f)) {                                // (alpha 0 too: a far lower reference's sums are still in acc)
+        if (__all(fresh)) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = zero16;
+        } else if (__any(alpha != 1.0f)) {                         // (fresh rows' is 0, or they stay fresh)
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[db][i] *= alpha;
+                for (int i = 0; i < 16; ++i) acc[db][i] = fresh ? 0.0f : acc[db][i] * alpha;
         }
         const float mc = fmaxf(m_run * c2, kLowest);
         float ls = 0.0f;
@@ -469,6 +475,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     // ---- the rows leave.  With two tiles a step the two waves of a row block merge first: each finishes half of the dims, leaves
     //      the other half with its (max, sum) in LDS and takes its own of the other wave.
     l_run += __shfl_xor(l_run, 32, kWave);
+    if (__any(m_run == kLowest))                                   // rows that saw no key here: zeros, as above
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] = m_run == kLowest ? 0.0f : acc[db][i];
     constexpr int HB = DB / TP, kArea = TP == 2 ? HB * 4 * 1024 : 0;         // 32-dim blocks a wave finishes, bytes it leaves
     constexpr int kMl = TP == 2 ? 512 : 0;
     typedef float floatx4 __attribute__((ext_vector_type(4)));

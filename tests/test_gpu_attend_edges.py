@@ -138,3 +138,24 @@ def test_an_infinity_in_the_newest_value_of_each_of_many(dy, dtype, d):
     c.cache.v.copy_(c.v)
     out[:, 2:, 5] = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale)[:, 2:, 5]
     c.check(out)
+
+
+# ---- queries that are no numbers
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("form,dtype,d", with_forms((BF16, 128), (BF16, 64), (F32, 64)), ids=str)
+@pytest.mark.parametrize("tree", [False, True], ids=["causal", "tree"])
+def test_a_query_that_is_no_number_is_no_matter_to_other_rows(dy, form, dtype, d, tree, bad):
+    """Not in one bit: rows are taken 32 at a time (those beside it may go by another reference), and no others are done again."""
+    print("form", form, dtype, d, tree, bad, flush=True)
+    n, context = 90, 700
+    c = Paged((n,), (context,), 4, 2, d, dtype, 16, 51, mask=random_mask((n,), 12)[0] if tree else None)
+    st, clean = in_form(dy, form, c)
+    assert st == 0
+    c.q_dev[20, 1, 7], c.q_dev[50, 0, 3] = bad, bad               # rows 41 and 100 of the first KV head
+    st, out = in_form(dy, form, c)
+    assert st == 0 and torch.isnan(out[20, 1]).all() and torch.isnan(out[50, 0]).all()
+    rows = (torch.arange(n)[:, None] * 2 + torch.arange(4)[None] % 2) // 32
+    others = (torch.arange(4)[None] >= 2) | ((rows != 41 // 32) & (rows != 100 // 32))
+    whole = torch.int16 if dtype is BF16 else torch.int32
+    assert others.sum() > 200 and torch.equal(out.cpu()[others].view(whole), clean.cpu()[others].view(whole))
