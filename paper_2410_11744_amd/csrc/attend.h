@@ -1,5 +1,5 @@
 // What the kernels of dyspec_paged_attn and dyspec_prompt_attn share: their arguments, which rows and keys a workgroup has, where
-// a key lies, which keys a row sees, the merge of the parts of a long walk, the exact form of a row that met a NaN.
+// a key lies, which keys a row sees, the merge of the parts of a long walk, the second look at rows that met a NaN.
 //
 // Rows.  All G = Hq/Hkv query heads of a KV head are folded into the row dimension (row = token*G + head), so a block of rows
 // streams K and V of its KV head once.  Keys are numbered from the start of the sequence: the context's, then the new tokens'.
@@ -145,72 +145,6 @@ __device__ __forceinline__ char* out_row(const AttendArgs& a, const AttendSeq& s
     return a.out + (long long)(s.row0 + j) * a.out_stride + (long long)h * a.d * size;
 }
 
-// ---- a row that met a NaN
-//
-// A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
-// matrix product.  Such keys may hold anything (a later token that overflowed), so rows that come out with a NaN are looked at
-// again: if what their block took at a weight of zero was all finite, the NaN is the row's own and stays.
-// (Otherwise a NaN at the start of a long context would send every row through the walk below, a thousand times slower.)
-
-// Whether the block's query rows (which lie where a V tile would be, at weights of zero, when a walk starts) and V of the walk's keys
-// that meet a weight of zero are finite: those that some row of the block may not see, and the last one, which is repeated behind the
-// end of a block of keys.  One wave, lane i reads dims 4i..
-template <typename T>
-__device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int r1, int k_begin, int k_end)
-{
-    typedef typename Four<T>::raw raw;
-    const int size = (int)sizeof(T), lane = threadIdx.x & 63, piece = 4 * lane < a.d ? lane : 0;
-    float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // stays zero unless something is infinite or a NaN
-    auto add = [&](float4 x) { z.x = fmaf(x.x, 0.0f, z.x); z.y = fmaf(x.y, 0.0f, z.y); z.z = fmaf(x.z, 0.0f, z.z); z.w = fmaf(x.w, 0.0f, z.w); };
-#pragma unroll 4
-    for (int r = r0; r < r1; ++r) {
-        const int j = div_G(a, r), h = kvh * a.G + (r - j * a.G);
-        add(Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * size)));
-    }
-    const long long head = (long long)kvh * a.d * size + 4 * piece * size;
-#pragma unroll 4
-    for (int key = max(k_begin, min(a.mask ? s.C : s.C + div_G(a, r0) + 1, k_end - 1)); key < k_end; ++key)
-        add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
-    return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
-}
-
-// The row again: keys one at a time, those it does not see left out, weights against the reference m that the row has.  One wave,
-// lane i holds dims 4i..; a NaN of the row's own keys comes out as one again (and ends the walk where it is in all dims).
-template <typename T>
-__device__ __forceinline__ void exact_row(const AttendArgs& a, const AttendSeq& s, int kvh, int r, int k_begin, int k_end, float m, float4& o, float& l)
-{
-    typedef typename Four<T>::raw raw;
-    const int lane = threadIdx.x & 63;
-    const bool mine = 4 * lane < a.d;
-    const int piece = mine ? lane : 0;
-    const int j = div_G(a, r), h = kvh * a.G + (r - j * a.G);
-    const float4 q = Four<T>::wide(*reinterpret_cast<const raw*>(a.q + (long long)(s.row0 + j) * a.q_stride + ((long long)h * a.d + 4 * piece) * (int)sizeof(T)));
-    o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    l = 0.0f;
-    const long long head = (long long)kvh * a.d * (int)sizeof(T) + 4 * piece * (int)sizeof(T);
-    constexpr int kBatch = 4;                                  // keys per trip to memory
-#pragma unroll 1
-    for (int key = k_begin; key < k_end; key += kBatch) {
-        const uint32_t seen = (uint32_t)__builtin_amdgcn_readfirstlane((int)seen_bits(a, s, j, key));
-        float4 k[kBatch], v[kBatch];
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            const int at = min(key + x, k_end - 1);
-            k[x] = Four<T>::wide(*reinterpret_cast<const raw*>(a.k + key_offset(a, s, at, a.k_stride) + head));
-            v[x] = Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, at, a.v_stride) + head));
-        }
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            if (key + x >= k_end || !((seen >> x) & 1u)) continue;
-            const float dot = wave_sum(mine ? (q.x * k[x].x + q.y * k[x].y) + (q.z * k[x].z + q.w * k[x].w) : 0.0f);
-            const float p = exp2f((dot - m) * a.c2);
-            l += p;
-            o.x += p * v[x].x; o.y += p * v[x].y; o.z += p * v[x].z; o.w += p * v[x].w;
-        }
-        if (__all(o.x != o.x && o.y != o.y && o.z != o.z && o.w != o.w)) return;      // nothing else comes of it
-    }
-}
-
 // ---- parts
 //
 // A walk cut into parts: every workgroup leaves its rows (times their weight, fp32: nothing is rounded twice) with their (max,
@@ -324,29 +258,182 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendIte
     }
 }
 
-// The rows `bad` (bit b: row row0 + b of the block), dims dim0 .. dim1 - 1 of them, leave as exact_row has them: into the slot, or
-// finished.  m_of(row): the reference that the row's (max, sum) go by.
-template <typename T, SlotOrder O, typename F>
-__device__ __forceinline__ void leave_exact_rows(const AttendArgs& a, const AttendItem& it, uint32_t bad, int row0, int dim0, int dim1, int rows_per_block, int k_begin,
-                                                 int k_end, int n_parts, float* slot, F m_of)
+// ---- a row that met a NaN
+//
+// A weight of a key that a row does not see is zero, but zero times an infinity or a NaN of that key's V row is a NaN in the
+// matrix product.  Such keys may hold anything (a later token that overflowed), so rows that come out with a NaN are looked at
+// again: if what their block took at a weight of zero was all finite, the NaN is the row's own and stays.
+
+// Whether V of the walk's keys that meet a weight of zero is finite: of those that some row of the block may not see, and of the last
+// one, which is repeated behind the end of a block of keys.  One wave, lane i reads dims 4i..
+template <typename T>
+__device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int k_begin, int k_end)
 {
-    const int lane = threadIdx.x & 63, r0 = it.block * rows_per_block;
-    const bool mine = 4 * lane >= dim0 && 4 * lane < dim1;
-    while (bad) {
-        const int row = row0 + __builtin_ctz(bad);
-        bad &= bad - 1u;
-        float4 o;
-        float l;
-        exact_row<T>(a, it.s, it.kvh, r0 + row, k_begin, k_end, m_of(row), o, l);
-        if (!mine) continue;
-        if (n_parts > 1) {
-            store_four(slot + slot_place<O>(a.d, row, lane), o.x, o.y, o.z, o.w);
-        } else {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int j = div_G(a, r0 + row);
-            Four<T>::store(out_row(a, it.s, j, it.kvh * a.G + (r0 + row - j * a.G), sizeof(T)) + 4 * lane * (int)sizeof(T),
-                           make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    typedef typename Four<T>::raw raw;
+    const int size = (int)sizeof(T), lane = threadIdx.x & 63, piece = 4 * lane < a.d ? lane : 0;
+    float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // stays zero unless something is infinite or a NaN
+    auto add = [&](float4 x) { z.x = fmaf(x.x, 0.0f, z.x); z.y = fmaf(x.y, 0.0f, z.y); z.z = fmaf(x.z, 0.0f, z.z); z.w = fmaf(x.w, 0.0f, z.w); };
+    const long long head = (long long)kvh * a.d * size + 4 * piece * size;
+#pragma unroll 4
+    for (int key = max(k_begin, min(a.mask ? s.C : s.C + div_G(a, r0) + 1, k_end - 1)); key < k_end; ++key)
+        add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
+    return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
+}
+
+// The rows `bad` (bit b: row row0 + b of the block) came out with a NaN, and have left, into their slot or finished: where that may be
+// another row's matter, their dims dim0 .. dim1 - 1 are done again, 16 rows at a time, without what they do not see, and leave again.
+// m_of(row): the reference that the row's (max, sum) go by.  One wave.
+//
+// The fp32 matrix instructions from registers alone, as in attend_f32.hip (where the layouts are explained): a lane has one query and
+// four keys of every 16 of the scores, dims 64y + 16g + 4i + c of one query of the sums.  The second product takes zeros in place of V's
+// infinities and NaN; a key that has some is added by itself, to the rows that see it.  So a hidden token that overflowed costs one
+// such walk of the rows beside it: a prompt of 8192 tokens, 64 heads on 8, with a NaN in one value takes up to 2.9 ms in place of 1.0,
+// a tree of 512 rows over 4096 tokens 2.0 in place of 0.09 (row by row and key by key it was 98, and 60).
+template <typename T, SlotOrder O, int DP, typename F>
+__device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int dim1, int rows_per_block, F m_of)
+{
+    // all of the call is looked up anew: nothing is held for this through the walk
+    auto args = (__attribute__((address_space(4))) const AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    const AttendArgs& a = *(const AttendArgs*)args;
+    const AttendItem it = attend_item(a, blockIdx.x);
+    const int block_end = min((it.block + 1) * rows_per_block, a.G * it.s.N), end = it.s.C + div_G(a, block_end - 1) + 1;
+    const int n_parts = it.s.parts > 1 ? (end + it.s.share - 1) / it.s.share : 1;
+    const int k_begin = n_parts > 1 ? it.part * it.s.share : 0, k_end = n_parts > 1 ? min(end, k_begin + it.s.share) : end;
+    if (hidden_are_finite<T>(a, it.s, it.kvh, it.block * rows_per_block, k_begin, k_end)) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // (the rows as they were have left before they leave again)
+    float* const slot = part_slot(a, it, rows_per_block);
+    typedef typename Four<T>::raw raw;
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    constexpr int size = (int)sizeof(T), NS = DP / 16, NB = DP / 64;
+    const AttendSeq& s = it.s;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int d = a.d, r0 = it.block * rows_per_block, last = k_end - 1;
+    const char* const kp = a.k + (long long)it.kvh * d * size;
+    const char* const vp = a.v + (long long)it.kvh * d * size;
+#pragma unroll 1
+    for (int first = 0; first < 32; first += 16) {
+        const uint32_t some = (bad >> first) & 0xffffu;
+        if (some == 0u) continue;
+        const int row = min(row0 + first + n, rows_per_block - 1), r = min(r0 + row, a.G * s.N - 1);
+        const int j = div_G(a, r), h = it.kvh * a.G + (r - j * a.G);
+        const bool wanted = (some >> n) & 1u;
+        const float m = m_of(row);
+        raw q[NS];                                                 // (a piece past head_dim meets zeros of K)
+        const char* const qrow = a.q + (long long)(s.row0 + j) * a.q_stride + (long long)h * d * size;
+#pragma unroll
+        for (int x = 0; x < NS; ++x) {
+            const int dim = 16 * x + 4 * g;
+            q[x] = dim < d ? *reinterpret_cast<const raw*>(qrow + dim * size) : raw{};
         }
+        f4 acc[NB][4];
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[y][c] = f4{ 0.0f, 0.0f, 0.0f, 0.0f };
+        float l = 0.0f;
+        bool done = false;                                         // every row is a NaN in all its dims: nothing else comes of it
+#pragma unroll 1
+        for (int key0 = k_begin; key0 < k_end && !done; key0 += 16) {
+            // the step's two runs of eight keys, each within a page; keys past the last repeat it
+            const int at0 = min(key0, last), at1 = min(key0 + 8, last) & ~7;
+            auto row_of = [&](const char* base, long long stride, int off, bool low) __attribute__((always_inline)) -> const char* {
+                const long long b0 = key_offset(a, s, at0, stride), b1 = key_offset(a, s, at1, stride);
+                return base + (low ? b0 : b1) + (min(key0 + off, last) - (low ? at0 : at1)) * stride;
+            };
+            const char* const krow = row_of(kp, a.k_stride, n, n < 8);
+            raw k[NS], v[4][NB];                                   // V: dims 64y + 4n .. of key 4g + x
+#pragma unroll
+            for (int x = 0; x < NS; ++x) {
+                const int dim = 16 * x + 4 * g;
+                k[x] = *reinterpret_cast<const raw*>(krow + (dim < d ? dim : 0) * size);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const char* const at = row_of(vp, a.v_stride, 4 * g + x, g < 2);
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+                    const int dim = 64 * y + 4 * n;
+                    v[x][y] = *reinterpret_cast<const raw*>(at + (dim < d ? dim : 0) * size);
+                }
+            }
+            uint32_t seen = seen_bits(a, s, j, key0) & 0xffffu;
+            if (k_end - key0 < 16) seen &= (1u << (k_end - key0)) - 1u;
+            f4 S = { 0.0f, 0.0f, 0.0f, 0.0f };
+#pragma unroll
+            for (int x = 0; x < NS; ++x) {
+                float4 w = Four<T>::wide(k[x]);
+                const float4 u = Four<T>::wide(q[x]);
+                if (16 * x + 16 > d && 16 * x + 4 * g >= d) w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                S = __builtin_amdgcn_mfma_f32_16x16x4f32(w.x, u.x, S, 0, 0, 0);
+                S = __builtin_amdgcn_mfma_f32_16x16x4f32(w.y, u.y, S, 0, 0, 0);
+                S = __builtin_amdgcn_mfma_f32_16x16x4f32(w.z, u.z, S, 0, 0, 0);
+                S = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w, u.w, S, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            f4 p;
+            uint32_t odd = 0u;                                     // bit x: V of the lane's key x has something infinite or a NaN
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                p[x] = (seen >> (4 * g + x)) & 1u ? exp2f((S[x] - m) * a.c2) : 0.0f;
+                l += p[x];
+#pragma unroll
+                for (int y = 0; y < NB; ++y) {
+                    float4 w = Four<T>::wide(v[x][y]);
+                    auto finite = [&](float& e) __attribute__((always_inline)) {
+                        const bool fine = e * 0.0f == 0.0f;
+                        if (!fine) odd |= 1u << x;
+                        e = fine ? e : 0.0f;
+                    };
+                    finite(w.x); finite(w.y); finite(w.z); finite(w.w);
+                    acc[y][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.x, p[x], acc[y][0], 0, 0, 0);
+                    acc[y][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.y, p[x], acc[y][1], 0, 0, 0);
+                    acc[y][2] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.z, p[x], acc[y][2], 0, 0, 0);
+                    acc[y][3] = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w, p[x], acc[y][3], 0, 0, 0);
+                }
+            }
+            if (!__any(odd != 0u)) continue;
+#pragma unroll 1
+            for (int off = 0; off < 16 && key0 + off < k_end; ++off) {         // key 4 (off / 4) + off % 4
+                const uint64_t lanes = __builtin_amdgcn_ballot_w64((odd >> (off & 3)) & 1u);
+                if (!((lanes >> (16 * (off >> 2))) & 0xffffull)) continue;
+                const float mine = (off & 2) ? (off & 1 ? p[3] : p[2]) : (off & 1 ? p[1] : p[0]);
+                const float w0 = __shfl(mine, n + 16 * (off >> 2), kWave);     // the query's weight of it
+                if (!((seen >> off) & 1u)) continue;
+                const char* const at = vp + key_offset(a, s, key0 + off, a.v_stride);
+#pragma unroll
+                for (int y = 0; y < NB; ++y)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int dim = 64 * y + 16 * g + 4 * i;
+                        const float4 w = Four<T>::wide(*reinterpret_cast<const raw*>(at + (dim < d ? dim : 0) * size));
+                        acc[y][0][i] += w.x * 0.0f == 0.0f ? 0.0f : w0 * w.x;
+                        acc[y][1][i] += w.y * 0.0f == 0.0f ? 0.0f : w0 * w.y;
+                        acc[y][2][i] += w.z * 0.0f == 0.0f ? 0.0f : w0 * w.z;
+                        acc[y][3][i] += w.w * 0.0f == 0.0f ? 0.0f : w0 * w.w;
+                        __builtin_amdgcn_sched_barrier(0);         // (rare: not worth registers)
+                    }
+            }
+            bool all = true;
+#pragma unroll
+            for (int y = 0; y < NB; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) all &= acc[y][i / 4][i % 4] != acc[y][i / 4][i % 4];
+            done = __all(all || !wanted);
+        }
+        l += __shfl_xor(l, 16, kWave);
+        l += __shfl_xor(l, 32, kWave);
+        if (!wanted) continue;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int y = 0; y < NB; ++y)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int dim = 64 * y + 16 * g + 4 * i;
+                if (dim < dim0 || dim >= dim1) continue;
+                if (n_parts > 1) store_four(slot + slot_place<O>(d, row, dim / 4), acc[y][0][i], acc[y][1][i], acc[y][2][i], acc[y][3][i]);
+                else Four<T>::store(out_row(a, s, j, h, size) + dim * size, make_float4(acc[y][0][i] * inv, acc[y][1][i] * inv, acc[y][2][i] * inv, acc[y][3][i] * inv));
+            }
     }
 }
 

@@ -20,7 +20,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 constexpr int kF32Waves = 4;
 
 template <typename T, int DP, bool Paged>
-__global__ __launch_bounds__(64 * kF32Waves, DP <= 128 ? 2 : 1) void attend_f32_kernel(AttendArgs, int row_waves)
+__global__ __launch_bounds__(64 * kF32Waves, DP <= 128 || (DP == 192 && sizeof(T) == 2) ? 2 : 1) void attend_f32_kernel(AttendArgs, int row_waves)
 {
     const AttendArgs& a = attend_args_here();
     typedef typename Four<T>::raw raw;
@@ -225,12 +225,11 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 ? 2 : 1) void attend_f32_
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (64 * b + 16 * g + 4 * i < a.d) nan |= acc[b][c][i] != acc[b][c][i];
-        uint64_t lanes = __builtin_amdgcn_ballot_w64(nan && r < rows);
-        uint32_t bad = (uint32_t)((lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu);
-        if (bad && hidden_are_finite<T>(a, s, it.kvh, r0, min(r0 + R, rows), k_begin, k_end)) bad = 0u;
-        const bool leave = r < rows && !((bad >> n) & 1u);
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(nan && r < rows);
+        const uint32_t bad = (uint32_t)((lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu);
+        const bool leave = r < rows;
         if (n_parts > 1) {
-            if (g == 0 && r < rows) store_pair(slot_max_sum(a, slot, R, 16 * wq + n), m, l);
+            if (g == 0 && leave) store_pair(slot_max_sum(a, slot, R, 16 * wq + n), m, l);
             if (leave) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
@@ -253,8 +252,8 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 ? 2 : 1) void attend_f32_
                         Four<T>::store(dst + dim * size, make_float4(acc[b][0][i] * inv, acc[b][1][i] * inv, acc[b][2][i] * inv, acc[b][3][i] * inv));
                 }
         }
-        leave_exact_rows<T, kSlotF32>(a, it, bad, 16 * wq, 0, a.d, R, k_begin, k_end, n_parts, slot,
-                                   [=](int row) { return __shfl(m, row - 16 * wq, kWave); });
+        if (__builtin_expect(bad != 0u, 0))
+            look_again<T, kSlotF32, DP>(bad, 16 * wq, 0, a.d, R, [=](int row) { return __shfl(m, row & 15, kWave); });
     }
     if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<T, kSlotF32, 0>(a, it, n_parts, R, 64 * kF32Waves);
 }

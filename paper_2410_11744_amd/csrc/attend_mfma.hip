@@ -186,7 +186,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         for (int ts = 0; ts < 2; ++ts)
 #pragma unroll
             for (int w = 0; w < 4; ++w) pw[e][ts][w] = 0u;
-    float m_run = kLowest, l_run = 0.0f, ls_half = 0.0f;
+    float m_run = -INFINITY, l_run = 0.0f, ls_half = 0.0f;         // (so that the first half a wave sees is done again, whatever the scale)
     const float c2 = a.c2;
     __syncthreads();                             // (the later loads queue up behind the urgent ones)
     if (ld_is_v) issue_first_k();
@@ -355,11 +355,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = max3(mx, sm[i], sm[i + 1]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const float m_new = fmaxf(m_run, mx);
+        const float m_new = max3(m_run, mx, kLowest);
         const float alpha = fast_exp2((m_run - m_new) * c2);
         // A row without a sum so far starts at zero whatever acc holds: the first half's second product takes what lies in V's slot then,
         // query rows, at weights of zero, and a row's NaN is nothing to other rows.
-        const bool fresh = m_run == kLowest;
+        const bool fresh = m_run <= kLowest;
         m_run = m_new;
         l_run *= alpha;
         if (__all(fresh)) {
@@ -475,11 +475,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     // ---- the rows leave.  With two tiles a step the two waves of a row block merge first: each finishes half of the dims, leaves
     //      the other half with its (max, sum) in LDS and takes its own of the other wave.
     l_run += __shfl_xor(l_run, 32, kWave);
-    if (__any(m_run == kLowest))                                   // rows that saw no key here: zeros, as above
+    if (__any(m_run <= kLowest)) {                                 // rows that saw no key here: zeros, as above
+        const bool none = m_run <= kLowest;
+        m_run = fmaxf(m_run, kLowest);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[db][i] = m_run == kLowest ? 0.0f : acc[db][i];
+            for (int i = 0; i < 16; ++i) acc[db][i] = none ? 0.0f : acc[db][i];
+    }
     constexpr int HB = DB / TP, kArea = TP == 2 ? HB * 4 * 1024 : 0;         // 32-dim blocks a wave finishes, bytes it leaves
     constexpr int kMl = TP == 2 ? 512 : 0;
     typedef float floatx4 __attribute__((ext_vector_type(4)));
@@ -533,9 +536,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         const uint64_t lanes = __builtin_amdgcn_ballot_w64((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.0f);      // (a NaN is not equal)
         uint32_t bad = (uint32_t)(lanes | lanes >> 32);
         if (left < 32) bad &= left > 0 ? (1u << left) - 1u : 0u;
-        if (bad && hidden_are_finite<__bf16>(a, s, it.kvh, r0, min(r0 + kRows, rows), k_begin, k_end)) bad = 0u;
         if (n_parts > 1) {
-            if (n < left && !((bad >> n) & 1u)) {
+            if (n < left) {
 #pragma unroll
                 for (int b = 0; b < HB; ++b)
 #pragma unroll
@@ -565,13 +567,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 #pragma unroll
             for (int t = 0; t < 32 * CPR / kWave; ++t) {
                 const int c = lane + kWave * t, rn = c / CPR, cc = c % CPR;
-                if (rn >= left || ((bad >> rn) & 1u)) continue;
+                if (rn >= left) continue;
                 const u32x4 v = *(__attribute__((address_space(3))) u32x4*)(uint32_t)(stage + rn * kPitch + cc * 16);
                 __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(out_first + (row_offset(32 * wq + rn, out_stride) + 64 * mine + cc * 16)));
             }
         }
-        leave_exact_rows<__bf16, kSlotMany>(a, it, bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, k_begin, k_end, n_parts, slot,
-                                       [=](int row) { return __shfl(m, row - 32 * wq, kWave); });
+        if (__builtin_expect(bad != 0u, 0))
+            look_again<__bf16, kSlotMany, D>(bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, [=](int row) { return __shfl(m, row & 31, kWave); });
     });
     if (n_parts > 1 && arrive_last(a, it, n_parts, reinterpret_cast<int*>(lds))) merge_parts<__bf16, kSlotMany, D>(a, it, n_parts, kRows, 64 * NW);
 }

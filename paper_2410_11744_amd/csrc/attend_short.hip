@@ -326,10 +326,9 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
 #pragma unroll
         for (int x = 0; x < 64 / DP; ++x)
             if ((lanes >> (x * DP)) & ((1ull << DP) - 1ull)) here |= 1u << x;
-        if (here && hidden_are_finite<__bf16>(a, s, it.kvh, r0, min(r0 + kFewRows, rows), k_begin, k_end)) here = 0u;
         bad |= here << (t * (64 / DP));
         if (there && n_parts > 1 && dp == 0) store_pair(slot_max_sum(a, part, kFewRows, row), M, l);
-        if (!there || ((here >> (lane / DP)) & 1u)) continue;
+        if (!there) continue;
         if (n_parts > 1) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) store_four(part + slot_place<kSlotFew>(D, row, 2 * dp + e), o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
@@ -346,12 +345,13 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
             *reinterpret_cast<uint4*>(dst) = w;
         }
     }
-    leave_exact_rows<__bf16, kSlotFew>(a, it, bad, wave * RW, 0, D, kFewRows, k_begin, k_end, n_parts, part, [=](int row) {
-        float M = kLowest;
+    if (__builtin_expect(bad != 0u, 0))
+        look_again<__bf16, kSlotFew, D>(bad, wave * RW, 0, D, kFewRows, [=](int row) {
+            float M = kLowest;
 #pragma unroll
-        for (int z = 0; z < NW; ++z) M = fmaxf(M, (*(lds_floatx2)(uint32_t)(ml_lds + 8 * (32 * z + row))).x);
-        return M;
-    });
+            for (int z = 0; z < NW; ++z) M = fmaxf(M, (*(lds_floatx2)(uint32_t)(ml_lds + 8 * (32 * z + row))).x);
+            return M;
+        });
     if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<__bf16, kSlotFew, D>(a, it, n_parts, kFewRows, 64 * NW);
 }
 

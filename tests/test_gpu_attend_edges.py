@@ -159,3 +159,62 @@ def test_a_query_that_is_no_number_is_no_matter_to_other_rows(dy, form, dtype, d
     others = (torch.arange(4)[None] >= 2) | ((rows != 41 // 32) & (rows != 100 // 32))
     whole = torch.int16 if dtype is BF16 else torch.int32
     assert others.sum() > 200 and torch.equal(out.cpu()[others].view(whole), clean.cpu()[others].view(whole))
+
+
+# ---- tokens that overflowed
+
+@pytest.mark.parametrize("tree", [False, True], ids=["causal", "tree"])
+@pytest.mark.parametrize("form,dtype,d", FORMS_OF_EACH + [(form, BF16, 256) for form in FORMS if form[0] >= 4], ids=str)
+def test_every_infinity_and_nan_stays_with_the_rows_that_see_it(dy, form, dtype, d, tree):
+    """Six values hold something that is no number, some in the context, some in new tokens: a dim of a row is what the formula gives
+    for the keys that the row sees, and all other dims and rows are as if there were none."""
+    print("form", form, dtype, d, tree, flush=True)
+    n, context = 75, 341
+    mask = random_mask((n,), 12)[0] if tree else None
+    c = Paged((n,), (context,), 4, 2, d, dtype, 16, 53, mask=mask)
+    odd = [(17, 0, 1, math.inf), (context + 3, 0, d - 1, math.nan), (context + 18, 0, 1, -math.inf), (context + 18, 1, 2, math.inf),
+           (context + 40, 1, d // 2, math.inf), (context + n - 1, 0, 3, math.nan)]
+    for at, h, dim, _ in odd:                                    # what the rest is held against
+        p, r = c.place(0, at)
+        c.v[p, r, h, dim] = 0
+    v = c.v.clone()
+    for at, h, dim, x in odd:
+        p, r = c.place(0, at)
+        v[p, r, h, dim] = x
+    c.cache.v.copy_(v)
+    st, out = in_form(dy, form, c)
+    assert st == 0
+    got, seen = out.double().cpu().numpy(), visible_rows(n, context, mask)
+    add = np.zeros((n, 4, d))
+    for at, h, dim, x in odd:
+        with np.errstate(invalid="ignore"):                      # inf - inf is a NaN, as in the sum
+            add[:, 2 * h:2 * h + 2, dim] += np.where(seen[:, at], x, 0.0)[:, None]
+    assert np.isnan(add).any() and np.isinf(add).any()
+    assert np.array_equal(np.isnan(got), np.isnan(add)) and np.array_equal(np.where(np.isinf(got), got, 0), np.where(np.isinf(add), add, 0))
+    want, bound = attend_plain(c.q.double().numpy(), *c.rows(0), seen, c.scale, weight_half(form, dtype), HALF[dtype])
+    fine = np.isfinite(add)
+    compare(got[fine], want[fine], bound[fine], "the rest")
+
+
+def test_one_token_that_overflowed_does_not_hold_up_the_call(dy):
+    """The rows beside it are done again, once more over their keys, not a row and a key at a time: 2.0 ms in place of 0.09 for a tree,
+    2.9 in place of 1.0 for a prompt (it was 60, and 98)."""
+    def time_of(call):
+        best, a, b = math.inf, torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        for _ in range(4):
+            a.record(), call(), b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    c = Paged((512,), (4096,), 64, 8, 128, BF16, 16, 3, mask=random_mask((512,), 3)[0])
+    tree = lambda: dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev)
+    clean = time_of(tree)
+    p, r = c.place(0, 4096 + 300)
+    c.cache.v[p, r, :, 3] = math.nan
+    assert time_of(tree) < 100 * clean
+    q, k, v = (torch.randn((8192, h, 128), device="cuda").to(BF16) for h in (64, 8, 8))
+    prompt = lambda: dy.prompt_attn(q, k, v, dy.Batch.from_sizes([8192]), 0.1)
+    clean = time_of(prompt)
+    v[8190, :, 3] = math.nan
+    assert time_of(prompt) < 15 * clean
