@@ -450,7 +450,8 @@ size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_
  *   accepted_nodes  DEVICE [sum N] i32, n_accepted DEVICE [n_seq] i32: as written by dyspec_verify.  Entries
  *                   are ascending rows of the tree without the root; one that is not behind its new place's
  *                   predecessor (<= i) or not below N moves nothing
- *   cache           layer 0; layer l's pages are l * layer_stride elements further (a multiple of 16 bytes)
+ *   cache           layer 0; layer l's pages are l * layer_stride elements further (a multiple of 16 bytes, with several layers at
+ *                   least a page): no page of one layer may lie on one of another, nor K on V, for all are moved at once
  *   n_layers        1 .. 32767
  */
 dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int64_t layer_stride,

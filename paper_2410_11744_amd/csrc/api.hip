@@ -544,6 +544,8 @@ dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int
     if (!accepted_nodes || !n_accepted || !aligned(accepted_nodes, 4) || !aligned(n_accepted, 4)) return DYSPEC_BAD_ARG;
     const int elt = dtype == DYSPEC_F32 ? 4 : 2;
     if (n_layers < 1 || n_layers > 32767 || layer_stride < 0 || layer_stride > ((int64_t)1 << 44) || (layer_stride * elt) % 16) return DYSPEC_BAD_SHAPE;
+    // (layers are moved beside each other: no page of one may lie on a page of the next)
+    if (n_layers > 1 && layer_stride < (int64_t)cache->page_size * n_kv_heads * head_dim) return DYSPEC_BAD_SHAPE;
     KeepHead a;
     Sequences<DYSPEC_MAX_SEQ> seq;
     a.k_pages = static_cast<char*>(cache->k); a.v_pages = static_cast<char*>(cache->v);
