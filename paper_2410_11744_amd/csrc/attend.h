@@ -265,7 +265,7 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendIte
 // again: if what their block took at a weight of zero was all finite, the NaN is the row's own and stays.
 
 // Whether V of the walk's keys that meet a weight of zero is finite: of those that some row of the block may not see, and of the last
-// one, which is repeated behind the end of a block of keys.  One wave, lane i reads dims 4i..
+// one, if it may be repeated to fill a block of (up to 64) keys.  One wave, lane i reads dims 4i..
 template <typename T>
 __device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int k_begin, int k_end)
 {
@@ -274,8 +274,9 @@ __device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const Att
     float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // stays zero unless something is infinite or a NaN
     auto add = [&](float4 x) { z.x = fmaf(x.x, 0.0f, z.x); z.y = fmaf(x.y, 0.0f, z.y); z.z = fmaf(x.z, 0.0f, z.z); z.w = fmaf(x.w, 0.0f, z.w); };
     const long long head = (long long)kvh * a.d * size + 4 * piece * size;
+    const int hidden = max(k_begin, a.mask ? s.C : s.C + div_G(a, r0) + 1), repeated = (k_end - k_begin) % 64 ? k_end - 1 : k_end;
 #pragma unroll 4
-    for (int key = max(k_begin, min(a.mask ? s.C : s.C + div_G(a, r0) + 1, k_end - 1)); key < k_end; ++key)
+    for (int key = min(hidden, repeated); key < k_end; ++key)
         add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
     return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
 }

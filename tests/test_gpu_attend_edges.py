@@ -218,3 +218,20 @@ def test_one_token_that_overflowed_does_not_hold_up_the_call(dy):
     clean = time_of(prompt)
     v[8190, :, 3] = math.nan
     assert time_of(prompt) < 15 * clean
+
+
+@pytest.mark.parametrize("form,dtype,d", with_forms((BF16, 128), (BF16, 64), (F32, 64)), ids=str)
+def test_a_nan_that_all_rows_see_is_not_looked_for_again(dy, form, dtype, d):
+    """One token whose own value has a NaN, its keys whole blocks: the other dims have the same bits as without it."""
+    for context in (63, 127, 511):
+        print("form", form, dtype, d, context, flush=True)
+        c = Paged((1,), (context,), 4, 2, d, dtype, 16, 57)
+        p, r = c.place(0, context)
+        c.cache.v[p, r, :, 3] = 0
+        st, clean = in_form(dy, form, c)
+        c.cache.v[p, r, :, 3] = math.nan
+        st2, out = in_form(dy, form, c)
+        assert st == st2 == 0 and torch.isnan(out[0, :, 3]).all()
+        whole = torch.int16 if dtype is BF16 else torch.int32
+        rest = [x for x in range(d) if x != 3]
+        assert torch.equal(out[..., rest].contiguous().view(whole), clean[..., rest].contiguous().view(whole))
