@@ -235,3 +235,19 @@ def test_a_nan_that_all_rows_see_is_not_looked_for_again(dy, form, dtype, d):
         whole = torch.int16 if dtype is BF16 else torch.int32
         rest = [x for x in range(d) if x != 3]
         assert torch.equal(out[..., rest].contiguous().view(whole), clean[..., rest].contiguous().view(whole))
+
+
+@pytest.mark.parametrize("tree", [False, True], ids=["causal", "tree"])
+@pytest.mark.parametrize("form,dtype,d", with_forms((BF16, 128), (BF16, 64), (F32, 64)), ids=str)
+def test_a_scale_of_nearly_nothing(dy, form, dtype, d, tree):
+    """All weights alike, beside a query that is no number: no running reference is ever passed by much."""
+    print("form", form, dtype, d, tree, flush=True)
+    n, context = 90, 130
+    c = Paged((n,), (context,), 4, 2, d, dtype, 16, 59, mask=random_mask((n,), 12)[0] if tree else None)
+    c.scale = 1e-38
+    c.q_dev[20, 1, 7] = math.nan
+    st, out = in_form(dy, form, c)
+    assert st == 0 and torch.isnan(out[20, 1]).all()
+    c.q_dev[20, 1, 7] = 0
+    out[20, 1] = in_form(dy, form, c)[1][20, 1]
+    check(c, out, form)
