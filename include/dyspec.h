@@ -419,7 +419,8 @@ dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, i
  * over every key of the context and, of the new tokens, key i if i <= j and (with a mask) bit i of
  * anc_mask row j is set.  A row that sees no key comes out as zeros.  Keys that a row does not see do not
  * matter to it, whatever they hold (infinities and NaN among it); rows of the pages behind a sequence's
- * last token are not read.
+ * last token are not read.  An infinity that a row sees in V comes out as one, or as a NaN where its weight
+ * is below 2^-126 of the row's largest.  (Keys that hold such things cost their row block a second walk.)
  *
  *   q, out     DEVICE [sum N, n_q_heads, head_dim] dense, distinct, 16-byte aligned
  *   anc_mask   NULL: causal.  Else DEVICE [sum N, mask_words] u64 as written by dyspec_build_tree, 8-byte

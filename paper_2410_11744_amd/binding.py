@@ -585,7 +585,8 @@ class PagedCache:
                 page, pages (and layers) may be strided: halves of one [n_pages, 2, page_size, Hkv, d] pool will do
     page_table  int32 [n_seq or more, max_pages]; rows may be strided
 
-    kv_append and paged_attn work on one layer (`layer(l)`), kv_keep on all at once."""
+    kv_append and paged_attn work on one layer (`layer(l)`: to be made once a layer, it costs more host time than a call), kv_keep on
+    all at once."""
     k: "torch.Tensor"
     v: "torch.Tensor"
     page_table: "torch.Tensor"

@@ -8,9 +8,18 @@ namespace dyspec {
 
 // A kernel as the choice sees it: a launch, then items (workgroups).  One that has a CU to itself takes `once` and `step` per
 // `keys` keys, more by the share `alone` over its sequence's row blocks (the first to read a key reads it from memory); of a CU
-// that is full, with `per_cu` items, each takes up `busy_once` and `busy_step`.  Microseconds, fitted to 230 shapes (1 to 64
-// sequences, 1 to 4096 new tokens, 0 to 16384 tokens of context, 1 to 32 KV heads, 1 to 8 query heads each): the choice is
-// 1.7 % (head_dim 128) and 3.6 % (64) from the best form on average.
+// that is full, with `per_cu` items, each takes up `busy_once` and `busy_step`.  Microseconds.  The bf16 kernels' are fitted to
+// measurements, those of the fp32 kernel are estimates, the same for all head sizes above 64.  How far the choice is from the best of
+// all kernels, each whole and in 2 to 32 parts (1 to 64 sequences, 1 to 4096 new tokens, 0 to 16384 tokens of context, 1 to 32 KV heads, 1 to
+// 8 query heads each; geometric mean, nine in ten, worst):
+//   bf16, 128   pages (153 shapes) 1.3 %, 7 %, 35 %: 256 tokens over 16384, 8 heads on 1, 47.0 us against 34.8 by attend_short.hip in 4 parts
+//               prompts (44) 1.5 %, 3.5 %, 23 %: six of 1500 to 20, 8 heads, 28.0 against 22.8 by attend_short.hip
+//   bf16, 64    pages (153) 3.2 %, 10 %, 22 %; prompts (44) 1.4 %, 5 %, 9 %
+//   fp32, 64    pages (95) 5.4 %, 18 %, 24 %; prompts (24) 1.1 %, 1.4 %, 18 %
+//   fp32, 128   pages (95) 7.4 %, 25 %, 30 %: one token over 300 stays whole, 16.5 against 12.7 in 3 parts; prompts (24) 1.4 %, 1.7 %, 30 %
+//   bf16, 80    pages (95) 6.2 %, 25 %, 29 %; prompts (24) 1.5 %, 1.6 %, 31 %
+//   bf16, 256   pages (95) 7.3 %, 26 %, 47 %: 64 tokens over 1500, 32 heads on 8, 96.0 against 65.3 with 16 rows a block in 2 parts;
+//               prompts (24) 2.3 %, 1.6 %, 35 %
 enum AttendKind { kFew8, kFew4, kMany8, kMany4, kF32Few, kF32Many, kKinds };
 struct KindCost { int rows, keys, per_cu; float launch, once, step, alone, busy_once, busy_step; };
 constexpr KindCost kCosts[2][kKinds] = {

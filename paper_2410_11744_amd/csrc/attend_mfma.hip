@@ -18,10 +18,12 @@
 // of eight rows that lie each within a page: their addresses are uniform over the wave and are made by the scalar unit from page
 // numbers which 64 lanes hold for 16 steps ahead.  So pages cost the vector and matrix units nothing.
 //
-// What bounds it: the power the card may draw.  Over a prompt of 8192 tokens the matrix cores are busy 70 % of the cycles, LDS 36 %,
-// and the clock goes down to 1.5 GHz; reading operands earlier, other wave priorities or orders of the loop's instructions change
-// nothing.  Measured, 64 query heads on 8: that prompt 0.92 to 1.04 ms, 1.06 to 1.19 PFLOP/s (a matrix product of 8192 cubed, by the
-// library: 1.34); a tree of 512 rows over 4096 tokens in pages of 16: 70 to 80 us, 0.86 to 0.98 PFLOP/s, by the clock that a card holds.
+// What bounds it: over a prompt of 8192 tokens, 64 query heads on 8, the power the card may draw: the matrix cores are busy 70 % of the
+// cycles, LDS 36 %, and the clock goes down to 1.5 GHz; reading operands earlier, other wave priorities or orders of the loop's
+// instructions change nothing (0.92 to 1.04 ms, 1.06 to 1.19 PFLOP/s by the clock that a card holds; a matrix product of 8192 cubed, by the
+// library: 1.34).  A tree of 512 rows over 4096 tokens in pages of 16, one row block a CU (70 to 80 us, 0.86 to 0.98 PFLOP/s), is another
+// matter: the matrix cores are busy 46 % of the cycles at 2.0 GHz.  17 us go without any context (launch, start, the tree's own tiles,
+// end), 14 to 15 with every 1024 tokens of it (1.2 PFLOP/s).
 #include <atomic>
 
 #include "attend.h"

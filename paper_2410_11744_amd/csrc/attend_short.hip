@@ -9,7 +9,7 @@
 //
 // What bounds it: for one token of many sequences memory (64 sequences of 500 to 8000 tokens, 8 KV heads of 128: 222 us, 5.6 TB/s,
 // what a kernel that only reads reaches); for one sequence the trips to memory one after the other (one token over 1024, 32 heads,
-// 17 MB: 10.5 us, of which memory could do with 3).  Eight waves a workgroup where the row blocks do not fill the chip, four where they do.
+// 17 MB: 10.8 us, of which memory could do with 3).  Eight waves a workgroup where the row blocks do not fill the chip, four where they do.
 #include <atomic>
 
 #include "attend.h"
