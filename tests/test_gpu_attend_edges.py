@@ -1,5 +1,6 @@
-"""Attention over pages and of prompts where one key decides: a score far above all others, an infinity that the last token sees.  Every kernel,
-whole and in parts (test_gpu_attend_forms.py), against the plain form in 64 bits (tests/serving.py: formulas and bounds)."""
+"""Attention over pages and of prompts at the edges of its numbers: a score far above all before it, infinities and NaN that some rows see
+and others do not, queries that are no numbers, a scale of nearly nothing.  Every kernel, whole and in parts (test_gpu_attend_forms.py),
+against the plain form in 64 bits (tests/serving.py: formulas and bounds)."""
 import ctypes
 import math
 
