@@ -477,6 +477,38 @@ dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k,
                                  float softmax_scale, void* out, void* hip_stream);
 
 /*
+ * dyspec_page_plan -- page tables and slot maps by the requests' lengths, on the device: sequence s has pages for
+ * held[s] tokens and is to have them for wanted[s].  With A = ceil(held / page_size) and B = ceil(wanted / page_size)
+ *   B > A   it takes B - A pages: page_table[s][A .. B-1] are the next free ones.  Demands are met in order of the
+ *           sequences as long as their sum is at most the pages that are free when the call starts; from the first
+ *           one that is not met on, no sequence gets any
+ *   B < A   it gives page_table[s][B .. A-1] back as they are (free for later calls); the entries become -1
+ * and granted[s] says for how many tokens it now has pages: wanted[s], or held[s] where its demand was not met, or
+ * -1 where a length is negative, above DYSPEC_MAX_CONTEXT or needs more than max_pages (nothing of it is changed).
+ * Pages that sequences share must not be given back while another sequence uses them: they are not counted.
+ *
+ *   pool        its free pages: state[1] of them, the first at ring[state[0]], the others behind it and on from ring[0]
+ *               after ring[n_pages - 1].  A full pool has state {0, n_pages, 0, 0} and every page's number in the ring
+ *   page_table  DEVICE, rows table_stride apart, as dyspec_paged_kv's; entries that no place reaches are not touched
+ *   held, wanted DEVICE [n_seq] i32
+ *   granted     DEVICE [n_seq] i32, none of held and wanted: it can be the next call's held
+ *   slots       DEVICE [n_slots] i64 or NULL, 8-byte aligned: where new tokens go, packed by sequences: for tokens
+ *               held[s] .. wanted[s] - 1 the row of the pool (page * page_size + row), -1 for all of a sequence whose
+ *               demand is not met.  What does not fit is left out, what is behind the last one stays as it is
+ *   n_seq       1 .. DYSPEC_MAX_SEQ
+ * Calls on one pool must be ordered (a stream does that).  No workspace; the other arrays 4-byte aligned.
+ */
+typedef struct {
+    int32_t* ring;                   /* DEVICE [n_pages]                                  */
+    int32_t* state;                  /* DEVICE [4]: first free place of the ring, free pages, 0, 0 */
+    int32_t n_pages;                 /* pages of the pool                                 */
+    int32_t page_size;               /* rows of a page: a power of two, 8 .. 65536        */
+} dyspec_page_pool;
+dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table, int32_t max_pages, int32_t table_stride,
+                               const int32_t* held, const int32_t* wanted, int32_t n_seq, int32_t* granted,
+                               int64_t* slots, int64_t n_slots, void* hip_stream);
+
+/*
  * Measurement helpers (no part of the method): ceilings to set beside the published peaks
  * of the chip, and the clock the chip runs at under load.  All only launch; the caller times
  * them (HIP events on hip_stream).

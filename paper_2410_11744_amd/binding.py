@@ -25,6 +25,7 @@ EXPORTS = ("dyspec_init", "dyspec_mask_words", "dyspec_workspace_bytes", "dyspec
            "dyspec_dfs_reorder", "dyspec_tree_attn", "dyspec_tree_attn_static_scratch", "dyspec_tree_attn_layers",
            "dyspec_tree_attn_layers_workspace_bytes", "dyspec_verify", "dyspec_verify_bf16",
            "dyspec_kv_append", "dyspec_kv_keep", "dyspec_paged_attn", "dyspec_paged_attn_workspace_bytes", "dyspec_prompt_attn",
+           "dyspec_page_plan",
            "dyspec_probe_mfma_bf16", "dyspec_probe_clock", "dyspec_probe_hbm_read")
 
 
@@ -49,6 +50,10 @@ class _Tree(ctypes.Structure):
 class _PagedKV(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_stride", ctypes.c_int64)]
+
+
+class _PagePool(ctypes.Structure):
+    _fields_ = [("ring", ctypes.c_void_p), ("state", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
 
 
 _lib = None
@@ -113,6 +118,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dyspec_paged_attn_workspace_bytes.argtypes = [PB, I32, I32, I32, I32]
     lib.dyspec_prompt_attn.restype = I32
     lib.dyspec_prompt_attn.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, V, V]
+    lib.dyspec_page_plan.restype = I32
+    lib.dyspec_page_plan.argtypes = [ctypes.POINTER(_PagePool), V, I32, I32, V, V, I32, V, V, I64, V]
     lib.dyspec_probe_mfma_bf16.restype = I32
     lib.dyspec_probe_mfma_bf16.argtypes = [I32, I32, ctypes.POINTER(ctypes.c_double), V, V]
     lib.dyspec_probe_clock.restype = I32
@@ -912,6 +919,77 @@ def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
     if stream is not None:
         _hand_over(stream, q, k, v, out)
     return (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ref, Hq, Hkv, d, code, softmax_scale, op, raw), out, device
+
+
+# ---------------------------------------------------------------------------------------- pages by the requests' lengths
+
+@dataclass(frozen=True)
+class PagePool:
+    """The free pages of a pool, as a ring on the device (see dyspec_page_pool in include/dyspec.h).
+
+    ring   int32 [n_pages]: page numbers, the free ones from state[0] on, round the end
+    state  int32 [4]: first free place of the ring, number of free pages, 0, 0"""
+    ring: "torch.Tensor"
+    state: "torch.Tensor"
+    page_size: int
+
+    def __post_init__(self):
+        ring, state = self.ring, self.state
+        i32 = _dtype("int32")
+        if ring.dim() != 1 or ring.numel() < 1 or ring.dtype is not i32 or not ring.is_cuda or not ring.is_contiguous():
+            raise ValueError("ring must be a contiguous int32 device tensor [n_pages]")
+        if state.shape != (4,) or state.dtype is not i32 or state.device != ring.device or not state.is_contiguous():
+            raise ValueError("state must be a contiguous int32 tensor [4] on the ring's device")
+        c = _PagePool(ring.data_ptr(), state.data_ptr(), int(ring.numel()), int(self.page_size))
+        for name, value in dict(_c=c, _ref=ctypes.byref(c), _device=ring.get_device()).items():
+            object.__setattr__(self, name, value)
+
+    @staticmethod
+    def full(n_pages: int, page_size: int, device) -> "PagePool":
+        """A pool of which every page is free."""
+        import torch
+        ring = torch.arange(n_pages, dtype=torch.int32, device=device)
+        return PagePool(ring, torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=ring.device), page_size)
+
+
+def page_plan(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None):
+    """dyspec_page_plan: every sequence gets pages for wanted[s] tokens in place of held[s], from the pool or back to it; returns
+    granted [n_seq], the tokens that it now has pages for (held[s] where the pool was short, -1 for lengths that cannot be).
+    page_table: int32 [n_seq or more, max_pages], a PagedCache's; held, wanted: int32 [n_seq]; slots: int64 [any], where the new
+    tokens' rows of the pool are noted, packed by sequences."""
+    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream)
+    _issue(_lib.dyspec_page_plan, args, pool._device, "dyspec_page_plan")
+    return granted
+
+
+def page_plan_call(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None) -> PreparedCall:
+    """page_plan's call, prepared: nothing is launched until the returned object is called."""
+    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream)
+    return DeviceCall(_lib.dyspec_page_plan, args, (pool, page_table, held, wanted, slots, granted), "dyspec_page_plan", granted, pool._device)
+
+
+def _plan_args(pool, page_table, held, wanted, slots, granted, stream):
+    if _lib is None:
+        load_library()
+    torch = _torch
+    device, n_seq, rows = pool._device, held.numel(), page_table.shape
+    if len(rows) != 2 or rows[0] < n_seq or page_table.dtype is not torch.int32 or page_table.get_device() != device or (rows[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table: int32 [n_seq or more, max_pages] on the pool's device expected")
+    hp, wp = _dense(held, (n_seq,), torch.int32, device, "held"), _dense(wanted, (n_seq,), torch.int32, device, "wanted")
+    sp = n_slots = 0
+    if slots is not None:
+        n_slots = slots.numel()
+        sp = _dense(slots, (n_slots,), torch.int64, device, "slots")
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    if granted is None:
+        with where:
+            granted = torch.empty_like(held)
+        gp = granted.data_ptr()
+    else:
+        gp = _dense(granted, (n_seq,), torch.int32, device, "granted")
+    if stream is not None:
+        _hand_over(stream, pool.ring, pool.state, page_table, held, wanted, slots, granted)
+    return (pool._ref, page_table.data_ptr(), rows[1], page_table.stride(0) if rows[0] > 1 else rows[1], hp, wp, n_seq, gp, sp, n_slots, raw), granted
 
 
 def probe_mfma_bf16(iterations: int, sink, stream=None, random_operands: bool = False) -> float:

@@ -4,6 +4,7 @@
 
 #include "attend.h"
 #include "kv_cache.h"
+#include "page_plan.h"
 
 namespace dyspec {
 
@@ -126,6 +127,7 @@ dyspec_status dyspec_init(void)
     void* scratch_address = nullptr;
     if (prepare_tree_attn() != hipSuccess || prepare_build_tree() != hipSuccess || prepare_build_threshold() != hipSuccess || prepare_verify() != hipSuccess ||
         prepare_reorder() != hipSuccess || prepare_attend() != hipSuccess || prepare_kv_cache() != hipSuccess ||
+        prepare_page_plan() != hipSuccess ||
         static_scratch_address(&scratch_address) != hipSuccess)
         return DYSPEC_HIP_ERROR;
     return DYSPEC_OK;
@@ -657,6 +659,34 @@ dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int
     const AttendForm f = { form[0], form[1], form[2] };
     return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
                               workspace_bytes, hip_stream);
+}
+
+// ---- pages by the requests' lengths
+
+// Whether n bytes at p and m bytes at q share any.
+static bool overlap(const void* p, size_t n, const void* q, size_t m)
+{
+    const size_t a = reinterpret_cast<size_t>(p), b = reinterpret_cast<size_t>(q);
+    return a < b + m && b < a + n;
+}
+
+dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table, int32_t max_pages, int32_t table_stride, const int32_t* held,
+                               const int32_t* wanted, int32_t n_seq, int32_t* granted, int64_t* slots, int64_t n_slots, void* hip_stream)
+{
+    if (!pool || !pool->ring || !pool->state || !page_table || !held || !wanted || !granted) return DYSPEC_BAD_ARG;
+    if (!aligned(pool->ring, 4) || !aligned(pool->state, 4) || !aligned(page_table, 4) || !aligned(held, 4) || !aligned(wanted, 4) || !aligned(granted, 4) ||
+        !aligned(slots, 8) || (n_slots > 0 && !slots))
+        return DYSPEC_BAD_ARG;
+    if (pool->page_size < 8 || pool->page_size > 65536 || (pool->page_size & (pool->page_size - 1))) return DYSPEC_UNSUPPORTED;
+    if (n_seq < 1 || n_seq > DYSPEC_MAX_SEQ || pool->n_pages < 1 || max_pages < 0 || table_stride < max_pages || n_slots < 0) return DYSPEC_BAD_SHAPE;
+    // (workgroups of other sequences read the lengths while these are written)
+    const size_t bytes = 4 * (size_t)n_seq;
+    if (overlap(granted, bytes, held, bytes) || overlap(granted, bytes, wanted, bytes)) return DYSPEC_BAD_ARG;
+    PlanArgs a;
+    a.ring = pool->ring; a.state = pool->state; a.table = page_table; a.granted = granted; a.held = held; a.wanted = wanted;
+    a.slots = reinterpret_cast<long long*>(slots); a.n_slots = n_slots;
+    a.n_pages = pool->n_pages; a.page_shift = log2_of(pool->page_size); a.max_pages = max_pages; a.table_stride = table_stride; a.n_seq = n_seq;
+    return launch_page_plan(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
 }  // extern "C"
