@@ -509,6 +509,40 @@ dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table
                                int64_t* slots, int64_t n_slots, void* hip_stream);
 
 /*
+ * dyspec_sample -- a token a row, drawn from what temperature, top-k, top-p and min-p leave of it, by given random
+ * numbers; dyspec_filter_logits -- the same filters, as logits: what they take out becomes -inf, the rest stays as it
+ * is.  Filtered draft and target tables are what dyspec_build_tree and dyspec_verify want, at the same temperatures.
+ *
+ * For a row x of vocab logits and its sequence's settings, w_i = exp((x_i - max x) / temperature) in 64 bits:
+ *   order     falling logit, equal ones by rising index
+ *   top-k     the first top_k tokens of the order                                      (0: all)
+ *   top-p     of these the ones before which less than top_p of their total weight lies (1: all; at least one)
+ *   min-p     of these the ones with w_i >= min_p                                      (0: all)
+ *   draw      the smallest index with which the sum of what is kept, by rising index, exceeds uniform * total
+ * temperature 0 keeps the largest logit alone, the smallest index winning a tie.  Sums are of weights rounded to 2^-45
+ * of the largest: tokens below half of that weigh nothing, and the result is the same bits in every call.
+ * Logits of -inf weigh nothing.  A row with a NaN or +inf, or without a finite logit, has no distribution: token -1,
+ * prob 0, n_kept 0, filtered: all -inf.
+ *
+ *   logits       DEVICE [rows, vocab], rows row_stride elements apart, DYSPEC_F32 or DYSPEC_BF16, aligned to an element
+ *                (rows that begin at 16 bytes are faster); vocab 1 .. DYSPEC_MAX_SAMPLE_VOCAB
+ *   batch        node_offset: sequence s has rows node_offset[s] .. node_offset[s+1]-1 (it may have none), up to 2^21
+ *                in all; nothing else of it is read
+ *   temperature  HOST [n_seq] finite, >= 0;  top_k HOST [n_seq] >= 0;  top_p HOST [n_seq] in (0, 1];  min_p HOST [n_seq]
+ *                in [0, 1]; the last three may be NULL: no such filter
+ *   uniform      DEVICE [rows] fp32 in [0, 1) (values outside, and NaN, count as the nearest inside, and as 0)
+ *   token, prob, n_kept  DEVICE [rows]: the token, its probability among what is kept, how many are kept
+ *   out          DEVICE [rows, vocab], rows out_stride apart; logits itself (with its stride), or no byte of its range
+ */
+#define DYSPEC_MAX_SAMPLE_VOCAB (1 << 18)
+dyspec_status dyspec_sample(const void* logits, int32_t dtype, int32_t vocab, int64_t row_stride, const dyspec_batch* batch,
+                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                            const float* uniform, int32_t* token, float* prob, int32_t* n_kept, void* hip_stream);
+dyspec_status dyspec_filter_logits(const void* logits, int32_t dtype, int32_t vocab, int64_t row_stride,
+                                   const dyspec_batch* batch, const float* temperature, const int32_t* top_k,
+                                   const float* top_p, const float* min_p, void* out, int64_t out_stride, void* hip_stream);
+
+/*
  * Measurement helpers (no part of the method): ceilings to set beside the published peaks
  * of the chip, and the clock the chip runs at under load.  All only launch; the caller times
  * them (HIP events on hip_stream).

@@ -25,7 +25,7 @@ EXPORTS = ("dyspec_init", "dyspec_mask_words", "dyspec_workspace_bytes", "dyspec
            "dyspec_dfs_reorder", "dyspec_tree_attn", "dyspec_tree_attn_static_scratch", "dyspec_tree_attn_layers",
            "dyspec_tree_attn_layers_workspace_bytes", "dyspec_verify", "dyspec_verify_bf16",
            "dyspec_kv_append", "dyspec_kv_keep", "dyspec_paged_attn", "dyspec_paged_attn_workspace_bytes", "dyspec_prompt_attn",
-           "dyspec_page_plan",
+           "dyspec_page_plan", "dyspec_sample", "dyspec_filter_logits",
            "dyspec_probe_mfma_bf16", "dyspec_probe_clock", "dyspec_probe_hbm_read")
 
 
@@ -120,6 +120,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dyspec_prompt_attn.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, V, V]
     lib.dyspec_page_plan.restype = I32
     lib.dyspec_page_plan.argtypes = [ctypes.POINTER(_PagePool), V, I32, I32, V, V, I32, V, V, I64, V]
+    lib.dyspec_sample.restype = I32
+    lib.dyspec_sample.argtypes = [V, I32, I32, I64, PB, V, V, V, V, V, V, V, V, V]
+    lib.dyspec_filter_logits.restype = I32
+    lib.dyspec_filter_logits.argtypes = [V, I32, I32, I64, PB, V, V, V, V, V, I64, V]
     lib.dyspec_probe_mfma_bf16.restype = I32
     lib.dyspec_probe_mfma_bf16.argtypes = [I32, I32, ctypes.POINTER(ctypes.c_double), V, V]
     lib.dyspec_probe_clock.restype = I32
@@ -990,6 +994,133 @@ def _plan_args(pool, page_table, held, wanted, slots, granted, stream):
     if stream is not None:
         _hand_over(stream, pool.ring, pool.state, page_table, held, wanted, slots, granted)
     return (pool._ref, page_table.data_ptr(), rows[1], page_table.stride(0) if rows[0] > 1 else rows[1], hp, wp, n_seq, gp, sp, n_slots, raw), granted
+
+
+# ---------------------------------------------------------------------------------------- filtered logits and drawn tokens
+
+@dataclass
+class Sampled:
+    token: "torch.Tensor"          # int32 [rows]; -1: the row has no distribution
+    prob: "torch.Tensor"           # fp32 [rows]: its probability among the tokens that are kept
+    n_kept: "torch.Tensor"         # int32 [rows]
+
+    @staticmethod
+    def empty(rows: int, device) -> "Sampled":
+        import torch
+        i = lambda: torch.empty(rows, dtype=torch.int32, device=device)
+        return Sampled(i(), torch.empty(rows, dtype=torch.float32, device=device), i())
+
+
+def sample(logits, batch: Batch, uniform, temperature, top_k=None, top_p=None, min_p=None, out: Optional[Sampled] = None, stream=None) -> Sampled:
+    """dyspec_sample: a token for every row of logits [rows, vocab] (a batch's n_nodes are its sequences' rows) by the given random
+    numbers uniform [rows] fp32 in [0, 1), after temperature, top-k, top-p and min-p: a number for all sequences, or one each; None:
+    no such filter."""
+    args, out, device, _ = _sample_args(logits, batch, uniform, temperature, top_k, top_p, min_p, out, stream)
+    if args is not None:
+        _issue(_lib.dyspec_sample, args, device, "dyspec_sample")
+    return out
+
+
+def sample_call(logits, batch: Batch, uniform, temperature, top_k=None, top_p=None, min_p=None, out: Optional[Sampled] = None, stream=None) -> PreparedCall:
+    """sample's call, prepared: nothing is launched until the returned object is called."""
+    args, out, device, held = _sample_args(logits, batch, uniform, temperature, top_k, top_p, min_p, out, stream)
+    if args is None:
+        return _Nothing(out)
+    return DeviceCall(_lib.dyspec_sample, args, (logits, uniform, batch._c(), held, out), "dyspec_sample", out, device)
+
+
+def filter_logits(logits, batch: Batch, temperature, top_k=None, top_p=None, min_p=None, out=None, stream=None):
+    """dyspec_filter_logits: logits [rows, vocab] with -inf in place of what top-k, top-p and min-p take out (settings as for
+    sample); build_tree and verify on such tables, at the same temperatures, draw from the filtered distributions.  out: may be
+    logits."""
+    args, out, device, _ = _filter_args(logits, batch, temperature, top_k, top_p, min_p, out, stream)
+    if args is not None:
+        _issue(_lib.dyspec_filter_logits, args, device, "dyspec_filter_logits")
+    return out
+
+
+def filter_logits_call(logits, batch: Batch, temperature, top_k=None, top_p=None, min_p=None, out=None, stream=None) -> PreparedCall:
+    """filter_logits' call, prepared: nothing is launched until the returned object is called."""
+    args, out, device, held = _filter_args(logits, batch, temperature, top_k, top_p, min_p, out, stream)
+    if args is None:
+        return _Nothing(out)
+    return DeviceCall(_lib.dyspec_filter_logits, args, (logits, batch._c(), held, out), "dyspec_filter_logits", out, device)
+
+
+def _per_sequence(x, kind, n_seq: int, what: str):
+    """A C array of one number a sequence, None for None."""
+    if x is None:
+        return None
+    if not isinstance(x, (list, tuple)):
+        x = [x] * n_seq if isinstance(x, (int, float)) else np.asarray(x).tolist()
+    if len(x) != n_seq:
+        raise ValueError(f"{what}: a number, or one for each of the {n_seq} sequences expected")
+    return (kind * n_seq)(*x)
+
+
+def _settings(batch, temperature, top_k, top_p, min_p):
+    n = batch.n_seq
+    return (_per_sequence(temperature, ctypes.c_float, n, "temperature"), _per_sequence(top_k, ctypes.c_int32, n, "top_k"),
+            _per_sequence(top_p, ctypes.c_float, n, "top_p"), _per_sequence(min_p, ctypes.c_float, n, "min_p"))
+
+
+def _logit_rows(t, total: int, what: str) -> int:
+    """Elements between the rows of t [total, vocab], each dense."""
+    if t.dim() != 2 or t.shape[0] != total or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a dense row for each of the batch's {total} expected, got {tuple(t.shape)}")
+    return t.stride(0) if total > 1 else t.shape[1]
+
+
+def _sample_args(logits, batch, uniform, temperature, top_k, top_p, min_p, out, stream):
+    if _lib is None:
+        load_library()
+    torch = _torch
+    total, ref = _chunks(batch)["chunks"]
+    device = logits.get_device()
+    if device < 0:
+        raise ValueError("device tensor required")
+    code, stride = _code(logits.dtype), _logit_rows(logits, total, "logits")
+    up = _dense(uniform, (total,), torch.float32, device, "uniform")
+    held = _settings(batch, temperature, top_k, top_p, min_p)
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    if out is None:
+        with where:
+            out = Sampled(uniform.new_empty(total, dtype=torch.int32), uniform.new_empty(total), uniform.new_empty(total, dtype=torch.int32))
+        tp, pp, np_ = out.token.data_ptr(), out.prob.data_ptr(), out.n_kept.data_ptr()
+    else:
+        tp, pp = _dense(out.token, (total,), torch.int32, device, "token"), _dense(out.prob, (total,), torch.float32, device, "prob")
+        np_ = _dense(out.n_kept, (total,), torch.int32, device, "n_kept")
+    if total == 0:
+        return None, out, device, held
+    if stream is not None:
+        _hand_over(stream, logits, uniform, out.token, out.prob, out.n_kept)
+    return (logits.data_ptr(), code, logits.shape[1], stride, ref, *held, up, tp, pp, np_, raw), out, device, held
+
+
+def _filter_args(logits, batch, temperature, top_k, top_p, min_p, out, stream):
+    if _lib is None:
+        load_library()
+    torch = _torch
+    total, ref = _chunks(batch)["chunks"]
+    device = logits.get_device()
+    if device < 0:
+        raise ValueError("device tensor required")
+    code, stride = _code(logits.dtype), _logit_rows(logits, total, "logits")
+    held = _settings(batch, temperature, top_k, top_p, min_p)
+    raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    if out is None:
+        with where:
+            out = logits.new_empty(logits.shape)
+        out_stride = logits.shape[1]
+    else:
+        if out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device:
+            raise ValueError("out: a table like logits expected")
+        out_stride = _logit_rows(out, total, "out")
+    if total == 0:
+        return None, out, device, held
+    if stream is not None:
+        _hand_over(stream, logits, out)
+    return (logits.data_ptr(), code, logits.shape[1], stride, ref, *held, out.data_ptr(), out_stride, raw), out, device, held
 
 
 def probe_mfma_bf16(iterations: int, sink, stream=None, random_operands: bool = False) -> float:

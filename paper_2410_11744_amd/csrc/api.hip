@@ -5,6 +5,7 @@
 #include "attend.h"
 #include "kv_cache.h"
 #include "page_plan.h"
+#include "sample.h"
 
 namespace dyspec {
 
@@ -127,7 +128,7 @@ dyspec_status dyspec_init(void)
     void* scratch_address = nullptr;
     if (prepare_tree_attn() != hipSuccess || prepare_build_tree() != hipSuccess || prepare_build_threshold() != hipSuccess || prepare_verify() != hipSuccess ||
         prepare_reorder() != hipSuccess || prepare_attend() != hipSuccess || prepare_kv_cache() != hipSuccess ||
-        prepare_page_plan() != hipSuccess ||
+        prepare_page_plan() != hipSuccess || prepare_sample() != hipSuccess ||
         static_scratch_address(&scratch_address) != hipSuccess)
         return DYSPEC_HIP_ERROR;
     return DYSPEC_OK;
@@ -687,6 +688,72 @@ dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table
     a.slots = reinterpret_cast<long long*>(slots); a.n_slots = n_slots;
     a.n_pages = pool->n_pages; a.page_shift = log2_of(pool->page_size); a.max_pages = max_pages; a.table_stride = table_stride; a.n_seq = n_seq;
     return launch_page_plan(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+}
+
+// ---- filtered logits and drawn tokens
+
+constexpr int kMostSampleRows = 1 << 21;         // (a workgroup of 1024 threads a row)
+
+// Where the sequences' rows begin and their settings; *rows: in all.
+static dyspec_status check_filters(const dyspec_batch* b, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int* row0,
+                                   Filter* filter, int* rows)
+{
+    if (!b || !b->node_offset || !temperature) return DYSPEC_BAD_ARG;
+    if (b->n_seq < 1 || b->n_seq > DYSPEC_MAX_SEQ || b->node_offset[0] != 0) return DYSPEC_BAD_SHAPE;
+    for (int s = 0; s < b->n_seq; ++s) {
+        if (b->node_offset[s + 1] < b->node_offset[s]) return DYSPEC_BAD_SHAPE;
+        row0[s] = b->node_offset[s];
+        filter[s] = Filter{ temperature[s], top_p ? top_p[s] : 1.0f, min_p ? min_p[s] : 0.0f, top_k ? top_k[s] : 0 };
+        const Filter& f = filter[s];
+        if (!(f.temperature >= 0.0f) || f.temperature > 3.402823466e38f || !(f.top_p > 0.0f) || f.top_p > 1.0f || !(f.min_p >= 0.0f) || f.min_p > 1.0f || f.top_k < 0)
+            return DYSPEC_BAD_ARG;
+    }
+    *rows = b->node_offset[b->n_seq];
+    return *rows <= kMostSampleRows ? DYSPEC_OK : DYSPEC_BAD_SHAPE;
+}
+
+static dyspec_status check_logits(const void* logits, int32_t dtype, int32_t vocab, int64_t stride)
+{
+    if (dtype != DYSPEC_F32 && dtype != DYSPEC_BF16) return DYSPEC_UNSUPPORTED;
+    if (!logits || !aligned(logits, dtype == DYSPEC_F32 ? 4 : 2)) return DYSPEC_BAD_ARG;
+    if (vocab < 1) return DYSPEC_BAD_SHAPE;
+    if (vocab > DYSPEC_MAX_SAMPLE_VOCAB) return DYSPEC_UNSUPPORTED;
+    return stride >= vocab && stride <= ((int64_t)1 << 40) ? DYSPEC_OK : DYSPEC_BAD_SHAPE;
+}
+
+dyspec_status dyspec_sample(const void* logits, int32_t dtype, int32_t vocab, int64_t row_stride, const dyspec_batch* batch, const float* temperature,
+                            const int32_t* top_k, const float* top_p, const float* min_p, const float* uniform, int32_t* token, float* prob,
+                            int32_t* n_kept, void* hip_stream)
+{
+    int row0[DYSPEC_MAX_SEQ];
+    Filter filter[DYSPEC_MAX_SEQ];
+    SampleHead a;
+    dyspec_status st = check_filters(batch, temperature, top_k, top_p, min_p, row0, filter, &a.rows);
+    if (st == DYSPEC_OK) st = check_logits(logits, dtype, vocab, row_stride);
+    if (st != DYSPEC_OK) return st;
+    if (!uniform || !token || !prob || !n_kept || !aligned(uniform, 4) || !aligned(token, 4) || !aligned(prob, 4) || !aligned(n_kept, 4)) return DYSPEC_BAD_ARG;
+    a.logits = logits; a.out = nullptr; a.uniform = uniform; a.token = token; a.prob = prob; a.n_kept = n_kept;
+    a.stride = row_stride; a.out_stride = 0; a.V = vocab; a.n_seq = batch->n_seq;
+    return launch_sample(a, row0, filter, dtype, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
+}
+
+dyspec_status dyspec_filter_logits(const void* logits, int32_t dtype, int32_t vocab, int64_t row_stride, const dyspec_batch* batch,
+                                   const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, void* out,
+                                   int64_t out_stride, void* hip_stream)
+{
+    int row0[DYSPEC_MAX_SEQ];
+    Filter filter[DYSPEC_MAX_SEQ];
+    SampleHead a;
+    dyspec_status st = check_filters(batch, temperature, top_k, top_p, min_p, row0, filter, &a.rows);
+    if (st == DYSPEC_OK) st = check_logits(logits, dtype, vocab, row_stride);
+    if (st == DYSPEC_OK) st = check_logits(out, dtype, vocab, out_stride);
+    if (st != DYSPEC_OK) return st;
+    // in place, or apart: workgroups of other rows read while these are written
+    const size_t elt = dtype == DYSPEC_F32 ? 4 : 2, last = a.rows ? (size_t)a.rows - 1 : 0;
+    if (out == logits ? out_stride != row_stride && a.rows > 1 : overlap(logits, (last * row_stride + vocab) * elt, out, (last * out_stride + vocab) * elt)) return DYSPEC_BAD_ARG;
+    a.logits = logits; a.out = out; a.uniform = nullptr; a.token = nullptr; a.prob = nullptr; a.n_kept = nullptr;
+    a.stride = row_stride; a.out_stride = out_stride; a.V = vocab; a.n_seq = batch->n_seq;
+    return launch_sample(a, row0, filter, dtype, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
 }  // extern "C"
