@@ -442,6 +442,29 @@ size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_
                                          int32_t head_dim, int32_t dtype);
 
 /*
+ * dyspec_paged_attn_scored -- dyspec_paged_attn where scores are capped, keys kept to a window, or both:
+ *   cap > 0     a score s = scale * <q, k> counts as cap * tanh(s / cap).  (bf16 with head_dim 64 or 128: on the bf16 matrix cores
+ *               up to a cap of 256, where it is within 2^-22 * cap; elsewhere, and beyond, in fp32 throughout)
+ *   window > 0  a row also sees no key whose position is `window` or more before its own.  Key k of the context has position
+ *               k, new token j prefix_len[s] + j, or prefix_len[s] + rel_pos[j] (a draft tree passes its depths, as to
+ *               dyspec_kv_append; 0 .. N - 1, others count as the nearest).  Keys that no row sees are not read.
+ * cap 0 and window 0 (or scores NULL): dyspec_paged_attn.  cap is at most 1e30, scale / cap within 1.2e-38 .. 1e37.
+ * workspace as for dyspec_paged_attn, dyspec_paged_attn_scored_workspace_bytes() bytes.
+ */
+typedef struct {
+    float cap;                       /* 0: none                                           */
+    int32_t window;                  /* 0: none                                           */
+    const int32_t* rel_pos;          /* DEVICE [sum N] or NULL; read only with a window   */
+} dyspec_scores;
+dyspec_status dyspec_paged_attn_scored(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
+                                       const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int32_t dtype, float softmax_scale,
+                                       const dyspec_scores* scores, void* out, void* workspace,
+                                       size_t workspace_bytes, void* hip_stream);
+size_t dyspec_paged_attn_scored_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                                int32_t head_dim, int32_t dtype, const dyspec_scores* scores);
+
+/*
  * dyspec_kv_keep -- keeps the accepted path of verified trees: in every layer, the rows of place
  * prefix_len[s] + accepted_nodes[i] move to place prefix_len[s] + 1 + i, i < n_accepted[s], so that the
  * root and the path lie end to end and the sequence goes on with prefix_len[s] + 1 + n_accepted[s] tokens.
@@ -475,6 +498,13 @@ dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k,
                                  const void* v, int64_t v_stride, const dyspec_batch* batch,
                                  int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                  float softmax_scale, void* out, void* hip_stream);
+
+/* dyspec_prompt_attn with capped scores, a window, or both, as for dyspec_paged_attn_scored (row j of a prompt has position j, or
+ * rel_pos[j]). */
+dyspec_status dyspec_prompt_attn_scored(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                        const void* v, int64_t v_stride, const dyspec_batch* batch,
+                                        int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                        float softmax_scale, const dyspec_scores* scores, void* out, void* hip_stream);
 
 /*
  * dyspec_page_plan -- page tables and slot maps by the requests' lengths, on the device: sequence s has pages for

@@ -25,6 +25,7 @@ EXPORTS = ("dyspec_init", "dyspec_mask_words", "dyspec_workspace_bytes", "dyspec
            "dyspec_dfs_reorder", "dyspec_tree_attn", "dyspec_tree_attn_static_scratch", "dyspec_tree_attn_layers",
            "dyspec_tree_attn_layers_workspace_bytes", "dyspec_verify", "dyspec_verify_bf16",
            "dyspec_kv_append", "dyspec_kv_keep", "dyspec_paged_attn", "dyspec_paged_attn_workspace_bytes", "dyspec_prompt_attn",
+           "dyspec_paged_attn_scored", "dyspec_paged_attn_scored_workspace_bytes", "dyspec_prompt_attn_scored",
            "dyspec_page_plan", "dyspec_sample", "dyspec_filter_logits",
            "dyspec_probe_mfma_bf16", "dyspec_probe_clock", "dyspec_probe_hbm_read")
 
@@ -50,6 +51,10 @@ class _Tree(ctypes.Structure):
 class _PagedKV(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("page_stride", ctypes.c_int64)]
+
+
+class _Scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32), ("rel_pos", ctypes.c_void_p)]
 
 
 class _PagePool(ctypes.Structure):
@@ -118,6 +123,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dyspec_paged_attn_workspace_bytes.argtypes = [PB, I32, I32, I32, I32]
     lib.dyspec_prompt_attn.restype = I32
     lib.dyspec_prompt_attn.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, V, V]
+    PS = ctypes.POINTER(_Scores)
+    lib.dyspec_paged_attn_scored.restype = I32
+    lib.dyspec_paged_attn_scored.argtypes = [V, PC, PB, V, I32, I32, I32, I32, F, PS, V, V, SZ, V]
+    lib.dyspec_paged_attn_scored_workspace_bytes.restype = SZ
+    lib.dyspec_paged_attn_scored_workspace_bytes.argtypes = [PB, I32, I32, I32, I32, PS]
+    lib.dyspec_prompt_attn_scored.restype = I32
+    lib.dyspec_prompt_attn_scored.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, PS, V, V]
     lib.dyspec_page_plan.restype = I32
     lib.dyspec_page_plan.argtypes = [ctypes.POINTER(_PagePool), V, I32, I32, V, V, I32, V, V, I64, V]
     lib.dyspec_sample.restype = I32
@@ -824,24 +836,42 @@ def kv_keep(cache: PagedCache, batch: Batch, accepted_nodes, n_accepted, stream=
     _issue(_lib.dyspec_kv_keep, (cache._ref, cache._layers or 1, cache._layer_stride, ref, ap, np_, Hkv, d, cache._code, raw), device, "dyspec_kv_keep")
 
 
-def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None):
-    """dyspec_paged_attn: the new tokens (appended before) attend to the pages: to their context and, causally or by an ancestor
-    mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d]."""
-    args, out, _ = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, False)
+def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None, cap: Optional[float] = None,
+               window: Optional[int] = None, rel_pos=None):
+    """dyspec_paged_attn, with cap or window dyspec_paged_attn_scored: the new tokens (appended before) attend to the pages: to their
+    context and, causally or by an ancestor mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d].
+    cap: scores s count as cap * tanh(s / cap); window: of keys less than that many positions back; rel_pos: int32 [sum N] positions of
+    the new tokens relative to each sequence's context (a tree's depths, as for kv_append), by default 0, 1, ..."""
+    where = "dyspec_paged_attn" if cap is None and window is None else "dyspec_paged_attn_scored"
+    args, out, _ = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, False, cap, window, rel_pos)
     if args is not None:
-        _issue(_lib.dyspec_paged_attn, args, cache._device, "dyspec_paged_attn")
+        _issue(getattr(_lib, where), args, cache._device, where)
     return out
 
 
-def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None) -> PreparedCall:
+def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mask=None, out=None, stream=None, cap: Optional[float] = None,
+                    window: Optional[int] = None, rel_pos=None) -> PreparedCall:
     """paged_attn's call, prepared: nothing is launched until the returned object is called.  It has a workspace of its own."""
-    args, out, ws = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, True)
+    where = "dyspec_paged_attn" if cap is None and window is None else "dyspec_paged_attn_scored"
+    args, out, ws = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, True, cap, window, rel_pos)
     if args is None:
         return _Nothing(out)
-    return DeviceCall(_lib.dyspec_paged_attn, args, (q, batch._c(), cache, anc_mask, out, ws), "dyspec_paged_attn", out, cache._device)
+    return DeviceCall(getattr(_lib, where), args, (q, batch._c(), cache, anc_mask, out, ws, rel_pos), where, out, cache._device)
 
 
-def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared):
+def _scores(cap, window, rel_pos, total: int, device: int):
+    """The C struct for capped scores and windows, None where there is neither."""
+    if cap is None and window is None:
+        return None
+    if cap is not None and not cap > 0:
+        raise ValueError("cap: a positive number, or None")
+    if window is not None and not window >= 1:
+        raise ValueError("window: at least 1, or None")
+    rp = 0 if rel_pos is None else _dense(rel_pos, (total,), _torch.int32, device, "rel_pos")
+    return _Scores(cap or 0.0, min(window or 0, (1 << 31) - 1), rp)
+
+
+def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared, cap=None, window=None, rel_pos=None):
     if _lib is None:
         load_library()
     torch = _torch
@@ -860,6 +890,7 @@ def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared):
             words = memo["chunk_words"] = max(1, -(-int(np.diff(batch.node_offset).max()) // 64))
         mp = _dense(anc_mask, (total, words), torch.int64, device, "anc_mask")
     raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
+    scores = _scores(cap, window, rel_pos, total, device)
     if out is None:
         with where:
             out = torch.empty_like(q)
@@ -868,37 +899,44 @@ def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared):
         op = _dense(out, shape, dtype, device, "out")
     if total == 0:
         return None, out, None
-    key = ("ws_paged", Hq, Hkv, d, code)
+    key = ("ws_paged", Hq, Hkv, d, code) if scores is None else ("ws_paged", Hq, Hkv, d, code, cap, window, rel_pos is None)
     nbytes = memo.get(key)
     if nbytes is None:
-        nbytes = memo[key] = int(_lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code))
+        nbytes = memo[key] = int(_lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code) if scores is None else
+                                 _lib.dyspec_paged_attn_scored_workspace_bytes(ref, Hq, Hkv, d, code, scores))
     ws, wp = None, 0
     if nbytes:
         ws = _attend_workspace(device, raw, where, nbytes, prepared)
         wp = ws.data_ptr()
     if stream is not None:
-        _hand_over(stream, q, out, anc_mask, cache.k, cache.v, cache.page_table)
-    return (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, op, wp, nbytes, raw), out, ws
+        _hand_over(stream, q, out, anc_mask, rel_pos, cache.k, cache.v, cache.page_table)
+    if scores is None:
+        return (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, op, wp, nbytes, raw), out, ws
+    return (qp, cache._ref, ref, mp, Hq, Hkv, d, code, softmax_scale, scores, op, wp, nbytes, raw), out, ws
 
 
-def prompt_attn(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None):
-    """dyspec_prompt_attn: packed prompts attend to themselves, causally.  q [sum N, Hq, d], k, v [sum N, Hkv, d], which may be
-    slices of one projection's rows; the batch's n_nodes are the prompts' lengths, its prefix_len zeros."""
-    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream)
+def prompt_attn(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None, cap: Optional[float] = None, window: Optional[int] = None, rel_pos=None):
+    """dyspec_prompt_attn, with cap or window dyspec_prompt_attn_scored: packed prompts attend to themselves, causally.  q [sum N, Hq, d],
+    k, v [sum N, Hkv, d], which may be slices of one projection's rows; the batch's n_nodes are the prompts' lengths, its prefix_len
+    zeros.  cap, window, rel_pos as for paged_attn."""
+    where = "dyspec_prompt_attn" if cap is None and window is None else "dyspec_prompt_attn_scored"
+    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap, window, rel_pos)
     if args is not None:
-        _issue(_lib.dyspec_prompt_attn, args, device, "dyspec_prompt_attn")
+        _issue(getattr(_lib, where), args, device, where)
     return out
 
 
-def prompt_attn_call(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None) -> PreparedCall:
+def prompt_attn_call(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=None, cap: Optional[float] = None, window: Optional[int] = None,
+                     rel_pos=None) -> PreparedCall:
     """prompt_attn's call, prepared: nothing is launched until the returned object is called."""
-    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream)
+    where = "dyspec_prompt_attn" if cap is None and window is None else "dyspec_prompt_attn_scored"
+    args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap, window, rel_pos)
     if args is None:
         return _Nothing(out)
-    return DeviceCall(_lib.dyspec_prompt_attn, args, (q, k, v, batch._c(), out), "dyspec_prompt_attn", out, device)
+    return DeviceCall(getattr(_lib, where), args, (q, k, v, batch._c(), out, rel_pos), where, out, device)
 
 
-def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
+def _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap=None, window=None, rel_pos=None):
     if _lib is None:
         load_library()
     total, ref = _chunks(batch)["chunks"]
@@ -918,11 +956,14 @@ def _prompt_args(q, k, v, batch, softmax_scale, out, stream):
         op = out.data_ptr()
     else:
         op = _dense(out, shape, dtype, device, "out")
+    scores = _scores(cap, window, rel_pos, total, device)
     if total == 0:
         return None, out, device
     if stream is not None:
-        _hand_over(stream, q, k, v, out)
-    return (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ref, Hq, Hkv, d, code, softmax_scale, op, raw), out, device
+        _hand_over(stream, q, k, v, out, rel_pos)
+    if scores is None:
+        return (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ref, Hq, Hkv, d, code, softmax_scale, op, raw), out, device
+    return (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, ref, Hq, Hkv, d, code, softmax_scale, scores, op, raw), out, device
 
 
 # ---------------------------------------------------------------------------------------- pages by the requests' lengths

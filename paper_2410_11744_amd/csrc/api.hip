@@ -481,14 +481,13 @@ static dyspec_status check_cache(const dyspec_paged_kv* c, const AttendBatch& b,
     return DYSPEC_OK;
 }
 
-static AttendArgs attend_args(int Hq, int Hkv, int d, float scale)
+static AttendArgs attend_args(int Hq, int Hkv, int d)
 {
     AttendArgs a;
     a.table = nullptr; a.mask = nullptr; a.part = nullptr; a.counters = nullptr;
     a.page_bytes = 0; a.table_stride = 0; a.page_shift = 0; a.n_pages = 0; a.mask_words = 0;
     a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.d = d;
     a.g_magic = a.G == 1 ? 0u : (uint32_t)((0xffffffffull + a.G) / a.G);
-    a.c2 = scale * 1.4426950408889634f;
     return a;
 }
 
@@ -499,6 +498,20 @@ static void sequences(Sequences<DYSPEC_MAX_SEQ>& seq, const AttendBatch& b)
 }
 
 static bool scale_ok(float x) { return x > 0.0f && x <= 2.3e38f; }      // (times log2 e it is finite still)
+
+// How scores are taken: *to, from what the caller says (NULL: as they are).
+static dyspec_status check_scores(const dyspec_scores* x, float scale, AttendScores* to)
+{
+    *to = AttendScores{ scale, 0.0f, kNoWindow, nullptr };
+    if (!x) return DYSPEC_OK;
+    if (!(x->cap >= 0.0f) || x->cap > 1e30f || x->window < 0 || !aligned(x->rel_pos, 4)) return DYSPEC_BAD_ARG;
+    // (a ratio that is finite, and not so small that it is none)
+    if (x->cap > 0.0f && (!(x->cap >= 1e-30f) || !(scale / x->cap <= 1e37f) || !(scale / x->cap >= 1.2e-38f))) return DYSPEC_BAD_ARG;
+    to->cap = x->cap;
+    to->window = x->window > 0 && x->window < kNoWindow ? x->window : kNoWindow;
+    to->rel = x->rel_pos;
+    return DYSPEC_OK;
+}
 
 dyspec_status dyspec_kv_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const dyspec_paged_kv* cache, const dyspec_batch* batch, const int32_t* rel_pos, const float* inv_freq,
@@ -562,11 +575,19 @@ dyspec_status dyspec_kv_keep(const dyspec_paged_kv* cache, int32_t n_layers, int
     return launch_kv_keep(a, seq, n_layers, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
 }
 
-size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype)
+size_t dyspec_paged_attn_scored_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                                const dyspec_scores* scores)
 {
     AttendBatch b;
+    AttendScores sc;
     if (check_chunks(batch, true, DYSPEC_MAX_CHUNK, &b) != DYSPEC_OK || n_q_heads < 1 || check_heads(n_q_heads, n_kv_heads, head_dim, dtype) != DYSPEC_OK) return 0;
-    return attend_workspace_bytes(b, dtype, n_q_heads, n_kv_heads, head_dim);
+    if (check_scores(scores, scores ? scores->cap > 0.0f ? scores->cap : 1.0f : 1.0f, &sc) != DYSPEC_OK) return 0;      // (the scale does not matter)
+    return attend_workspace_bytes(b, sc, dtype, n_q_heads, n_kv_heads, head_dim);
+}
+
+size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype)
+{
+    return dyspec_paged_attn_scored_workspace_bytes(batch, n_q_heads, n_kv_heads, head_dim, dtype, nullptr);
 }
 
 static dyspec_status launched(hipError_t e, const AttendForm* form)
@@ -576,18 +597,19 @@ static dyspec_status launched(hipError_t e, const AttendForm* form)
 
 static dyspec_status paged_attn_common(const AttendForm* form, const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
                                        const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
-                                       float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+                                       float softmax_scale, const dyspec_scores* scores, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     AttendBatch b;
+    AttendScores sc;
     dyspec_status st = check_chunks(batch, true, anc_mask ? DYSPEC_MAX_NODES : DYSPEC_MAX_CHUNK, &b);
     if (st == DYSPEC_OK) st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
     if (st == DYSPEC_OK && (n_q_heads < 1 || !rows_ok(b, n_q_heads, n_q_heads / n_kv_heads))) st = DYSPEC_BAD_SHAPE;
     if (st == DYSPEC_OK) st = check_cache(cache, b, n_kv_heads, head_dim, dtype);
     if (st != DYSPEC_OK) return st;
-    if (!q || !out || q == out || !scale_ok(softmax_scale)) return DYSPEC_BAD_ARG;
+    if (!q || !out || q == out || !scale_ok(softmax_scale) || check_scores(scores, softmax_scale, &sc) != DYSPEC_OK) return DYSPEC_BAD_ARG;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(anc_mask, 8) || !aligned(workspace, 16)) return DYSPEC_BAD_ARG;
     const long long elt = dtype == DYSPEC_F32 ? 4 : 2;
-    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim, softmax_scale);
+    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim);
     a.q = static_cast<const char*>(q); a.out = static_cast<char*>(out);
     a.k = static_cast<const char*>(cache->k); a.v = static_cast<const char*>(cache->v);
     a.table = cache->page_table; a.table_stride = cache->table_stride; a.page_shift = log2_of(cache->page_size); a.n_pages = cache->n_pages;
@@ -600,43 +622,62 @@ static dyspec_status paged_attn_common(const AttendForm* form, const void* q, co
         a.mask = reinterpret_cast<const uint32_t*>(anc_mask);
         a.mask_words = 2 * ((most + 63) / 64);
     }
-    return launched(launch_attend(a, b, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
+    return launched(launch_attend(a, b, sc, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
 }
 
 dyspec_status dyspec_paged_attn(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch, const uint64_t* anc_mask,
                                 int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, float softmax_scale,
                                 void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
 {
-    return paged_attn_common(nullptr, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
+    return paged_attn_common(nullptr, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, nullptr, out, workspace,
+                             workspace_bytes, hip_stream);
+}
+
+dyspec_status dyspec_paged_attn_scored(const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch, const uint64_t* anc_mask,
+                                       int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, float softmax_scale,
+                                       const dyspec_scores* scores, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    return paged_attn_common(nullptr, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, scores, out, workspace,
                              workspace_bytes, hip_stream);
 }
 
 static dyspec_status prompt_attn_common(const AttendForm* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                         int64_t v_stride, const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
-                                        int32_t dtype, float softmax_scale, void* out, void* workspace, size_t workspace_bytes, void* hip_stream)
+                                        int32_t dtype, float softmax_scale, const dyspec_scores* scores, void* out, void* workspace, size_t workspace_bytes,
+                                        void* hip_stream)
 {
     AttendBatch b;
+    AttendScores sc;
     dyspec_status st = check_chunks(batch, false, DYSPEC_MAX_CHUNK, &b);
     if (st == DYSPEC_OK) st = check_heads(n_q_heads, n_kv_heads, head_dim, dtype);
     if (st == DYSPEC_OK && (n_q_heads < 1 || !rows_ok(b, n_q_heads, n_q_heads / n_kv_heads))) st = DYSPEC_BAD_SHAPE;
     if (st != DYSPEC_OK) return st;
-    if (!q || !k || !v || !out || out == q || out == k || out == v || !scale_ok(softmax_scale)) return DYSPEC_BAD_ARG;
+    if (!q || !k || !v || !out || out == q || out == k || out == v || !scale_ok(softmax_scale) || check_scores(scores, softmax_scale, &sc) != DYSPEC_OK)
+        return DYSPEC_BAD_ARG;
     const long long elt = dtype == DYSPEC_F32 ? 4 : 2;
     const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim, most = (int64_t)1 << 22;
     if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride > most || k_stride > most || v_stride > most) return DYSPEC_BAD_SHAPE;
     const size_t four = 4 * elt;
     if (q_stride % 4 || k_stride % 4 || v_stride % 4 || !aligned(q, four) || !aligned(k, four) || !aligned(v, four) || !aligned(out, four)) return DYSPEC_BAD_ARG;
-    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim, softmax_scale);
+    AttendArgs a = attend_args(n_q_heads, n_kv_heads, head_dim);
     a.q = static_cast<const char*>(q); a.k = static_cast<const char*>(k); a.v = static_cast<const char*>(v); a.out = static_cast<char*>(out);
     a.q_stride = q_stride * elt; a.k_stride = k_stride * elt; a.v_stride = v_stride * elt; a.out_stride = q_row * elt;
-    return launched(launch_attend(a, b, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
+    return launched(launch_attend(a, b, sc, dtype, form, workspace, workspace ? workspace_bytes : 0, static_cast<hipStream_t>(hip_stream)), form);
 }
 
 dyspec_status dyspec_prompt_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                  const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                  float softmax_scale, void* out, void* hip_stream)
 {
-    return prompt_attn_common(nullptr, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out,
+    return prompt_attn_common(nullptr, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, nullptr, out,
+                              nullptr, 0, hip_stream);
+}
+
+dyspec_status dyspec_prompt_attn_scored(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                        const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                        float softmax_scale, const dyspec_scores* scores, void* out, void* hip_stream)
+{
+    return prompt_attn_common(nullptr, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, scores, out,
                               nullptr, 0, hip_stream);
 }
 
@@ -650,7 +691,18 @@ dyspec_status dyspec_paged_attn_in_form(const int32_t* form, const void* q, cons
 {
     if (!form) return DYSPEC_BAD_ARG;
     const AttendForm f = { form[0], form[1], form[2] };
-    return paged_attn_common(&f, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace, workspace_bytes, hip_stream);
+    return paged_attn_common(&f, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, nullptr, out, workspace, workspace_bytes,
+                             hip_stream);
+}
+dyspec_status dyspec_paged_attn_scored_in_form(const int32_t* form, const void* q, const dyspec_paged_kv* cache, const dyspec_batch* batch,
+                                               const uint64_t* anc_mask, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                               float softmax_scale, const dyspec_scores* scores, void* out, void* workspace, size_t workspace_bytes,
+                                               void* hip_stream)
+{
+    if (!form) return DYSPEC_BAD_ARG;
+    const AttendForm f = { form[0], form[1], form[2] };
+    return paged_attn_common(&f, q, cache, batch, anc_mask, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, scores, out, workspace, workspace_bytes,
+                             hip_stream);
 }
 dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                          int64_t v_stride, const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -658,8 +710,18 @@ dyspec_status dyspec_prompt_attn_in_form(const int32_t* form, const void* q, int
 {
     if (!form) return DYSPEC_BAD_ARG;
     const AttendForm f = { form[0], form[1], form[2] };
-    return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, out, workspace,
-                              workspace_bytes, hip_stream);
+    return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, nullptr, out,
+                              workspace, workspace_bytes, hip_stream);
+}
+dyspec_status dyspec_prompt_attn_scored_in_form(const int32_t* form, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                                int64_t v_stride, const dyspec_batch* batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                int32_t dtype, float softmax_scale, const dyspec_scores* scores, void* out, void* workspace,
+                                                size_t workspace_bytes, void* hip_stream)
+{
+    if (!form) return DYSPEC_BAD_ARG;
+    const AttendForm f = { form[0], form[1], form[2] };
+    return prompt_attn_common(&f, q, q_stride, k, k_stride, v, v_stride, batch, n_q_heads, n_kv_heads, head_dim, dtype, softmax_scale, scores, out,
+                              workspace, workspace_bytes, hip_stream);
 }
 
 // ---- pages by the requests' lengths

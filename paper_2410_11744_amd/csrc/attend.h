@@ -5,13 +5,19 @@
 // streams K and V of its KV head once.  Keys are numbered from the start of the sequence: the context's, then the new tokens'.
 //
 // Row j of the new tokens sees every key of the context and, of the new ones, key i if i <= j and, under an ancestor mask, bit i
-// of its mask row is set.
+// of its mask row is set; with a window, of all these the ones less than `window` positions before its own.  Key k of the context has
+// position k, new token i C + i or, with positions given, C + rel[i].
 #pragma once
 #include "dyspec_device.h"
 
 namespace dyspec {
 
 constexpr float kLowest = -3.402823466e38f;      // running maximum before the first key
+
+// What a kernel is built for: kPlainScores; kWindowed: keys of a window only; kCapped: a score s counts as cap * tanh(s / cap), and there
+// may be a window.
+enum Scores { kPlainScores, kWindowed, kCapped };
+constexpr int kNoWindow = DYSPEC_MAX_CONTEXT;    // no key is that far back
 
 // One sequence of a launch, or some row blocks of one.  Its row blocks (of the kernel's R rows) times `parts` are consecutive items;
 // a workgroup takes one item of one KV head.  Blocks come last row first: under a causal mask the long walks start first.
@@ -40,7 +46,10 @@ struct AttendArgs {
     int mask_words;                // 32-bit words per mask row
     int Hq, Hkv, G, d;
     uint32_t g_magic;              // r / G = hi(r * g_magic), G = 1: r
-    float c2;                      // softmax scale * log2(e): weights are exp2(c2 * score)
+    float c2;                      // softmax scale * log2(e): weights are exp2(c2 * score); of capped scores see capped_score
+    float cap, cap_in;             // capped scores: the cap, what <q, k> is multiplied by; else 0
+    int window;
+    const int* rel;                // positions of the new tokens, by the context's length less, or nullptr: 0, 1, ...
     int n_seq;                     // entries of the table
     AttendSeq seq[DYSPEC_MAX_SEQ];
 };
@@ -105,7 +114,42 @@ __device__ __forceinline__ uint32_t causal_bits(const AttendSeq& s, int j, int k
     const int upto = s.C + j + 1 - k0;
     return upto >= 32 ? ~0u : upto <= 0 ? 0u : (1u << upto) - 1u;
 }
+// ---- windows.  Without positions given a row's window ends at one key for all keys alike.  With positions (a tree's depths) it ends at
+// one key of the context, and new tokens are looked at one by one, which is only needed where the window is shorter than the tree.
+__device__ __forceinline__ int rel_of(const AttendArgs& a, const AttendSeq& s, int i) { return min(max(a.rel[s.row0 + i], 0), s.N - 1); }
+// First key (of the context, with positions given) that row j sees.  (Lengths and windows are at most 2^30.)
+template <int SC> __device__ __forceinline__ int window_begin(const AttendArgs& a, const AttendSeq& s, int j)
+{
+    if constexpr (SC == kPlainScores) return 0;
+    return a.rel ? min(s.C, s.C + rel_of(a, s, j) + 1 - a.window) : s.C + j + 1 - a.window;
+}
+// Where the walk of rows whose first token is j begins: no row sees a key before it.
+template <int SC> __device__ __forceinline__ int walk_begin(const AttendArgs& a, const AttendSeq& s, int j)
+{
+    if constexpr (SC == kPlainScores) return 0;
+    return max((a.rel ? s.C : s.C + j) + 1 - a.window, 0) & ~63;
+}
+// Keys before this one may be outside the window of a row whose last token is j.
+__device__ __forceinline__ int window_border(const AttendArgs& a, const AttendSeq& s, int j) { return a.rel ? min(s.C, s.C + s.N - a.window) : s.C + j + 1 - a.window; }
+// Bit b: key k0 + b is `begin` or behind it.
+__device__ __forceinline__ uint32_t bits_from(int begin, int k0)
+{
+    const int low = begin - k0;
+    return low <= 0 ? ~0u : low >= 32 ? 0u : ~0u << low;
+}
+// w without the new tokens that are out of row j's window, where positions are given.
+__device__ __forceinline__ uint32_t near_tokens(const AttendArgs& a, const AttendSeq& s, int j, int k0, uint32_t w)
+{
+    if (!a.rel || a.window >= s.N) return w;
+    const int mine = rel_of(a, s, j);
+    for (uint32_t left = w & bits_from(s.C, k0); left; left &= left - 1u) {
+        const int b = __builtin_ctz(left);
+        if (mine - rel_of(a, s, k0 + b - s.C) >= a.window) w &= ~(1u << b);
+    }
+    return w;
+}
 // Bit b: row j of the new tokens sees key k0 + b.
+template <int SC = kPlainScores>
 __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const AttendSeq& s, int j, int k0)
 {
     uint32_t w = causal_bits(s, j, k0);
@@ -113,7 +157,31 @@ __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const AttendS
         const int i0 = k0 - s.C;                           // key k0 + b is new token i0 + b
         w &= __builtin_amdgcn_alignbit(mask_word(a, s, j, (i0 >> 5) + 1), mask_word(a, s, j, i0 >> 5), (uint32_t)i0 & 31u);
     }
+    if constexpr (SC != kPlainScores) w = near_tokens(a, s, j, k0, w & bits_from(window_begin<SC>(a, s, j), k0));
     return w;
+}
+
+// ---- capped scores: y = scale <q, k> / cap, cap * tanh(y) = cap * (1 - 2 / (1 + exp(2 y)))
+//
+// Softmax only knows differences of scores, so the bf16 kernels work on -1 / (1 + exp(2 y)), in [-1, 0], with c2 = 2 cap log2(e) and
+// cap_in = 2 log2(e) scale / cap: one multiplication, one exponential, one sum, one reciprocal.  Its error (2^-25, half a step at the end
+// of the range, and about as much of the reciprocal) times 2 cap is 6e-6 at a cap of 50 and 3e-5 at kMostBf16Cap, far below a weight's
+// rounding to bf16 (2^-8 of it); scores small against larger caps would lose more, and go to the fp32 kernel.
+//
+// That one (Exact) keeps tanh(y) itself, c2 = cap log2(e), cap_in = scale / cap, right to a few 2^-24 of it however small: below 0.55 by an odd
+// polynomial (through Chebyshev's nodes, 4e-9), above as 1 - 2 / (1 + exp(2 y)), which is at least one half there.
+constexpr float kMostBf16Cap = 256.0f;
+template <bool Exact> __device__ __forceinline__ float capped_score(float s, float cap_in)
+{
+    if constexpr (!Exact) return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * cap_in));
+    const float y = s * cap_in, x = fabsf(y), z = y * y;
+    float p = -0.006610227831114734f;
+    p = fmaf(p, z, 0.021309388664443474f);
+    p = fmaf(p, z, -0.05390942882746055f);
+    p = fmaf(p, z, 0.1333311372902087f);
+    p = fmaf(p, z, -0.3333333200797698f);
+    const float big = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * 2.885390081777926815f)), 1.0f);
+    return x < 0.55f ? fmaf(y * z, p, y) : copysignf(big, y);
 }
 
 template <typename T> struct Four;
@@ -264,20 +332,26 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const AttendIte
 // matrix product.  Such keys may hold anything (a later token that overflowed), so rows that come out with a NaN are looked at
 // again: if what their block took at a weight of zero was all finite, the NaN is the row's own and stays.
 
-// Whether V of the walk's keys that meet a weight of zero is finite: of those that some row of the block may not see, and of the last
-// one, if it may be repeated to fill a block of (up to 64) keys.  One wave, lane i reads dims 4i..
-template <typename T>
-__device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int k_begin, int k_end)
+// Whether V of the walk's keys that meet a weight of zero is finite: of those that some row (r0 .. r1) of the block may not see, and of the
+// last one, if it may be repeated to fill a block of (up to 64) keys.  One wave, lane i reads dims 4i..
+template <typename T, int SC>
+__device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const AttendSeq& s, int kvh, int r0, int r1, int k_begin, int k_end)
 {
     typedef typename Four<T>::raw raw;
     const int size = (int)sizeof(T), lane = threadIdx.x & 63, piece = 4 * lane < a.d ? lane : 0;
     float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);            // stays zero unless something is infinite or a NaN
     auto add = [&](float4 x) { z.x = fmaf(x.x, 0.0f, z.x); z.y = fmaf(x.y, 0.0f, z.y); z.z = fmaf(x.z, 0.0f, z.z); z.w = fmaf(x.w, 0.0f, z.w); };
     const long long head = (long long)kvh * a.d * size + 4 * piece * size;
-    const int hidden = max(k_begin, a.mask ? s.C : s.C + div_G(a, r0) + 1), repeated = (k_end - k_begin) % 64 ? k_end - 1 : k_end;
+    const int hidden = max(k_begin, a.mask || (SC != kPlainScores && a.rel) ? s.C : s.C + div_G(a, r0) + 1), repeated = (k_end - k_begin) % 64 ? k_end - 1 : k_end;
 #pragma unroll 4
     for (int key = min(hidden, repeated); key < k_end; ++key)
         add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
+    if constexpr (SC != kPlainScores) {
+        const int border = min(window_border(a, s, div_G(a, r1)), k_end);
+#pragma unroll 4
+        for (int key = k_begin; key < border; ++key)
+            add(Four<T>::wide(*reinterpret_cast<const raw*>(a.v + key_offset(a, s, key, a.v_stride) + head)));
+    }
     return !__any((z.x + z.y) + (z.z + z.w) != 0.0f);          // (a NaN is not equal)
 }
 
@@ -290,7 +364,7 @@ __device__ __forceinline__ bool hidden_are_finite(const AttendArgs& a, const Att
 // infinities and NaN; a key that has some is added by itself, to the rows that see it.  So a hidden token that overflowed costs one
 // such walk of the rows beside it: a prompt of 8192 tokens, 64 heads on 8, with a NaN in one value takes up to 2.9 ms in place of 1.0,
 // a tree of 512 rows over 4096 tokens 2.0 in place of 0.09 (row by row and key by key it was 98, and 60).
-template <typename T, SlotOrder O, int DP, typename F>
+template <typename T, SlotOrder O, int DP, int SC, typename F>
 __device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int dim1, int rows_per_block, F m_of)
 {
     // all of the call is looked up anew: nothing is held for this through the walk
@@ -299,9 +373,10 @@ __device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int
     const AttendArgs& a = *(const AttendArgs*)args;
     const AttendItem it = attend_item(a, blockIdx.x);
     const int block_end = min((it.block + 1) * rows_per_block, a.G * it.s.N), end = it.s.C + div_G(a, block_end - 1) + 1;
-    const int n_parts = it.s.parts > 1 ? (end + it.s.share - 1) / it.s.share : 1;
-    const int k_begin = n_parts > 1 ? it.part * it.s.share : 0, k_end = n_parts > 1 ? min(end, k_begin + it.s.share) : end;
-    if (hidden_are_finite<T>(a, it.s, it.kvh, it.block * rows_per_block, k_begin, k_end)) return;
+    const int begin = walk_begin<SC>(a, it.s, div_G(a, it.block * rows_per_block));
+    const int n_parts = it.s.parts > 1 ? (end - begin + it.s.share - 1) / it.s.share : 1;
+    const int k_begin = begin + (n_parts > 1 ? it.part * it.s.share : 0), k_end = n_parts > 1 ? min(end, k_begin + it.s.share) : end;
+    if (hidden_are_finite<T, SC>(a, it.s, it.kvh, it.block * rows_per_block, block_end - 1, k_begin, k_end)) return;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // (the rows as they were have left before they leave again)
     float* const slot = part_slot(a, it, rows_per_block);
     typedef typename Four<T>::raw raw;
@@ -358,7 +433,7 @@ __device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int
                     v[x][y] = *reinterpret_cast<const raw*>(at + (dim < d ? dim : 0) * size);
                 }
             }
-            uint32_t seen = seen_bits(a, s, j, key0) & 0xffffu;
+            uint32_t seen = seen_bits<SC>(a, s, j, key0) & 0xffffu;
             if (k_end - key0 < 16) seen &= (1u << (k_end - key0)) - 1u;
             f4 S = { 0.0f, 0.0f, 0.0f, 0.0f };
 #pragma unroll
@@ -372,6 +447,9 @@ __device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int
                 S = __builtin_amdgcn_mfma_f32_16x16x4f32(w.w, u.w, S, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (SC == kCapped)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) S[x] = capped_score<O == kSlotF32>(S[x], a.cap_in);
             f4 p;
             uint32_t odd = 0u;                                     // bit x: V of the lane's key x has something infinite or a NaN
 #pragma unroll
@@ -440,15 +518,18 @@ __device__ __forceinline__ void look_again(uint32_t bad, int row0, int dim0, int
 
 // ---- launches
 struct AttendBatch { int n_seq; int row0[DYSPEC_MAX_SEQ + 1]; int context[DYSPEC_MAX_SEQ]; };
-size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d);
+// cap 0: none; window kNoWindow: none; rel: nullptr, or positions on the device
+struct AttendScores { float scale, cap; int window; const int* rel; };
+size_t attend_workspace_bytes(const AttendBatch& b, const AttendScores& scores, int dtype, int Hq, int Hkv, int d);
 // `a` without its sequences, which are dealt to the kernels and cut into items (attend.hip), or, with a form (tests), all given to
 // one kernel (0 .. 5: few rows, 8 and 4 waves; many rows, 8 and 4 waves; fp32, blocks of 16 and 64 rows), walks cut into shares of
 // that many keys (0: not) but for those of the first `whole` row blocks; hipErrorInvalidValue where there is no such form
 struct AttendForm { int kernel, share, whole; };
-hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream);
+hipError_t launch_attend(AttendArgs a, const AttendBatch& b, const AttendScores& scores, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream);
 hipError_t prepare_attend();
 
 // the kernels, on `items` items of a's sequences
+inline Scores scores_of(const AttendArgs& a) { return a.cap_in != 0.0f ? kCapped : a.window < kNoWindow ? kWindowed : kPlainScores; }
 constexpr int kManyRows = 128, kFewRows = 32;                      // rows of a block: attend_mfma.hip, attend_short.hip
 hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream);      // blocks of 16 * row_waves rows
 hipError_t launch_attend_mfma(const AttendArgs& a, int waves, int items, hipStream_t stream);

@@ -48,7 +48,14 @@ static const KindCost& cost_of(const AttendArgs& a, AttendKind k) { return kCost
 struct Set { AttendKind kind; int n, share, whole; int seq[DYSPEC_MAX_SEQ]; };
 
 static int new_of(const AttendBatch& b, int s) { return b.row0[s + 1] - b.row0[s]; }
-static int keys_of(const AttendBatch& b, int s) { return b.context[s] + new_of(b, s); }
+// Keys that the longest walk of a sequence's tokens before `to` has, in blocks of `rows` rows: with a window, those of a block's first row,
+// what its other rows (with positions given: any row) have behind that, and the 63 before that it may begin with.
+static int walk_of(const AttendArgs& a, const AttendBatch& b, int s, int to, int rows)
+{
+    if (a.window >= kNoWindow) return b.context[s] + to;
+    return (int)min((long long)b.context[s] + to, (long long)a.window + (a.rel ? to : (rows - 1) / a.G + 1) + 63);
+}
+static int keys_of(const AttendArgs& a, const AttendBatch& b, int s) { return walk_of(a, b, s, new_of(b, s), kManyRows); }
 static int blocks_of(const AttendArgs& a, const AttendBatch& b, int s, int rows) { return (int)(((long long)new_of(b, s) * a.G + rows - 1) / rows); }
 static int parts_of(int keys, int share) { return share >= keys ? 1 : (keys + share - 1) / share; }
 
@@ -65,7 +72,7 @@ template <typename F> static void each_piece(const AttendArgs& a, const AttendBa
         left -= uncut;
         const int border = cut ? min(N, (int)(((long long)cut * rows + a.G - 1) / a.G)) : 0;      // tokens of the blocks that are cut
         if (uncut) f(Piece{ s, blocks, uncut, 1, border, N });
-        if (cut) f(Piece{ s, cut, cut, parts_of(b.context[s] + border, set.share), 0, border });
+        if (cut) f(Piece{ s, cut, cut, parts_of(walk_of(a, b, s, border, rows), set.share), 0, border });
     }
 }
 
@@ -80,11 +87,11 @@ static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, 
     each_piece(a, b, set, [&](const Piece& p) {
         if (blocks_before == set.whole) { head = busy; before = 0; worst = 0.0f; }
         blocks_before += p.blocks;
-        const int keys = b.context[p.s] + p.to;
+        const int keys = walk_of(a, b, p.s, p.to, c.rows);
         const long long items = (long long)p.blocks * p.parts * a.Hkv;
         const float near = 1.0f + c.alone / (float)p.blocks, unit = 1.0f / (float)c.keys;
         const float whole = (float)keys / (float)p.parts * unit + 0.5f;
-        const float mean = (float)(b.context[p.s] + (p.from + p.to + 1) / 2) / (float)p.parts * unit + 0.5f;
+        const float mean = (float)walk_of(a, b, p.s, (p.from + p.to + 1) / 2, c.rows) / (float)p.parts * unit + 0.5f;
         const float item = c.once + c.step * near * whole, usual = c.once + c.step * near * mean, full = c.busy_once + c.busy_step * mean;
         before += items;
         busy += (double)items * full / kCus;
@@ -93,7 +100,7 @@ static float time_of(const AttendArgs& a, const AttendBatch& b, const Set& set, 
         const float cu = (float)(q - rest) * full + (rest ? fmaxf(usual, (float)rest * full) : 0.0f);
         longest = fmaxf(longest, item);
         worst = fmaxf(worst, fmaxf(item, cu));
-        if (p.to == new_of(b, p.s)) bytes += (float)keys * (float)a.Hkv * (float)(a.d * 2 * elt);
+        if (p.to == new_of(b, p.s)) bytes += (float)min((long long)b.context[p.s] + p.to, (long long)a.window + p.to) * (float)a.Hkv * (float)(a.d * 2 * elt);
         if (p.parts > 1) slot_bytes += (float)items * (float)(min((long long)c.rows, (long long)p.to * a.G) * a.d * 4);
     });
     const float shared = (float)busy, memory = bytes / kBytesPerUs;
@@ -132,7 +139,7 @@ static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, b
             if (set.share == kUnit) break;
         }
     };
-    tries(keys_of(b, set.seq[0]), 0);
+    tries(keys_of(a, b, set.seq[0]), 0);
     if (cost_of(a, set.kind).rows != kManyRows) { set = found; return best; }
     // long walks of single blocks beside sequences of many: those whole and first, these cut
     const int rows = cost_of(a, set.kind).rows;
@@ -149,7 +156,7 @@ static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, b
         if (!single && (n == 0 || n == before.n)) break;
         if (!single) longest_single = n;
     }
-    if (longest_single) tries(keys_of(b, set.seq[longest_single]), whole);
+    if (longest_single) tries(keys_of(a, b, set.seq[longest_single]), whole);
     // what is left after some rounds of a workgroup a CU cut
     set = before;
     const long long rounds = counters_of(a, b, set) / kCus;
@@ -158,7 +165,7 @@ static float cut(const AttendArgs& a, const AttendBatch& b, Set& set, int elt, b
         int x = 0;                                         // the sequence in which they end, its longest walk after them
         long long upto = blocks_of(a, b, set.seq[0], rows);
         while (x < set.n - 1 && upto <= whole) upto += blocks_of(a, b, set.seq[++x], rows);
-        if (upto > whole) tries(b.context[set.seq[x]] + (int)min((long long)new_of(b, set.seq[x]), ((upto - whole) * rows + a.G - 1) / a.G), whole);
+        if (upto > whole) tries(walk_of(a, b, set.seq[x], (int)min((long long)new_of(b, set.seq[x]), ((upto - whole) * rows + a.G - 1) / a.G), rows), whole);
     }
     set = found;
     return best;
@@ -169,7 +176,7 @@ struct Plan { int n; Set set[2]; };
 static bool on_bf16_cores(const AttendArgs& a, int dtype)
 {
     auto pieces = [](const void* p, long long stride) { return reinterpret_cast<size_t>(p) % 16 == 0 && stride % 16 == 0; };
-    return dtype == DYSPEC_BF16 && (a.d == 64 || a.d == 128) && pieces(a.q, a.q_stride) && pieces(a.k, a.k_stride) && pieces(a.v, a.v_stride) &&
+    return dtype == DYSPEC_BF16 && a.cap <= kMostBf16Cap && (a.d == 64 || a.d == 128) && pieces(a.q, a.q_stride) && pieces(a.k, a.k_stride) && pieces(a.v, a.v_stride) &&
            pieces(a.out, a.out_stride);
 }
 
@@ -196,7 +203,7 @@ static void plan_of(const AttendArgs& a, const AttendBatch& b, int dtype, bool p
     for (int s = 0; s < b.n_seq; ++s) {
         if (new_of(b, s) == 0) continue;
         int at = n++;
-        for (; at > 0 && keys_of(b, order[at - 1]) < keys_of(b, s); --at) order[at] = order[at - 1];
+        for (; at > 0 && keys_of(a, b, order[at - 1]) < keys_of(a, b, s); --at) order[at] = order[at - 1];
         order[at] = s;
     }
     const bool bf16 = on_bf16_cores(a, dtype);
@@ -248,7 +255,7 @@ static int fill(AttendArgs& a, const AttendBatch& b, const Set& set, int* groups
     int items = 0, n = 0;
     *groups = 0; *slots = 0; *most_new = 0;
     each_piece(a, b, set, [&](const Piece& p) {
-        const int s = p.s, keys = b.context[s] + p.to;
+        const int s = p.s, keys = walk_of(a, b, s, p.to, cost_of(a, set.kind).rows);
         AttendSeq& q = a.seq[n];
         q.id = s; q.row0 = b.row0[s]; q.N = new_of(b, s); q.C = b.context[s];
         q.item0 = items; q.end_block = p.end; q.slot0 = (int)*slots;
@@ -265,9 +272,24 @@ static int fill(AttendArgs& a, const AttendBatch& b, const Set& set, int* groups
     return items;
 }
 
-size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, int d)
+static void set_scores(AttendArgs& a, const AttendScores& x)
+{
+    a.window = x.window; a.rel = x.window < kNoWindow ? x.rel : nullptr;
+    a.cap = x.cap;
+    a.cap_in = 0.0f; a.c2 = x.scale * 1.4426950408889634f;
+}
+// What a kernel multiplies scores by (capped_score).
+static void set_cap(AttendArgs& a, const AttendScores& x, bool exact)
+{
+    if (x.cap == 0.0f) return;
+    a.c2 = (exact ? 1.0f : 2.0f) * x.cap * 1.4426950408889634f;
+    a.cap_in = exact ? x.scale / x.cap : 2.0f * 1.4426950408889634f * (x.scale / x.cap);
+}
+
+size_t attend_workspace_bytes(const AttendBatch& b, const AttendScores& scores, int dtype, int Hq, int Hkv, int d)
 {
     AttendArgs a;
+    set_scores(a, scores);
     a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.d = d;
     a.q = a.k = a.v = a.out = nullptr;
     a.q_stride = a.out_stride = a.k_stride = a.v_stride = 16;
@@ -283,8 +305,9 @@ size_t attend_workspace_bytes(const AttendBatch& b, int dtype, int Hq, int Hkv, 
     return bytes ? DYSPEC_PAGED_COUNTER_BYTES + bytes : 0;
 }
 
-hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream)
+hipError_t launch_attend(AttendArgs a, const AttendBatch& b, const AttendScores& scores, int dtype, const AttendForm* form, void* workspace, size_t workspace_bytes, hipStream_t stream)
 {
+    set_scores(a, scores);
     Plan plan;
     for (int parts = workspace != nullptr; parts >= 0; --parts) {
         if (form && !plan_given(a, b, dtype, *form, plan)) return hipErrorInvalidValue;
@@ -313,6 +336,7 @@ hipError_t launch_attend(AttendArgs a, const AttendBatch& b, int dtype, const At
             slots_at += (size_t)slots * slot_bytes(a, set.kind);
             counters += groups * a.Hkv;
         }
+        set_cap(a, scores, set.kind >= kF32Few);
         hipError_t e = hipSuccess;
         switch (set.kind) {
             case kMany8: e = launch_attend_mfma(a, 8, items, stream); break;

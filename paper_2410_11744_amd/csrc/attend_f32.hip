@@ -19,7 +19,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kF32Waves = 4;
 
-template <typename T, int DP, bool Paged>
+template <typename T, int DP, bool Paged, int SC>
 __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 || (DP == 192 && sizeof(T) == 2) ? 2 : 1) void attend_f32_kernel(AttendArgs, int row_waves)
 {
     const AttendArgs& a = attend_args_here();
@@ -41,11 +41,18 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 || (DP == 192 && sizeof(T
     const int r = r0 + 16 * wq + n, rc = min(r, rows - 1);
     const int j = div_G(a, rc), h = it.kvh * a.G + (rc - j * a.G);
     const int end = s.C + div_G(a, min(r0 + R, rows) - 1) + 1;     // keys that some row of the block may see
-    const int n_parts = s.parts > 1 ? (end + s.share - 1) / s.share : 1;
+    const int begin = walk_begin<SC>(a, s, div_G(a, r0));
+    const int n_parts = s.parts > 1 ? (end - begin + s.share - 1) / s.share : 1;
     if (it.part >= n_parts) return;
-    const int k_begin = s.parts > 1 ? it.part * s.share : 0, k_end = s.parts > 1 ? min(end, k_begin + s.share) : end;
+    const int k_begin = begin + (s.parts > 1 ? it.part * s.share : 0), k_end = s.parts > 1 ? min(end, k_begin + s.share) : end;
     const int last = k_end - 1;
-    const int full = a.mask ? s.C : s.C + div_G(a, min(r0 + 16 * wq, rows - 1)) + 1;       // keys before this one are every row's of the wave
+    const int full = a.mask || (SC != kPlainScores && a.rel) ? s.C : s.C + div_G(a, min(r0 + 16 * wq, rows - 1)) + 1;       // keys before this one are every row's of the wave
+    int border = 0;                                                // keys before this one may be behind some row's window
+    if constexpr (SC != kPlainScores) {
+        border = window_begin<SC>(a, s, j);
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) border = max(border, __shfl_xor(border, o, kWave));
+    }
     const int size = (int)sizeof(T);
     const long long k_stride = a.k_stride, v_stride = a.v_stride, page_bytes = a.page_bytes;
     const char* const kp = a.k + (long long)it.kvh * d * size;
@@ -141,9 +148,14 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 || (DP == 192 && sizeof(T
                 if (((i + 1) & (kAhead - 1)) == 0) pages = fetch_pages(i + 1);
             load_k(kr, pages, i + 1, key0 + key_step);
         }
+        if constexpr (SC == kCapped)
+#pragma unroll
+            for (int b = 0; b < N16; ++b)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) S[b][x] = capped_score<true>(S[b][x], a.cap_in);
         // scores of keys a row does not see: -inf, whatever K holds there
-        if (key0 + KB > full || key0 + KB > k_end) {
-            uint32_t seen = seen_bits(a, s, j, key0);
+        if (key0 + KB > full || key0 + KB > k_end || (SC != kPlainScores && key0 < border)) {
+            uint32_t seen = seen_bits<SC>(a, s, j, key0);
             if (k_end - key0 < KB) seen &= (1u << (k_end - key0)) - 1u;
 #pragma unroll
             for (int b = 0; b < N16; ++b)
@@ -253,27 +265,36 @@ __global__ __launch_bounds__(64 * kF32Waves, DP <= 128 || (DP == 192 && sizeof(T
                 }
         }
         if (__builtin_expect(bad != 0u, 0))
-            look_again<T, kSlotF32, DP>(bad, 16 * wq, 0, a.d, R, [=](int row) { return __shfl(m, row & 15, kWave); });
+            look_again<T, kSlotF32, DP, SC>(bad, 16 * wq, 0, a.d, R, [=](int row) { return __shfl(m, row & 15, kWave); });
     }
     if (n_parts > 1 && arrive_last(a, it, n_parts, &flag)) merge_parts<T, kSlotF32, 0>(a, it, n_parts, R, 64 * kF32Waves);
 }
 
-template <typename T, bool Paged>
+template <typename T, bool Paged, int SC>
 static void launch_f32(const AttendArgs& a, int row_waves, int blocks, hipStream_t stream)
 {
-    if (a.d <= 64) attend_f32_kernel<T, 64, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else if (a.d <= 128) attend_f32_kernel<T, 128, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else if (a.d <= 192) attend_f32_kernel<T, 192, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
-    else attend_f32_kernel<T, 256, Paged><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    if (a.d <= 64) attend_f32_kernel<T, 64, Paged, SC><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 128) attend_f32_kernel<T, 128, Paged, SC><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else if (a.d <= 192) attend_f32_kernel<T, 192, Paged, SC><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+    else attend_f32_kernel<T, 256, Paged, SC><<<blocks, 64 * kF32Waves, 0, stream>>>(a, row_waves);
+}
+template <int SC>
+static void launch_f32(const AttendArgs& a, int dtype, int row_waves, int blocks, hipStream_t stream)
+{
+    if (dtype == DYSPEC_F32) {
+        if (a.table) launch_f32<float, true, SC>(a, row_waves, blocks, stream); else launch_f32<float, false, SC>(a, row_waves, blocks, stream);
+    } else {
+        if (a.table) launch_f32<__bf16, true, SC>(a, row_waves, blocks, stream); else launch_f32<__bf16, false, SC>(a, row_waves, blocks, stream);
+    }
 }
 
 hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int items, hipStream_t stream)
 {
     const int blocks = items * a.Hkv;
-    if (dtype == DYSPEC_F32) {
-        if (a.table) launch_f32<float, true>(a, row_waves, blocks, stream); else launch_f32<float, false>(a, row_waves, blocks, stream);
-    } else {
-        if (a.table) launch_f32<__bf16, true>(a, row_waves, blocks, stream); else launch_f32<__bf16, false>(a, row_waves, blocks, stream);
+    switch (scores_of(a)) {
+        case kPlainScores: launch_f32<kPlainScores>(a, dtype, row_waves, blocks, stream); break;
+        case kWindowed: launch_f32<kWindowed>(a, dtype, row_waves, blocks, stream); break;
+        case kCapped: launch_f32<kCapped>(a, dtype, row_waves, blocks, stream); break;
     }
     return hipGetLastError();
 }
@@ -281,7 +302,7 @@ hipError_t launch_attend_f32(const AttendArgs& a, int dtype, int row_waves, int 
 hipError_t prepare_attend_f32()                                    // (asking loads the code)
 {
     hipFuncAttributes at;
-    return hipFuncGetAttributes(&at, reinterpret_cast<const void*>(&attend_f32_kernel<float, 64, true>));
+    return hipFuncGetAttributes(&at, reinterpret_cast<const void*>(&attend_f32_kernel<float, 64, true, kPlainScores>));
 }
 
 }  // namespace dyspec

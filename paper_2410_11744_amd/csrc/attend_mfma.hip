@@ -47,7 +47,7 @@ template <int D, int NW> struct ManyGeo {
     static constexpr int kLoads = 32 / kRowsPerLoad;             // direct loads of a wave per step
 };
 
-template <int D, bool Paged, int NW>
+template <int D, bool Paged, int NW, int SC>
 __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 {
     const AttendArgs& a = attend_args_here();
@@ -66,9 +66,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     const int rows = a.G * s.N, r0 = it.block * kRows;
     const int j_first = div_G(a, r0);
     const int end = s.C + div_G(a, min(r0 + kRows, rows) - 1) + 1;           // keys that some row of the block may see
-    const int n_parts = s.parts > 1 ? (end + s.share - 1) / s.share : 1;
+    const int begin = walk_begin<SC>(a, s, j_first);
+    const int n_parts = s.parts > 1 ? (end - begin + s.share - 1) / s.share : 1;
     if (it.part >= n_parts) return;
-    const int k_begin = s.parts > 1 ? it.part * s.share : 0;
+    const int k_begin = begin + (s.parts > 1 ? it.part * s.share : 0);
     const int k_end = s.parts > 1 ? min(end, k_begin + s.share) : end;
     const int last = k_end - 1;
     const int nT = (k_end - k_begin + kTile - 1) / kTile;                    // tiles; one from there on stands for "no tile"
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 #pragma unroll
             for (int w = 0; w < 4; ++w) pw[e][ts][w] = 0u;
     float m_run = -INFINITY, l_run = 0.0f, ls_half = 0.0f;         // (so that the first half a wave sees is done again, whatever the scale)
-    const float c2 = a.c2;
+    const float c2 = a.c2, cap_in = a.cap_in;
     __syncthreads();                             // (the later loads queue up behind the urgent ones)
     if (ld_is_v) issue_first_k();
     issue_first_v();
@@ -223,6 +224,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         }
     }
 
+    // ---- windows: first key of the lane's row's; steps before `lead` have keys that are behind some row's of this wave
+    int window0 = 0, lead = 0;
+    if constexpr (SC != kPlainScores) {
+        int border = window0 = window_begin<SC>(a, s, row_j);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) border = max(border, __shfl_xor(border, o, kWave));
+        lead = (max(__builtin_amdgcn_readfirstlane(border) - k_begin, 0) + kTile * TP - 1) / (kTile * TP);
+    }
     // ---- which of a tile's 64 keys the lane's row sees.  The mask's words are fetched a step ahead and put together when they are due.
     struct Words { uint32_t w[3]; };
     auto fetch_words = [=](int t) __attribute__((always_inline)) -> Words {
@@ -242,6 +251,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         const uint32_t r = (uint32_t)(k0 - s.C) & 31u;
         const uint32_t lo = causal_bits(s, row_j, k0) & __builtin_amdgcn_alignbit(x.w[1], x.w[0], r);
         const uint32_t hi = causal_bits(s, row_j, k0 + 32) & __builtin_amdgcn_alignbit(x.w[2], x.w[1], r);
+        if constexpr (SC != kPlainScores)
+            return ((uint64_t)near_tokens(a, s, row_j, k0 + 32, hi & bits_from(window0, k0 + 32)) << 32) | near_tokens(a, s, row_j, k0, lo & bits_from(window0, k0));
         return ((uint64_t)hi << 32) | lo;
     };
 
@@ -268,6 +279,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         // X the exponentials, M the mask, C the rounding, D the sum.  A dependent instruction waits for its operand, so the stages
         // of a pair sit in different items: item h holds X(k) and D(k-1) when even, M(k), F(k+1) and C(k) when odd.
         float ft[8][2], pt[8][2];
+        // capped scores: T the exponential, U the reciprocal, in place
+        auto stage_t = [&](auto kc) __attribute__((always_inline)) {
+            constexpr int k = decltype(kc)::value;
+            S[E][2 * k] = fast_exp2(S[E][2 * k] * cap_in);
+            S[E][2 * k + 1] = fast_exp2(S[E][2 * k + 1] * cap_in);
+        };
+        auto stage_u = [&](auto kc) __attribute__((always_inline)) {
+            constexpr int k = decltype(kc)::value;
+            S[E][2 * k] = __builtin_amdgcn_rcpf(-1.0f - S[E][2 * k]);
+            S[E][2 * k + 1] = __builtin_amdgcn_rcpf(-1.0f - S[E][2 * k + 1]);
+        };
         auto stage_f = [&](auto kc) __attribute__((always_inline)) {
             constexpr int k = decltype(kc)::value;
             ft[k][0] = fmaf(S[E][2 * k], c2, -mc);
@@ -284,6 +306,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
                 pt[k][0] = fast_exp2(ft[k][0]);
                 pt[k][1] = fast_exp2(ft[k][1]);
                 if constexpr (k > 0) stage_d(std::integral_constant<int, k - 1>{});
+                if constexpr (SC == kCapped && k + 2 < 8) stage_t(std::integral_constant<int, k + 2>{});
             } else {
                 float p0 = pt[k][0], p1 = pt[k][1];
                 if constexpr (MK) {
@@ -291,6 +314,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
                     p1 = and_bits(p1, __builtin_amdgcn_sbfe((int)seen, 8 * (i / 4) + (i % 4) + 1, 1));
                 }
                 if constexpr (k + 1 < 8) stage_f(std::integral_constant<int, k + 1>{});
+                if constexpr (SC == kCapped && k + 2 < 8) stage_u(std::integral_constant<int, k + 2>{});
                 floatx2 pp = { p0, p1 };
                 uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector(pp, bf16x2));
                 asm volatile("" : "+v"(w));                        // the conversion stays in this scheduling group
@@ -298,6 +322,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
                 pw[E][k / 4][k % 4] = w;
             }
         };
+        if constexpr (HS && SC == kCapped) {
+            static_for<2>([&](auto kc) { stage_t(kc); });
+            static_for<2>([&](auto kc) { stage_u(kc); });
+        }
         if constexpr (HS) stage_f(std::integral_constant<int, 0>{});
         // with both products, even slots belong to the first and odd slots to the second
         bf16x8 fr[NS];
@@ -409,7 +437,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     };
     // ---- plain steps: the step's tiles are seen whole by every row, what it loads (tiles up to TP (i + 3) - 1) is whole or does not
     //      exist
-    const int full = max(min(a.mask ? s.C : s.C + j_first + 1, k_end) - k_begin, 0) / kTile;
+    const bool by_row = a.mask || (SC != kPlainScores && a.rel);
+    const int full = max(min(by_row ? s.C : s.C + j_first + 1, k_end) - k_begin, 0) / kTile;
     const int nPlain = min(full / TP, nWhole < nT ? max(nWhole - 2 * TP, 0) / TP : full);
     auto plain_step = [&](auto sp_c, int ii) __attribute__((always_inline)) {
         if constexpr (decltype(sp_c)::value == 0) turn_pages(ii);
@@ -418,21 +447,25 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         run_half(no, no, yes, sp_c, odd, 0u, ii, st_dst + slot_of(ii));
     };
     int i = 0;
-    for (; i + 1 < nPlain; i += 2) {
-        plain_step(even, i);
-        plain_step(odd, i + 1);
-    }
-    if (i < nPlain) plain_step(even, i++);
+    auto plain_steps = [&]() __attribute__((always_inline)) {
+        for (; i + 1 < nPlain; i += 2) {
+            plain_step(even, i);
+            plain_step(odd, i + 1);
+        }
+        if (i < nPlain) plain_step(even, i++);
+    };
+    if constexpr (SC == kPlainScores) plain_steps();
     // ---- masked steps.  A half step is run only if the wave's rows see a key of the half or of a neighbour, whose product it
     //      carries; otherwise its weights are cleared.
     const int nIt = (nT + TP - 1) / TP;
     uint64_t visC, visN;
-    {
-        const int tc = TP * i + wk, tn = TP * (i + 1) + wk;
+    auto look_ahead = [&](int ii) __attribute__((always_inline)) {
+        const int tc = TP * ii + wk, tn = TP * (ii + 1) + wk;
         const Words xc = fetch_words(tc), xn = fetch_words(tn);
         visC = seen_in(tc, xc);
         visN = seen_in(tn, xn);
-    }
+    };
+    if constexpr (SC == kPlainScores) look_ahead(i);
     auto masked_half = [&](auto sp_c, auto e_c, bool act, uint32_t seen) __attribute__((always_inline)) {
         if (act) {
             run_half(yes, no, no, sp_c, e_c, seen, 0, 0u);
@@ -461,10 +494,27 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
         visC = visN;
         visN = seen_in(t2, x2);
     };
-    if ((i & 1) && i < nIt) masked_step(odd, i++);
-    for (; i < nIt; i += 2) {
-        masked_step(even, i);
-        if (i + 1 < nIt) masked_step(odd, i + 1);
+    auto masked_steps = [&](int upto) __attribute__((always_inline)) {
+        if ((i & 1) && i < upto) masked_step(odd, i++);
+        for (; i < upto; i += 2) {
+            masked_step(even, i);
+            if (i + 1 < upto) masked_step(odd, i + 1);
+        }
+    };
+    if constexpr (SC == kPlainScores) {
+        masked_steps(nIt);
+    } else {
+        // where windows begin masked steps come first (each wave goes by its own rows: both kinds have the same loads and barriers)
+        const int first = (lead + 1) & ~1, then = first < nPlain ? first : nIt;
+#pragma unroll 1
+        for (int turn = first > 0 ? 0 : 1; turn < 2; ++turn) {
+            if (turn == 1 && i < nPlain) {
+                plain_steps();
+                aP1 = true;
+            }
+            look_ahead(i);
+            masked_steps(turn == 0 ? then : nIt);
+        }
     }
     // ---- the second product of the last upper half
     if (aP1) {
@@ -575,36 +625,45 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
             }
         }
         if (__builtin_expect(bad != 0u, 0))
-            look_again<__bf16, kSlotMany, D>(bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, [=](int row) { return __shfl(m, row & 31, kWave); });
+            look_again<__bf16, kSlotMany, D, SC>(bad, 32 * wq, 32 * mine, 32 * (mine + HB), kRows, [=](int row) { return __shfl(m, row & 31, kWave); });
     });
     if (n_parts > 1 && arrive_last(a, it, n_parts, reinterpret_cast<int*>(lds))) merge_parts<__bf16, kSlotMany, D>(a, it, n_parts, kRows, 64 * NW);
 }
 
-template <int D, bool Paged, int NW>
+template <int D, bool Paged, int NW, int SC>
 static hipError_t launch_many(const AttendArgs* a, int blocks, hipStream_t stream)
 {
     static std::atomic<unsigned long long> done{0};
     constexpr int lds = ManyGeo<D, NW>::kLdsBytes;
-    const hipError_t e = raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_mfma_kernel<D, Paged, NW>), lds, done);
+    const hipError_t e = raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_mfma_kernel<D, Paged, NW, SC>), lds, done);
     if (e != hipSuccess || !a) return e;
-    attend_mfma_kernel<D, Paged, NW><<<blocks, 64 * NW, lds, stream>>>(*a);
+    attend_mfma_kernel<D, Paged, NW, SC><<<blocks, 64 * NW, lds, stream>>>(*a);
     return hipGetLastError();
 }
-template <int D, bool Paged>
+template <int D, bool Paged, int SC>
 static hipError_t launch_many(const AttendArgs* a, int waves, int blocks, hipStream_t stream)
 {
-    return waves == 8 ? launch_many<D, Paged, 8>(a, blocks, stream) : launch_many<D, Paged, 4>(a, blocks, stream);
+    return waves == 8 ? launch_many<D, Paged, 8, SC>(a, blocks, stream) : launch_many<D, Paged, 4, SC>(a, blocks, stream);
 }
+template <int SC>
 static hipError_t launch_many(const AttendArgs* a, int d, bool paged, int waves, int blocks, hipStream_t stream)
 {
-    if (d == 128) return paged ? launch_many<128, true>(a, waves, blocks, stream) : launch_many<128, false>(a, waves, blocks, stream);
-    return paged ? launch_many<64, true>(a, waves, blocks, stream) : launch_many<64, false>(a, waves, blocks, stream);
+    if (d == 128) return paged ? launch_many<128, true, SC>(a, waves, blocks, stream) : launch_many<128, false, SC>(a, waves, blocks, stream);
+    return paged ? launch_many<64, true, SC>(a, waves, blocks, stream) : launch_many<64, false, SC>(a, waves, blocks, stream);
+}
+static hipError_t launch_many(const AttendArgs* a, Scores scores, int d, bool paged, int waves, int blocks, hipStream_t stream)
+{
+    switch (scores) {
+        case kPlainScores: return launch_many<kPlainScores>(a, d, paged, waves, blocks, stream);
+        case kWindowed: return launch_many<kWindowed>(a, d, paged, waves, blocks, stream);
+        default: return launch_many<kCapped>(a, d, paged, waves, blocks, stream);
+    }
 }
 
 hipError_t prepare_attend_mfma()
 {
-    for (int x = 0; x < 8; ++x) {
-        const hipError_t e = launch_many(nullptr, x & 1 ? 128 : 64, x & 2, x & 4 ? 8 : 4, 0, nullptr);
+    for (int x = 0; x < 24; ++x) {
+        const hipError_t e = launch_many(nullptr, (Scores)(x / 8), x & 1 ? 128 : 64, x & 2, x & 4 ? 8 : 4, 0, nullptr);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -612,7 +671,7 @@ hipError_t prepare_attend_mfma()
 
 hipError_t launch_attend_mfma(const AttendArgs& a, int waves, int items, hipStream_t stream)
 {
-    return launch_many(&a, a.d, a.table != nullptr, waves, items * a.Hkv, stream);
+    return launch_many(&a, scores_of(a), a.d, a.table != nullptr, waves, items * a.Hkv, stream);
 }
 
 }  // namespace dyspec

@@ -35,7 +35,7 @@ template <int D, int NW> constexpr int few_lds_bytes(int seen_blocks)
 
 template <int N> __device__ __forceinline__ void wait_loads_but() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
-template <int D, int NW>
+template <int D, int NW, int SC>
 __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
 {
     const AttendArgs& a = attend_args_here();
@@ -53,9 +53,10 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
     const int rows = a.G * s.N, r0 = it.block * kFewRows;
     const int j_first = div_G(a, r0);
     const int end = s.C + div_G(a, min(r0 + kFewRows, rows) - 1) + 1;        // keys that some row of the block may see
-    const int n_parts = s.parts > 1 ? (end + s.share - 1) / s.share : 1;
+    const int begin = walk_begin<SC>(a, s, j_first);
+    const int n_parts = s.parts > 1 ? (end - begin + s.share - 1) / s.share : 1;
     if (it.part >= n_parts) return;
-    const int k_begin = s.parts > 1 ? it.part * s.share : 0;
+    const int k_begin = begin + (s.parts > 1 ? it.part * s.share : 0);
     const int k_end = s.parts > 1 ? min(end, k_begin + s.share) : end;
     const int last = k_end - 1;
     const int n_blocks = (k_end - k_begin + kKeys - 1) / kKeys;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
     if (a.mask) {
         typedef __attribute__((address_space(3))) uint32_t* lds_u32;
         for (int x = threadIdx.x; x < (n_blocks - seen0) * kFewRows; x += 64 * NW)
-            *(lds_u32)(uint32_t)(seen_lds + 4 * x) = seen_bits(a, s, div_G(a, min(r0 + (x & 31), rows - 1)), k_begin + kKeys * (seen0 + (x >> 5)));
+            *(lds_u32)(uint32_t)(seen_lds + 4 * x) = seen_bits<SC>(a, s, div_G(a, min(r0 + (x & 31), rows - 1)), k_begin + kKeys * (seen0 + (x >> 5)));
     }
     // ---- direct loads of a block: load x brings rows kRowsPerLoad * x ..; rows past the last key repeat it
     const uint32_t k_stride = (uint32_t)a.k_stride, v_stride = (uint32_t)a.v_stride;
@@ -174,7 +175,13 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
     for (int db = 0; db < DB; ++db) acc[db] = zero16;
     float m_run = kLowest, l_run = 0.0f;
     const float c2 = a.c2;
-    const int full = a.mask ? s.C : s.C + j_first + 1;                       // keys before this one are every row's
+    const int full = a.mask || (SC != kPlainScores && a.rel) ? s.C : s.C + j_first + 1;      // keys before this one are every row's
+    int window0 = 0, border = 0;                 // first key of the lane's row's window; keys before `border` may be behind some row's
+    if constexpr (SC != kPlainScores) {
+        border = window0 = window_begin<SC>(a, s, row_j);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) border = max(border, __shfl_xor(border, o, kWave));
+    }
 
     while (have) {
         const int key0 = k_begin + kKeys * b, next = b + NW;
@@ -188,11 +195,12 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
         bf16x8 fr[KK];
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) fr[kk] = *(lds_bf16x8)(uint32_t)k_off[kk];
-        const bool masked = key0 + kKeys > full || key0 + kKeys > k_end;
+        const bool masked = key0 + kKeys > full || key0 + kKeys > k_end || (SC != kPlainScores && key0 < border);
         uint32_t seen = ~0u;                     // bit 8 (x / 4) + x % 4: the lane's key of register x
         if (masked) {
             if (a.mask && b >= seen0) seen = *(__attribute__((address_space(3))) const uint32_t*)(uint32_t)(seen_lds + 4 * (kFewRows * (b - seen0) + n));
-            else seen = causal_bits(s, row_j, key0);
+            else if constexpr (SC == kPlainScores) seen = causal_bits(s, row_j, key0);
+            else seen = near_tokens(a, s, row_j, key0, causal_bits(s, row_j, key0) & bits_from(window0, key0));
             if (k_end - key0 < kKeys) seen &= (1u << (k_end - key0)) - 1u;
             seen >>= 4 * g;
         }
@@ -202,6 +210,10 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
         floatx16 S = zero16;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk], qf[kk], S, 0, 0, 0);
+        if constexpr (SC == kCapped) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) S[x] = capped_score<false>(S[x], a.cap_in);
+        }
         // ---- weights against the reference as it stands; if a lane's sum says that is too low (the first block's always does)
         //      it is raised to the true maximum and they are taken again
         float p[16], ls = 0.0f;
@@ -346,7 +358,7 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
         }
     }
     if (__builtin_expect(bad != 0u, 0))
-        look_again<__bf16, kSlotFew, D>(bad, wave * RW, 0, D, kFewRows, [=](int row) {
+        look_again<__bf16, kSlotFew, D, SC>(bad, wave * RW, 0, D, kFewRows, [=](int row) {
             float M = kLowest;
 #pragma unroll
             for (int z = 0; z < NW; ++z) M = fmaxf(M, (*(lds_floatx2)(uint32_t)(ml_lds + 8 * (32 * z + row))).x);
@@ -358,35 +370,51 @@ __global__ __launch_bounds__(64 * NW) void attend_short_kernel(AttendArgs)
 // the last blocks of a tree of N rows: it may begin and end inside a block
 static int seen_blocks(const AttendArgs& a, int most_new) { return a.mask ? (most_new + kKeys - 1) / kKeys + 1 : 0; }
 
-template <int D, int NW>
+template <int D, int NW, int SC>
 static hipError_t raise_lds()
 {
     static std::atomic<unsigned long long> done{0};
-    return raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_short_kernel<D, NW>), few_lds_bytes<D, NW>(DYSPEC_MAX_NODES / kKeys + 1), done);
+    return raise_dynamic_lds_once(reinterpret_cast<const void*>(&attend_short_kernel<D, NW, SC>), few_lds_bytes<D, NW>(DYSPEC_MAX_NODES / kKeys + 1), done);
+}
+template <int SC>
+static hipError_t raise_lds_of_all()
+{
+    hipError_t e = raise_lds<128, 8, SC>();
+    if (e == hipSuccess) e = raise_lds<128, 4, SC>();
+    if (e == hipSuccess) e = raise_lds<64, 8, SC>();
+    return e == hipSuccess ? raise_lds<64, 4, SC>() : e;
 }
 
 hipError_t prepare_attend_short()
 {
-    hipError_t e = raise_lds<128, 8>();
-    if (e == hipSuccess) e = raise_lds<128, 4>();
-    if (e == hipSuccess) e = raise_lds<64, 8>();
-    return e == hipSuccess ? raise_lds<64, 4>() : e;
+    hipError_t e = raise_lds_of_all<kPlainScores>();
+    if (e == hipSuccess) e = raise_lds_of_all<kWindowed>();
+    return e == hipSuccess ? raise_lds_of_all<kCapped>() : e;
 }
 
-template <int D, int NW>
+template <int D, int NW, int SC>
 static hipError_t launch_few(const AttendArgs& a, int most_new, int blocks, hipStream_t stream)
 {
-    const hipError_t e = raise_lds<D, NW>();
+    const hipError_t e = raise_lds<D, NW, SC>();
     if (e != hipSuccess) return e;
-    attend_short_kernel<D, NW><<<blocks, 64 * NW, few_lds_bytes<D, NW>(seen_blocks(a, most_new)), stream>>>(a);
+    attend_short_kernel<D, NW, SC><<<blocks, 64 * NW, few_lds_bytes<D, NW>(seen_blocks(a, most_new)), stream>>>(a);
     return hipGetLastError();
+}
+template <int SC>
+static hipError_t launch_few(const AttendArgs& a, int waves, int most_new, int blocks, hipStream_t stream)
+{
+    if (a.d == 128) return waves == 8 ? launch_few<128, 8, SC>(a, most_new, blocks, stream) : launch_few<128, 4, SC>(a, most_new, blocks, stream);
+    return waves == 8 ? launch_few<64, 8, SC>(a, most_new, blocks, stream) : launch_few<64, 4, SC>(a, most_new, blocks, stream);
 }
 
 hipError_t launch_attend_short(const AttendArgs& a, int waves, int most_new, int items, hipStream_t stream)
 {
     const int blocks = items * a.Hkv;
-    if (a.d == 128) return waves == 8 ? launch_few<128, 8>(a, most_new, blocks, stream) : launch_few<128, 4>(a, most_new, blocks, stream);
-    return waves == 8 ? launch_few<64, 8>(a, most_new, blocks, stream) : launch_few<64, 4>(a, most_new, blocks, stream);
+    switch (scores_of(a)) {
+        case kPlainScores: return launch_few<kPlainScores>(a, waves, most_new, blocks, stream);
+        case kWindowed: return launch_few<kWindowed>(a, waves, most_new, blocks, stream);
+        default: return launch_few<kCapped>(a, waves, most_new, blocks, stream);
+    }
 }
 
 }  // namespace dyspec
