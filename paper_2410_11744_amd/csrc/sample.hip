@@ -10,71 +10,79 @@
 //
 // A cut by sums (of weights, or of ones for top-k) is found in three steps: a histogram over 2048 even steps of the distance to the
 // maximum (a few tokens a bin; by the bits of the logits most tokens would meet in a few bins), the bin where the sum reaches what
-// is kept, and the tokens of that bin one by one: each adds up those before it.  A bin with more than kListed tokens (equal logits,
+// is kept, and the tokens of that bin one by one: each adds up those before it.  A bin with more than kRanked tokens (equal logits,
 // or masks of the type's lowest value) is gone through by the bits of its logits instead, and equal ones by index.
+//
+// Passes over the whole row cost most (a compute unit has 32000 tokens of it), so a draw makes a list of the tokens that can be kept, in
+// order of their indices, once the first cut's bin is known: what follows goes over the list if that has up to kListMost tokens.
 //
 // A workgroup has one row, held in registers up to 32768 tokens, else read again for every pass; each of its 16 waves has a run of
 // the vocabulary, so that sums over waves, and then over the threads of one run, find a place in the order of the indices.
 #include "sample.h"
 
+#include "lane_ops.h"
 #include "launch.h"
 #include "vocab_common.h"
 
 namespace dyspec {
 
-typedef unsigned long long u64;
-
 constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / kWave;
-constexpr int kBins = 2048, kListed = 1024;
+constexpr int kBins = 2048, kRanked = 1024;      // kRanked: tokens of a bin that are looked at one by one
+constexpr int kListMost = 4096;
+constexpr int kRankAll = 128;                    // of a list that short every token is, without a histogram
 constexpr int kHeldTokens = 32;                  // of a thread whose row is held
 constexpr int kWeightBits = 45;                  // the largest weight is 2^kWeightBits: 2^18 of them stay below 2^63
 static_assert(DYSPEC_MAX_SAMPLE_VOCAB <= 1 << (63 - kWeightBits), "sums fit");
+static_assert(kRowWaves == 16, "what the waves leave is gone through by a row of 16 lanes");
 
-struct Listed { float x; int i; u64 amount; };
+struct Token { float x; int i; };
+struct Ranked { float x; int i; u64 amount; };
 
 struct SampleLds {
     u64 hist[kBins];
-    Listed list[kListed];
+    Ranked ranked[kRanked];
     u64 sums[kRowWaves];
     float hi[kRowWaves], lo[kRowWaves];
-    int odd[kRowWaves];
-    int counts[kRowWaves];
-    u64 before;                                  // of a bin, of a token: the sum up to it
-    u64 amount;
-    int found, n_listed;
-    float cut_x;
-    int cut_i;
+    int odd[kRowWaves], counts[kRowWaves], kept[kRowWaves];
+    u64 before;                                  // of a bin: the sum up to it
+    u64 amount;                                  // of a token
+    int found, n_ranked;
+    Token cut;
 };
+struct ListLds { Token list[kListMost]; };
 
 template <typename T> struct RowPiece;           // 16 bytes of a row
 template <> struct RowPiece<float> {
     static constexpr int kTokens = 4;
     static __device__ __forceinline__ float value(const uint4& r, int e) { return __uint_as_float((&r.x)[e]); }
-    static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
 };
 template <> struct RowPiece<__bf16> {
     static constexpr int kTokens = 8;
     static __device__ __forceinline__ float value(const uint4& r, int e) { const uint32_t w = (&r.x)[e / 2]; return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16); }
 };
 
+// (of 64 bits, as an operand that takes no vector registers)
+__device__ __forceinline__ double constant(double c) { asm("" : "+s"(c)); return c; }
+
 // exp2(z) in whole numbers of 2^-kWeightBits, z <= 0.  The fraction's power by a polynomial through Chebyshev's nodes, to 3.7e-14.
 __device__ __forceinline__ u64 weight_of(double z)
 {
-    constexpr double kShift = 6755399441055744.0;              // 1.5 * 2^52: the sum's low bits are the nearest whole number
+    const double shift = constant(6755399441055744.0);         // 1.5 * 2^52: the sum's low bits are the nearest whole number
     z = fmax(z, -100.0);
-    const double t = z + kShift, f = z - (t - kShift);
+    const double t = z + shift, f = z - (t - shift);
     const int n = (int)__double2loint(t);
-    double p = 1.0203121063391729e-07;
-    p = fma(p, f, 1.3255224878668817e-06);
-    p = fma(p, f, 1.525268684626772e-05);
-    p = fma(p, f, 0.00015403455852453838);
-    p = fma(p, f, 0.0013333558179043112);
-    p = fma(p, f, 0.009618129159402558);
-    p = fma(p, f, 0.055504108664760424);
-    p = fma(p, f, 0.2402265069581299);
-    p = fma(p, f, 0.6931471805599453);
+    double p = constant(1.0203121063391729e-07);
+    p = fma(p, f, constant(1.3255224878668817e-06));
+    p = fma(p, f, constant(1.525268684626772e-05));
+    p = fma(p, f, constant(0.00015403455852453838));
+    p = fma(p, f, constant(0.0013333558179043112));
+    p = fma(p, f, constant(0.009618129159402558));
+    p = fma(p, f, constant(0.055504108664760424));
+    p = fma(p, f, constant(0.2402265069581299));
+    p = fma(p, f, constant(0.6931471805599453));
     p = fma(p, f, 1.0);
-    const double w = ldexp(p, n + kWeightBits) + 4503599627370496.0;      // + 2^52: rounded to a whole number in the low bits
+    // times 2^(n + kWeightBits) by the exponent's bits; + 2^52: rounded to a whole number in the low bits
+    const double w = __hiloint2double(__double2hiint(p) + ((n + kWeightBits) << 20), __double2loint(p)) + constant(4503599627370496.0);
     return (u64)__double_as_longlong(w) & 0xfffffffffffffull;
 }
 
@@ -84,6 +92,7 @@ __device__ __forceinline__ uint32_t ordered_bits(float x)
     const uint32_t u = __float_as_uint(x + 0.0f);
     return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float of_ordered_bits(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
 // A row as a thread has it.  Wave w has tokens w * span .. of the row, lane l of it the kTokens from w * span + (64 p + l) * kTokens
 // on, p < pieces.  Places past the row's end hold a NaN, which no comparison keeps.
@@ -131,10 +140,14 @@ template <typename T, bool Held> struct Row {
     {
         if constexpr (Held) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                if (p < pieces) f(held[p], index(p));
+            for (int p = 0; p < NP; ++p) {
+                int i = index(p);
+                asm volatile("" : "+v"(i));
+                if (p < pieces) f(held[p], i);
+            }
         } else {
             constexpr int kAhead = 4;
+#pragma unroll 1
             for (int p0 = 0; p0 < pieces; p0 += kAhead) {
                 uint4 r[kAhead];
 #pragma unroll
@@ -145,13 +158,35 @@ template <typename T, bool Held> struct Row {
             }
         }
     }
-    // f(logit, index)
+    // f(logit, index).  (What a pass makes of a logit is made anew by the next: kept from one to the other it would not fit the registers.)
     template <typename F> __device__ __forceinline__ void each(F&& f) const
     {
         each_piece([&](const uint4& r, int i) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f(RowPiece<T>::value(r, e), i + e);
+            for (int e = 0; e < VEC; ++e) {
+                float x = RowPiece<T>::value(r, e);
+                asm volatile("" : "+v"(x));
+                f(x, i + e);
+                if (e & 1) __builtin_amdgcn_sched_barrier(0);      // (two at a time: more chains of weights side by side would not fit either)
+            }
         });
+    }
+};
+
+// The list, of which a thread has a token or a few, one after the other.
+struct List {
+    const Token* at;
+    int n, each_n;                               // tokens of the list, of a thread
+
+    // f(logit, index); NaN where a thread has none
+    template <typename F> __device__ __forceinline__ void each(F&& f) const
+    {
+#pragma unroll 1
+        for (int y = 0; y < each_n; ++y) {
+            const int to = (int)threadIdx.x * each_n + y;
+            const Token k = at[min(to, kListMost - 1)];
+            f(to < n ? k.x : __uint_as_float(~0u), k.i);
+        }
     }
 };
 
@@ -159,55 +194,104 @@ template <typename T, bool Held> struct Row {
 struct Cut {
     float x;
     int i;
-    __device__ __forceinline__ bool keeps(float y, int j) const { return y > x || (y == x && j <= i); }
+    __device__ __forceinline__ bool keeps(float y, int j) const { return (y > x) | ((y == x) & (j <= i)); }
 };
 
-__device__ __forceinline__ u64 wave_upto(u64 v, int lane)
-{
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const u64 up = __shfl_up(v, o, kWave);
-        if (lane >= o) v += up;
+// Even steps of the distance to the maximum.  Roundings keep the order, so the bins are in it; a distance of infinity times a scale of
+// zero is a NaN, which fminf passes over, and so is what stands where there is no token: the last bin, at a weight of zero.
+struct Bins {
+    float top, scale;
+    __device__ __forceinline__ Bins(float top, float range) : top(top), scale(uniform(range > 1e-30f ? (float)(kBins - 1) / range : 0.0f)) {}
+    __device__ __forceinline__ int of(float x) const { return (int)fminf((top - x) * scale, (float)(kBins - 1)); }
+    // no token of the bins up to this one is below, none of it above (a few of the bins beside it may lie between)
+    __device__ __forceinline__ float least(int bin) const
+    {
+        if (bin == kBins - 1 || scale == 0.0f) return -INFINITY;
+        return uniform(top - (float)(bin + 1) / scale * (1.0f + 0x1p-20f) - fabsf(top) * 0x1p-22f);
     }
-    return v;
+    __device__ __forceinline__ float most(int bin) const
+    {
+        return bin == 0 ? top : uniform(top - (float)bin / scale * (1.0f - 0x1p-20f) + fabsf(top) * 0x1p-22f);
+    }
+};
+
+template <int CTRL, int ROW_MASK = 0xf> __device__ __forceinline__ u64 dpp_or_zero(u64 x)
+{
+    return (u64)(uint32_t)dpp_or_zero<CTRL, ROW_MASK>((int)(x >> 32)) << 32 | (uint32_t)dpp_or_zero<CTRL, ROW_MASK>((int)x);
+}
+// The sum over the lanes of a row of 16 up to this one; of the wave.
+template <typename N> __device__ __forceinline__ N row_upto(N x)
+{
+    x += dpp_or_zero<0x111>(x);
+    x += dpp_or_zero<0x112>(x);
+    x += dpp_or_zero<0x114>(x);
+    x += dpp_or_zero<0x118>(x);
+    return x;
+}
+__device__ __forceinline__ u64 wave_upto(u64 x)
+{
+    x = row_upto(x);
+    x += dpp_or_zero<kDppBcast15, 0xa>(x);
+    x += dpp_or_zero<kDppBcast31, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ int of_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
+__device__ __forceinline__ u64 of_lane(u64 x, int l) { return (u64)(uint32_t)of_lane((int)(x >> 32), l) << 32 | (uint32_t)of_lane((int)x, l); }
+__device__ __forceinline__ float dpp_max(float x)              // of the row of 16
+{
+    auto with = [](float y, auto ctrl) { return fmaxf(y, __int_as_float(dpp_or_zero<decltype(ctrl)::value>(__float_as_int(y)))); };
+    x = with(x, std::integral_constant<int, kDppXor1>{});
+    x = with(x, std::integral_constant<int, kDppXor2>{});
+    x = with(x, std::integral_constant<int, kDppHalfMirror>{});
+    return with(x, std::integral_constant<int, kDppMirror>{});
+}
+__device__ __forceinline__ float wave_max_dpp(float x)
+{
+    x = dpp_max(x);
+    return fmaxf(fmaxf(readlane_f32(x, 0), readlane_f32(x, 16)), fmaxf(readlane_f32(x, 32), readlane_f32(x, 48)));
 }
 
-// The token at which the sum of amount(logit, index), in order of the indices, first exceeds target_of(total); there is one.  Its sum
-// is left in lds.amount and the total returned.  By all threads; lds.sums and what follows it is free before and after.
-template <typename T, bool Held, typename A, typename G>
-__device__ __forceinline__ int locate(const Row<T, Held>& row, SampleLds& lds, A&& amount, G&& target_of, u64* total_out)
+// Of what the 16 waves left: the sum before this wave's, and of all.
+template <typename N> __device__ __forceinline__ N before_wave(const N* left, int wave, N* total)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const N upto = row_upto(left[threadIdx.x & 15]);
+    *total = of_lane(upto, 15);
+    return wave == 0 ? 0 : of_lane(upto, wave - 1);
+}
+// The sum of the threads' own up to and with this one's, and of all.  One barrier; lds.sums is free before.
+__device__ __forceinline__ u64 block_upto(SampleLds& lds, u64 mine, u64* total)
+{
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const u64 upto = wave_upto(mine);
+    if (lane == kWave - 1) lds.sums[wave] = upto;
+    __syncthreads();
+    return before_wave(lds.sums, wave, total) + upto;
+}
+
+// The token at which the sum of amount(logit, index), in order of the indices, first exceeds target_of(total); there is one.  Its amount
+// is left in lds.amount.  By all threads; lds.sums is free before and after.
+template <typename T, bool Held, typename A, typename G>
+__device__ __forceinline__ int locate(const Row<T, Held>& row, SampleLds& lds, A&& amount, G&& target_of, u64* total)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     u64 s = 0;
     row.each([&](float x, int i) __attribute__((always_inline)) { s += amount(x, i); });
-    s = wave_sum(s);
-    if (lane == 0) lds.sums[wave] = s;
+    s = wave_upto(s);
+    if (lane == kWave - 1) lds.sums[wave] = s;
     __syncthreads();
-    u64 total = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) total += lds.sums[w];
-    const u64 target = target_of(total);
-    u64 before = 0;
-    int owner = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) {
-        const bool past = before + lds.sums[w] <= target && owner == w;      // (all runs up to this one, and not yet there)
-        if (past) { before += lds.sums[w]; owner = w + 1; }
-    }
-    owner = min(owner, kRowWaves - 1);
+    const u64 upto = row_upto(lds.sums[lane & 15]);
+    *total = of_lane(upto, 15);
+    const u64 target = target_of(*total);
+    const int owner = min(__builtin_popcountll(ballot(upto <= target) & 0xffffull), kRowWaves - 1);      // the first run that goes past the target
+    const u64 before = owner == 0 ? 0 : of_lane(upto, owner - 1);
     __syncthreads();
     // that run once more, shared out among all threads
     const int each = (row.span() + kRowThreads - 1) / kRowThreads;
     const int begin = owner * row.span() + tid * each, end = min(min(begin + each, (owner + 1) * row.span()), row.V);
     u64 mine = 0;
     for (int i = begin; i < end; ++i) mine += amount(logit_to_float(row.at[i]), i);
-    const u64 upto = wave_upto(mine, lane);
-    if (lane == kWave - 1) lds.sums[wave] = upto;
-    __syncthreads();
-    u64 base = before;
-    for (int w = 0; w < wave; ++w) base += lds.sums[w];
-    u64 at = base + upto - mine;
-    if (at <= target && target < base + upto) {
+    u64 unused, at = before + block_upto(lds, mine, &unused) - mine;
+    if (at <= target && target < at + mine) {
         for (int i = begin; i < end; ++i) {
             const u64 a = amount(logit_to_float(row.at[i]), i);
             if (target < at + a) { lds.found = i; lds.amount = a; break; }
@@ -215,87 +299,95 @@ __device__ __forceinline__ int locate(const Row<T, Held>& row, SampleLds& lds, A
         }
     }
     __syncthreads();
-    *total_out = total;
-    return lds.found;
+    return uniform(lds.found);
+}
+// The same of the list.
+template <typename A, typename G>
+__device__ __forceinline__ int locate(const List& list, SampleLds& lds, A&& amount, G&& target_of, u64* total)
+{
+    u64 mine = 0;
+    list.each([&](float x, int i) __attribute__((always_inline)) { mine += amount(x, i); });
+    u64 at = block_upto(lds, mine, total) - mine;
+    const u64 target = target_of(*total);
+    if (at <= target && target < at + mine)
+        list.each([&](float x, int i) __attribute__((always_inline)) {
+            const u64 a = amount(x, i);
+            if (at <= target && target < at + a) { lds.found = i; lds.amount = a; }
+            at += a;
+        });
+    __syncthreads();
+    return uniform(lds.found);
 }
 
 // The histogram's bin, from bin 0 on, with which the sum first reaches what target_of(total) says.  lds.before: the sum before it.
 template <typename G>
-__device__ __forceinline__ int reach(SampleLds& lds, G&& target_of, u64* target_out)
+__device__ __forceinline__ int reach(SampleLds& lds, G&& target_of, u64* target)
 {
     constexpr int PER = kBins / kRowThreads;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     u64 h[PER], s = 0;
 #pragma unroll
-    for (int y = 0; y < PER; ++y) s += h[y] = lds.hist[PER * tid + y];
-    const u64 upto = wave_upto(s, lane);
-    if (lane == kWave - 1) lds.sums[wave] = upto;
-    __syncthreads();
-    u64 base = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) {
-        if (w == wave) base = total;
-        total += lds.sums[w];
-    }
-    const u64 target = target_of(total);
-    u64 at = base + upto - s;
-    if (at < target && target <= base + upto) {
+    for (int y = 0; y < PER; ++y) s += h[y] = lds.hist[PER * threadIdx.x + y];
+    u64 total, at = block_upto(lds, s, &total) - s;
+    *target = target_of(total);
+    if (at < *target && *target <= at + s) {
 #pragma unroll
         for (int y = 0; y < PER; ++y) {
-            if (at < target && target <= at + h[y]) { lds.found = PER * tid + y; lds.before = at; }
+            if (at < *target && *target <= at + h[y]) { lds.found = PER * threadIdx.x + y; lds.before = at; }
             at += h[y];
         }
     }
     __syncthreads();
-    *target_out = target;
-    return lds.found;
+    return uniform(lds.found);
 }
-
-__device__ __forceinline__ void clear_bins(SampleLds& lds)
+__device__ __forceinline__ void clear_bins(SampleLds& lds)     // (a barrier follows)
 {
 #pragma unroll
     for (int y = 0; y < kBins / kRowThreads; ++y) lds.hist[y * kRowThreads + threadIdx.x] = 0;
-    if (threadIdx.x == 0) lds.n_listed = 0;
-    __syncthreads();
+    if (threadIdx.x == 0) lds.n_ranked = 0;
 }
 
-// The cut within `cut` at which the sum of amount(logit), taken in the tokens' order, first reaches target_of(total).  `range`: distance
-// to the maximum that the bins share out.
-template <typename T, bool Held, typename A, typename G>
-__device__ __forceinline__ Cut select(const Row<T, Held>& row, SampleLds& lds, Cut cut, float top, float range, A&& amount, G&& target_of)
+// Of the n tokens in lds.ranked: the one with which `before` and the amounts of those in front of it first reach the target.
+__device__ __forceinline__ Cut rank(SampleLds& lds, int n, u64 before, u64 target)
 {
-    const int tid = threadIdx.x;
-    const float scale = range > 1e-30f ? (float)(kBins - 1) / range : 0.0f;
-    // (roundings keep the order, so bins are in it; a distance of infinity times a scale of zero is a NaN, which fminf passes over)
-    auto bin_of = [=](float x) __attribute__((always_inline)) -> int { return (int)fminf((top - x) * scale, (float)(kBins - 1)); };
-    clear_bins(lds);
-    row.each([&](float x, int i) __attribute__((always_inline)) {
-        if (cut.keeps(x, i)) atomicAdd(&lds.hist[bin_of(x)], amount(x));
-    });
-    __syncthreads();
-    u64 target;
-    const int bin = reach(lds, target_of, &target);
-    u64 before = lds.before;
-    row.each([&](float x, int i) __attribute__((always_inline)) {
-        if (cut.keeps(x, i) && bin_of(x) == bin) {
-            const int n = atomicAdd(&lds.n_listed, 1);
-            if (n < kListed) lds.list[n] = Listed{ x, i, amount(x) };
+    if ((int)threadIdx.x < n) {
+        const Ranked me = lds.ranked[threadIdx.x];
+        u64 at = before;
+        constexpr int kAhead = 4;                                  // (a read of LDS takes longer than looking at what came)
+#pragma unroll 1
+        for (int y0 = 0; y0 < n; y0 += kAhead) {
+            Ranked l[kAhead];
+#pragma unroll
+            for (int y = 0; y < kAhead; ++y) l[y] = lds.ranked[min(y0 + y, kRanked - 1)];
+#pragma unroll
+            for (int y = 0; y < kAhead; ++y)
+                at += (y0 + y < n) & ((l[y].x > me.x) | ((l[y].x == me.x) & (l[y].i < me.i))) ? l[y].amount : 0;
         }
-    });
+        if (at < target && target <= at + me.amount) lds.cut = Token{ me.x, me.i };
+    }
     __syncthreads();
-    const int n = lds.n_listed;
-    if (n <= kListed) {
-        if (tid < n) {
-            const Listed me = lds.list[tid];
-            u64 at = before;
-            for (int y = 0; y < n; ++y) {
-                const Listed l = lds.list[y];
-                if (l.x > me.x || (l.x == me.x && l.i < me.i)) at += l.amount;
+    return Cut{ uniform(lds.cut.x), uniform(lds.cut.i) };
+}
+
+// The cut inside a bin: where, with `before` before the bin, the sum of the amounts of its tokens first reaches the target.  src: the row
+// or the list, of which `cut` says what counts.
+template <typename T, bool Held, typename Src, typename A>
+__device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, SampleLds& lds, const Cut& cut, const Bins& bins, int bin, u64 before, u64 target, A&& amount)
+{
+    const float least = bins.least(bin), most = bins.most(bin);
+    src.each([&](float x, int i) __attribute__((always_inline)) {
+        if ((x >= least) & (x <= most)) {
+            if (cut.keeps(x, i) & (bins.of(x) == bin)) {
+                const int n = atomicAdd(&lds.n_ranked, 1);
+                if (n < kRanked) { lds.ranked[n].x = x; lds.ranked[n].i = i; }
             }
-            if (at < target && target <= at + me.amount) { lds.cut_x = me.x; lds.cut_i = me.i; }
         }
+    });
+    __syncthreads();
+    const int n = uniform(lds.n_ranked);
+    if (n <= kRanked) {
+        if ((int)threadIdx.x < n) lds.ranked[threadIdx.x].amount = amount(lds.ranked[threadIdx.x].x);
         __syncthreads();
-        return Cut{ lds.cut_x, lds.cut_i };
+        return rank(lds, n, before, target);
     }
     // too many: by the bits of the logits, eleven at a time, from the highest value down
     __syncthreads();                                               // (all have seen n)
@@ -305,32 +397,68 @@ __device__ __forceinline__ Cut select(const Row<T, Held>& row, SampleLds& lds, C
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 1023u : 2047u, high = pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u;
         clear_bins(lds);
-        row.each([&](float x, int i) __attribute__((always_inline)) {
+        __syncthreads();
+        src.each([&](float x, int i) __attribute__((always_inline)) {
             const uint32_t key = ordered_bits(x);
-            if (cut.keeps(x, i) && bin_of(x) == bin && (key & high) == known) atomicAdd(&lds.hist[digits - ((key >> shift) & digits)], amount(x));
+            if (cut.keeps(x, i) & (bins.of(x) == bin) & ((key & high) == known)) atomicAdd(&lds.hist[digits - ((key >> shift) & digits)], amount(x));
         });
         __syncthreads();
         u64 unused;
         const u64 rest = target - before;
         const int digit = reach(lds, [=](u64) { return rest; }, &unused);
         known |= (digits - (uint32_t)digit) << shift;
-        before += lds.before;
+        before += uniform(lds.before);
         __syncthreads();
     }
-    const float x_cut = __uint_as_float(known & 0x80000000u ? known ^ 0x80000000u : ~known);
+    const float x_cut = of_ordered_bits(known);
     const u64 each = amount(x_cut), last = (target - before + each - 1) / each - 1;      // so many equal ones are before the last that is kept
     u64 unused;
-    const int i_cut = locate(row, lds, [=](float x, int i) -> u64 { return x == x_cut && cut.keeps(x, i); }, [=](u64) { return last; }, &unused);
-    return Cut{ x_cut, i_cut };
+    const Cut within = cut;
+    return Cut{ x_cut, locate(row, lds, [=](float x, int i) -> u64 { return (x == x_cut) & within.keeps(x, i); }, [=](u64) { return last; }, &unused) };
 }
 
-template <typename T, bool Held, int S>
+// The tokens with a logit of `least` or more, in order of their indices, if they are kListMost or fewer.
+template <typename T, bool Held>
+__device__ __forceinline__ bool make_list(const Row<T, Held>& row, SampleLds& lds, Token* to, float least, List& list)
+{
+    constexpr int VEC = RowPiece<T>::kTokens;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    int mine = 0;
+    row.each([&](float x, int) __attribute__((always_inline)) { mine += __builtin_popcountll(ballot(x >= least)); });
+    if (lane == 0) lds.counts[wave] = mine;
+    __syncthreads();
+    int at = before_wave(lds.counts, wave, &list.n);
+    __syncthreads();
+    list.at = to;
+    list.each_n = (list.n + kRowThreads - 1) / kRowThreads;
+    if (list.n > kListMost) return false;
+    row.each_piece([&](const uint4& r, int i) __attribute__((always_inline)) {
+        u64 there[VEC], any = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) any |= there[e] = ballot(RowPiece<T>::value(r, e) >= least);
+        if (any == 0) return;                                      // (the same for the wave)
+        int place = at;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            place += __builtin_amdgcn_mbcnt_hi((uint32_t)(there[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there[e], 0));
+            at += __builtin_popcountll(there[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if ((there[e] >> lane) & 1ull) to[place++] = Token{ RowPiece<T>::value(r, e), i + e };
+    });
+    __syncthreads();
+    return true;
+}
+
+// Drawn: a token is drawn; else the filtered logits are written.
+template <typename T, bool Held, bool Drawn, int S>
 __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
 {
     const SampleArgs<S>& a = *(const SampleArgs<S>*)(__attribute__((address_space(4))) const SampleArgs<S>*)__builtin_amdgcn_kernarg_segment_ptr();
     __shared__ SampleLds lds;
     constexpr int VEC = RowPiece<T>::kTokens;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = blockIdx.x;
     Row<T, Held> row;
     row.at = static_cast<const T*>(a.logits) + r * a.stride;
@@ -338,43 +466,86 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
     row.pieces = (a.V + kRowThreads * VEC - 1) / (kRowThreads * VEC);
     row.first = wave * row.span() + lane * VEC;
     row.load();
-    const int seq = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.n_seq && r >= a.row0[lane < a.n_seq ? lane : 0])) - 1;
+    const int seq = __builtin_popcountll(ballot(lane < a.n_seq && r >= a.row0[lane < a.n_seq ? lane : 0])) - 1;
     const Filter filter = a.filter[seq];
-    // ---- the largest logit, the smallest finite one; a row with a NaN or +inf, or without a finite logit, has no distribution
+    clear_bins(lds);
+    // ---- the largest logit and the smallest; a row with a NaN or +inf, or without a finite logit, has no distribution
     float hi = -INFINITY, lo = INFINITY;
-    int odd = 0;
+    bool odd = false;
     row.each([&](float x, int i) __attribute__((always_inline)) {
-        odd |= !(x < INFINITY) && i < a.V;
+        odd |= (x != x) & (i < a.V);
         hi = fmaxf(hi, x);
-        lo = fminf(lo, x > -INFINITY ? x : INFINITY);
+        lo = fminf(lo, x);
     });
-    hi = wave_max(hi);
-    lo = -wave_max(-lo);
-    odd = __any(odd);
-    if (lane == 0) { lds.hi[wave] = hi; lds.lo[wave] = lo; lds.odd[wave] = odd; }
+    hi = wave_max_dpp(hi);
+    lo = -wave_max_dpp(-lo);
+    const bool any_odd = ballot(odd) != 0;
+    if (lane == 0) { lds.hi[wave] = hi; lds.lo[wave] = lo; lds.odd[wave] = any_odd; }
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kRowWaves; ++w) { hi = fmaxf(hi, lds.hi[w]); lo = fminf(lo, lds.lo[w]); odd |= lds.odd[w]; }
-    const float top = hi;
-    const bool none = odd || !(top > -INFINITY);
+    const float top = uniform(dpp_max(lds.hi[lane & 15]));
+    lo = uniform(-dpp_max(-lds.lo[lane & 15]));
+    const bool none = ballot(lds.odd[lane & 15] != 0) != 0 || !(fabsf(top) < INFINITY);
+    const bool greedy = filter.temperature == 0.0f;
     Cut cut{ -INFINITY, a.V };
-    const double per_nat = 1.4426950408889634074 / (double)filter.temperature;
-    auto weight = [=](float x) __attribute__((always_inline)) -> u64 { return weight_of(((double)x - (double)top) * per_nat); };
+    List list;
+    list.n = 0;
+    bool listed = false;                                           // the list holds every token that is kept
+    Token* list_lds = nullptr;
+    if constexpr (Drawn) {
+        __shared__ ListLds room;
+        list_lds = room.list;
+    }
+    const double per_nat = uniform(1.4426950408889634074 / (double)filter.temperature), top64 = uniform((double)top);
+    auto weight = [=](float x) __attribute__((always_inline)) -> u64 { return weight_of(((double)x - top64) * per_nat); };
     if (none) {
         cut = Cut{ INFINITY, -1 };
-    } else if (filter.temperature == 0.0f) {
-        u64 unused;
-        cut = Cut{ top, locate(row, lds, [=](float x, int) -> u64 { return x == top; }, [](u64) -> u64 { return 0; }, &unused) };
+    } else if (greedy) {
+        int first = 0x7fffffff;
+        row.each([&](float x, int i) __attribute__((always_inline)) { first = min(first, x == top ? i : 0x7fffffff); });
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) first = min(first, __shfl_xor(first, o, kWave));
+        if (lane == 0) lds.counts[wave] = first;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) first = min(first, lds.counts[w]);
+        cut = Cut{ top, uniform(first) };
     } else {
-        if (filter.top_k > 0 && filter.top_k < a.V) {
-            const u64 k = (u64)filter.top_k;
-            cut = select(row, lds, cut, top, fminf(top - lo, 64.0f), [](float) -> u64 { return 1; }, [=](u64) { return k; });
-        }
-        if (filter.top_p < 1.0f) {
-            const double p = (double)filter.top_p;
-            // (kept: what has less than p of the sum before it)
-            cut = select(row, lds, cut, top, fminf(top - lo, 32.0f * filter.temperature), weight,
-                         [=](u64 total) -> u64 { return max((u64)1, (u64)ceil(p * (double)total)); });
+        bool cleared = true;
+#pragma unroll 1
+        for (int by_weight = 0; by_weight < 2; ++by_weight) {      // top-k's cut by ones, top-p's by weights
+            if (by_weight ? !(filter.top_p < 1.0f) : filter.top_k == 0 || filter.top_k >= a.V) continue;
+            auto amount = [=](float x) __attribute__((always_inline)) -> u64 { return by_weight ? weight(x) : 1; };
+            // (top-p keeps what has less than its share of the sum before it)
+            auto target_of = [=](u64 total) -> u64 { return by_weight ? max((u64)1, (u64)ceil((double)filter.top_p * (double)total)) : (u64)filter.top_k; };
+            if (Drawn && listed && list.n <= kRankAll) {           // (a token a thread)
+                const Token k = list.at[tid];
+                const u64 mine = tid < list.n && cut.keeps(k.x, k.i) ? amount(k.x) : 0;
+                u64 total;
+                block_upto(lds, mine, &total);
+                if (tid < list.n) lds.ranked[tid] = Ranked{ k.x, k.i, mine };
+                __syncthreads();
+                cut = rank(lds, list.n, 0, target_of(total));
+                continue;
+            }
+            const Bins bins(top, fminf(top - lo, by_weight ? 32.0f * filter.temperature : 64.0f));
+            const bool whole = cut.x == -INFINITY && cut.i >= a.V;
+            if (!cleared) {
+                clear_bins(lds);
+                __syncthreads();
+            }
+            cleared = false;
+            auto add = [&](float x, u64 n) __attribute__((always_inline)) { atomicAdd(&lds.hist[bins.of(x)], n); };
+            if (Drawn && listed) list.each([&](float x, int i) __attribute__((always_inline)) { if (cut.keeps(x, i)) add(x, amount(x)); });
+            else if (!whole) row.each([&](float x, int i) __attribute__((always_inline)) { if (cut.keeps(x, i)) add(x, weight(x)); });      // (top-k was first)
+            else if (by_weight) row.each([&](float x, int) __attribute__((always_inline)) { add(x, weight(x)); });
+            else row.each([&](float x, int) __attribute__((always_inline)) { add(x, 1); });
+            __syncthreads();
+            u64 target;
+            const int bin = reach(lds, target_of, &target);
+            const u64 before = uniform(lds.before);
+            if (Drawn && whole) listed = make_list(row, lds, list_lds, bins.least(bin), list);
+            if (Drawn && listed) cut = resolve(row, list, lds, cut, bins, bin, before, target, amount);
+            else cut = resolve(row, row, lds, cut, bins, bin, before, target, amount);
         }
         if (filter.min_p > 0.0f) {
             // the smallest logit whose weight, as a number of 64 bits, is min_p or more (those within 2^-54 of 1 are 1)
@@ -383,13 +554,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
             uint32_t key = max(ordered_bits(near), ordered_bits(-3.402823466e38f) + 2u) - 2u;
             float x;
             for (;; ++key) {
-                x = __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+                x = of_ordered_bits(key);
                 if (((double)x - (double)top) * per_nat >= least || x >= top) break;
             }
+            x = uniform(x);
             if (x > cut.x) cut = Cut{ x, a.V };
         }
     }
-    if (a.out) {
+    if constexpr (!Drawn) {
         T* const out = static_cast<T*>(a.out) + r * a.out_stride;
         constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80u;      // -inf
         __syncthreads();                                           // (in place: every thread has read what it wants of others)
@@ -411,68 +583,69 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
                 }
             }
         });
-        return;
-    }
-    // ---- the draw
-    if (none) {
-        if (tid == 0) { a.token[r] = -1; a.prob[r] = 0.0f; a.n_kept[r] = 0; }
-        return;
-    }
-    int kept = 0;
-    row.each([&](float x, int i) __attribute__((always_inline)) { kept += __builtin_popcountll(__builtin_amdgcn_ballot_w64(cut.keeps(x, i))); });
-    if (lane == 0) lds.counts[wave] = kept;
-    int token;
-    u64 total, mine;
-    if (filter.temperature == 0.0f) {
-        __syncthreads();
-        token = cut.i;
-        total = mine = 1;
     } else {
+        if (none || greedy) {
+            if (tid == 0) { a.token[r] = none ? -1 : cut.i; a.prob[r] = none ? 0.0f : 1.0f; a.n_kept[r] = none ? 0 : 1; }
+            return;
+        }
+        const bool whole = cut.x == -INFINITY && cut.i >= a.V;     // every token is kept
+        if (!listed && cut.x > -INFINITY) listed = make_list(row, lds, list_lds, cut.x, list);
         const double u = (double)fminf(fmaxf(a.uniform[r], 0.0f), 1.0f - 0x1p-24f);
-        token = locate(row, lds, [=](float x, int i) __attribute__((always_inline)) -> u64 { return cut.keeps(x, i) ? weight(x) : 0; },
-                       [=](u64 total) -> u64 { return (u64)(u * (double)total); }, &total);
-        mine = lds.amount;
-    }
-    if (tid == 0) {
-        int n = 0;
-        for (int w = 0; w < kRowWaves; ++w) n += lds.counts[w];
-        a.token[r] = token;
-        a.prob[r] = (float)((double)mine / (double)total);
-        a.n_kept[r] = n;
+        auto kept_weight = [=](float x, int i) __attribute__((always_inline)) -> u64 { return cut.keeps(x, i) ? weight(x) : 0; };
+        auto target_of = [=](u64 total) -> u64 { return (u64)(u * (double)total); };
+        int kept = 0;
+        auto count = [&](float x, int i) __attribute__((always_inline)) { kept += __builtin_popcountll(ballot(cut.keeps(x, i))); };
+        if (listed) list.each(count);
+        else if (!whole) row.each(count);
+        if (lane == 0) lds.kept[wave] = kept;
+        u64 total;
+        int token;
+        if (listed) token = locate(list, lds, kept_weight, target_of, &total);
+        else if (!whole) token = locate(row, lds, kept_weight, target_of, &total);
+        else token = locate(row, lds, [=](float x, int) __attribute__((always_inline)) -> u64 { return weight(x); }, target_of, &total);
+        int n;
+        before_wave(lds.kept, 0, &n);
+        if (tid == 0) {
+            a.token[r] = token;
+            a.prob[r] = (float)((double)lds.amount / (double)total);
+            a.n_kept[r] = whole ? a.V : n;
+        }
     }
 }
 
-template <typename T, bool Held, int S>
+template <typename T, bool Held, bool Drawn, int S>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, S>));
+    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, Drawn, S>));
     SampleArgs<S> a;
     static_cast<SampleHead&>(a) = head;
     for (int s = 0; s < head.n_seq; ++s) { a.row0[s] = row0[s]; a.filter[s] = filter[s]; }
     return kernel.launch(dim3(head.rows), kRowThreads, 0, stream, a);
 }
-template <typename T, bool Held>
+template <typename T, bool Held, bool Drawn>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    return head.n_seq <= 8 ? launch_rows<T, Held, 8>(head, row0, filter, stream) : launch_rows<T, Held, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
+    return head.n_seq <= 8 ? launch_rows<T, Held, Drawn, 8>(head, row0, filter, stream) : launch_rows<T, Held, Drawn, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
 }
 template <typename T>
-static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, bool held, hipStream_t stream)
+static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    return held ? launch_rows<T, true>(head, row0, filter, stream) : launch_rows<T, false>(head, row0, filter, stream);
+    const bool drawn = head.out == nullptr;
+    if (head.V <= kHeldTokens * kRowThreads)
+        return drawn ? launch_rows<T, true, true>(head, row0, filter, stream) : launch_rows<T, true, false>(head, row0, filter, stream);
+    return drawn ? launch_rows<T, false, true>(head, row0, filter, stream) : launch_rows<T, false, false>(head, row0, filter, stream);
 }
 
 hipError_t launch_sample(const SampleHead& a, const int* row0, const Filter* filter, int dtype, hipStream_t stream)
 {
     if (a.rows == 0) return hipSuccess;
-    const bool held = a.V <= kHeldTokens * kRowThreads;
-    return dtype == DYSPEC_F32 ? launch_rows<float>(a, row0, filter, held, stream) : launch_rows<__bf16>(a, row0, filter, held, stream);
+    return dtype == DYSPEC_F32 ? launch_rows<float>(a, row0, filter, stream) : launch_rows<__bf16>(a, row0, filter, stream);
 }
 
 hipError_t prepare_sample()                      // (asking loads the code)
 {
     hipFunction_t f;
-    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, 8>)).find(&f);
+    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, true, 8>)).find(&f);
 }
 
 }  // namespace dyspec
