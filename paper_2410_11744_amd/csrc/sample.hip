@@ -26,14 +26,14 @@
 
 namespace dyspec {
 
-constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / kWave;
+constexpr int kMostWaves = 16;
+constexpr int kHeldTokens = 32768;               // rows up to that are held in registers
 constexpr int kBins = 2048, kRanked = 1024;      // kRanked: tokens of a bin that are looked at one by one
 constexpr int kListMost = 4096;
 constexpr int kRankAll = 128;                    // of a list that short every token is, without a histogram
-constexpr int kHeldTokens = 32;                  // of a thread whose row is held
 constexpr int kWeightBits = 45;                  // the largest weight is 2^kWeightBits: 2^18 of them stay below 2^63
 static_assert(DYSPEC_MAX_SAMPLE_VOCAB <= 1 << (63 - kWeightBits), "sums fit");
-static_assert(kRowWaves == 16, "what the waves leave is gone through by a row of 16 lanes");
+static_assert(kMostWaves == 16, "what the waves leave is gone through by a row of 16 lanes");
 
 struct Token { float x; int i; };
 struct Ranked { float x; int i; u64 amount; };
@@ -41,15 +41,16 @@ struct Ranked { float x; int i; u64 amount; };
 struct SampleLds {
     u64 hist[kBins];
     Ranked ranked[kRanked];
-    u64 sums[kRowWaves];
-    float hi[kRowWaves], lo[kRowWaves];
-    int odd[kRowWaves], counts[kRowWaves], kept[kRowWaves];
+    u64 in_front[kRanked];                       // of a token in `ranked`: the amounts of those in front of it
+    u64 sums[kMostWaves];                        // (what a smaller workgroup has no wave for stays zero)
+    float hi[kMostWaves], lo[kMostWaves];
+    int odd[kMostWaves], counts[kMostWaves], kept[kMostWaves];
     u64 before;                                  // of a bin: the sum up to it
     u64 amount;                                  // of a token
     int found, n_ranked;
     Token cut;
+    Token list[kListMost];
 };
-struct ListLds { Token list[kListMost]; };
 
 template <typename T> struct RowPiece;           // 16 bytes of a row
 template <> struct RowPiece<float> {
@@ -60,6 +61,10 @@ template <> struct RowPiece<__bf16> {
     static constexpr int kTokens = 8;
     static __device__ __forceinline__ float value(const uint4& r, int e) { const uint32_t w = (&r.x)[e / 2]; return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16); }
 };
+
+// (without the moves that fmaxf and fminf make to quiet NaN)
+__device__ __forceinline__ float max3(float x, float y, float z) { asm("v_max3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z)); return x; }
+__device__ __forceinline__ float min3(float x, float y, float z) { asm("v_min3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z)); return x; }
 
 // (of 64 bits, as an operand that takes no vector registers)
 __device__ __forceinline__ double constant(double c) { asm("" : "+s"(c)); return c; }
@@ -96,8 +101,8 @@ __device__ __forceinline__ float of_ordered_bits(uint32_t key) { return __uint_a
 
 // A row as a thread has it.  Wave w has tokens w * span .. of the row, lane l of it the kTokens from w * span + (64 p + l) * kTokens
 // on, p < pieces.  Places past the row's end hold a NaN, which no comparison keeps.
-template <typename T, bool Held> struct Row {
-    static constexpr int VEC = RowPiece<T>::kTokens, NP = Held ? kHeldTokens / VEC : 1;
+template <typename T, bool Held, int NT> struct Row {
+    static constexpr int VEC = RowPiece<T>::kTokens, NP = Held ? kHeldTokens / NT / VEC : 1;
     const T* at;
     int V, pieces, first;                        // first: of this thread
     uint4 held[NP];
@@ -144,6 +149,7 @@ template <typename T, bool Held> struct Row {
                 int i = index(p);
                 asm volatile("" : "+v"(i));
                 if (p < pieces) f(held[p], i);
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
             constexpr int kAhead = 4;
@@ -270,8 +276,8 @@ __device__ __forceinline__ u64 block_upto(SampleLds& lds, u64 mine, u64* total)
 
 // The token at which the sum of amount(logit, index), in order of the indices, first exceeds target_of(total); there is one.  Its amount
 // is left in lds.amount.  By all threads; lds.sums is free before and after.
-template <typename T, bool Held, typename A, typename G>
-__device__ __forceinline__ int locate(const Row<T, Held>& row, SampleLds& lds, A&& amount, G&& target_of, u64* total)
+template <typename T, bool Held, int NT, typename A, typename G>
+__device__ __forceinline__ int locate(const Row<T, Held, NT>& row, SampleLds& lds, A&& amount, G&& target_of, u64* total)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     u64 s = 0;
@@ -282,11 +288,11 @@ __device__ __forceinline__ int locate(const Row<T, Held>& row, SampleLds& lds, A
     const u64 upto = row_upto(lds.sums[lane & 15]);
     *total = of_lane(upto, 15);
     const u64 target = target_of(*total);
-    const int owner = min(__builtin_popcountll(ballot(upto <= target) & 0xffffull), kRowWaves - 1);      // the first run that goes past the target
+    const int owner = min(__builtin_popcountll(ballot(upto <= target) & 0xffffull), NT / kWave - 1);      // the first run that goes past the target
     const u64 before = owner == 0 ? 0 : of_lane(upto, owner - 1);
     __syncthreads();
     // that run once more, shared out among all threads
-    const int each = (row.span() + kRowThreads - 1) / kRowThreads;
+    const int each = (row.span() + NT - 1) / NT;
     const int begin = owner * row.span() + tid * each, end = min(min(begin + each, (owner + 1) * row.span()), row.V);
     u64 mine = 0;
     for (int i = begin; i < end; ++i) mine += amount(logit_to_float(row.at[i]), i);
@@ -319,11 +325,12 @@ __device__ __forceinline__ int locate(const List& list, SampleLds& lds, A&& amou
     return uniform(lds.found);
 }
 
-// The histogram's bin, from bin 0 on, with which the sum first reaches what target_of(total) says.  lds.before: the sum before it.
-template <typename G>
+// The histogram's bin, from bin 0 on, with which the sum first reaches what target_of(total) says (the last one, where that is not
+// reached).  lds.before: the sum before it.
+template <int NT, typename G>
 __device__ __forceinline__ int reach(SampleLds& lds, G&& target_of, u64* target)
 {
-    constexpr int PER = kBins / kRowThreads;
+    constexpr int PER = kBins / NT;
     u64 h[PER], s = 0;
 #pragma unroll
     for (int y = 0; y < PER; ++y) s += h[y] = lds.hist[PER * threadIdx.x + y];
@@ -336,33 +343,50 @@ __device__ __forceinline__ int reach(SampleLds& lds, G&& target_of, u64* target)
             at += h[y];
         }
     }
+    if (total < *target && threadIdx.x == NT - 1) { lds.found = kBins - 1; lds.before = total - h[PER - 1]; }      // (the last bin is not filled whole)
     __syncthreads();
     return uniform(lds.found);
 }
-__device__ __forceinline__ void clear_bins(SampleLds& lds)     // (a barrier follows)
+template <int NT> __device__ __forceinline__ void clear_bins(SampleLds& lds)     // (a barrier follows)
 {
 #pragma unroll
-    for (int y = 0; y < kBins / kRowThreads; ++y) lds.hist[y * kRowThreads + threadIdx.x] = 0;
+    for (int y = 0; y < kBins / NT; ++y) lds.hist[y * NT + threadIdx.x] = 0;
     if (threadIdx.x == 0) lds.n_ranked = 0;
 }
 
-// Of the n tokens in lds.ranked: the one with which `before` and the amounts of those in front of it first reach the target.
-__device__ __forceinline__ Cut rank(SampleLds& lds, int n, u64 before, u64 target)
+// Of the n tokens in lds.ranked, their amounts to be filled in: the one with which `before` and the amounts of those in front of it first
+// reach the target.  A lane has a token, the waves share out those that it is compared with.
+template <int NT, typename A>
+__device__ __forceinline__ Cut rank(SampleLds& lds, int n, u64 before, u64 target, A&& amount)
 {
-    if ((int)threadIdx.x < n) {
-        const Ranked me = lds.ranked[threadIdx.x];
-        u64 at = before;
+    constexpr int NW = NT / kWave;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    for (int y = threadIdx.x; y < n; y += NT) {
+        lds.ranked[y].amount = amount(lds.ranked[y].x, lds.ranked[y].i);
+        lds.in_front[y] = 0;
+    }
+    __syncthreads();
+    const int share = (n + NW - 1) / NW, from = wave * share, to = min(from + share, n);
+#pragma unroll 1
+    for (int c = 0; c < n; c += kWave) {
+        const Ranked me = lds.ranked[min(c + lane, n - 1)];
+        u64 front = 0;
         constexpr int kAhead = 4;                                  // (a read of LDS takes longer than looking at what came)
 #pragma unroll 1
-        for (int y0 = 0; y0 < n; y0 += kAhead) {
+        for (int y0 = from; y0 < to; y0 += kAhead) {
             Ranked l[kAhead];
 #pragma unroll
-            for (int y = 0; y < kAhead; ++y) l[y] = lds.ranked[min(y0 + y, kRanked - 1)];
+            for (int y = 0; y < kAhead; ++y) l[y] = lds.ranked[min(y0 + y, n - 1)];
 #pragma unroll
             for (int y = 0; y < kAhead; ++y)
-                at += (y0 + y < n) & ((l[y].x > me.x) | ((l[y].x == me.x) & (l[y].i < me.i))) ? l[y].amount : 0;
+                front += (y0 + y < to) & ((l[y].x > me.x) | ((l[y].x == me.x) & (l[y].i < me.i))) ? l[y].amount : 0;
         }
-        if (at < target && target <= at + me.amount) lds.cut = Token{ me.x, me.i };
+        if (front != 0 && c + lane < n) atomicAdd(&lds.in_front[c + lane], front);
+    }
+    __syncthreads();
+    for (int y = threadIdx.x; y < n; y += NT) {
+        const u64 at = before + lds.in_front[y];
+        if (at < target && target <= at + lds.ranked[y].amount) lds.cut = Token{ lds.ranked[y].x, lds.ranked[y].i };
     }
     __syncthreads();
     return Cut{ uniform(lds.cut.x), uniform(lds.cut.i) };
@@ -370,8 +394,8 @@ __device__ __forceinline__ Cut rank(SampleLds& lds, int n, u64 before, u64 targe
 
 // The cut inside a bin: where, with `before` before the bin, the sum of the amounts of its tokens first reaches the target.  src: the row
 // or the list, of which `cut` says what counts.
-template <typename T, bool Held, typename Src, typename A>
-__device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, SampleLds& lds, const Cut& cut, const Bins& bins, int bin, u64 before, u64 target, A&& amount)
+template <typename T, bool Held, int NT, typename Src, typename A>
+__device__ __forceinline__ Cut resolve(const Row<T, Held, NT>& row, const Src& src, SampleLds& lds, const Cut& cut, const Bins& bins, int bin, u64 before, u64 target, A&& amount)
 {
     const float least = bins.least(bin), most = bins.most(bin);
     src.each([&](float x, int i) __attribute__((always_inline)) {
@@ -384,11 +408,7 @@ __device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, 
     });
     __syncthreads();
     const int n = uniform(lds.n_ranked);
-    if (n <= kRanked) {
-        if ((int)threadIdx.x < n) lds.ranked[threadIdx.x].amount = amount(lds.ranked[threadIdx.x].x);
-        __syncthreads();
-        return rank(lds, n, before, target);
-    }
+    if (n <= kRanked) return rank<NT>(lds, n, before, target, [=](float x, int) { return amount(x); });
     // too many: by the bits of the logits, eleven at a time, from the highest value down
     __syncthreads();                                               // (all have seen n)
     uint32_t known = 0u;                                           // the bits so far
@@ -396,7 +416,7 @@ __device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, 
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
         const uint32_t digits = pass == 2 ? 1023u : 2047u, high = pass == 0 ? 0u : pass == 1 ? 0xffe00000u : 0xfffffc00u;
-        clear_bins(lds);
+        clear_bins<NT>(lds);
         __syncthreads();
         src.each([&](float x, int i) __attribute__((always_inline)) {
             const uint32_t key = ordered_bits(x);
@@ -405,7 +425,7 @@ __device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, 
         __syncthreads();
         u64 unused;
         const u64 rest = target - before;
-        const int digit = reach(lds, [=](u64) { return rest; }, &unused);
+        const int digit = reach<NT>(lds, [=](u64) { return rest; }, &unused);
         known |= (digits - (uint32_t)digit) << shift;
         before += uniform(lds.before);
         __syncthreads();
@@ -418,8 +438,8 @@ __device__ __forceinline__ Cut resolve(const Row<T, Held>& row, const Src& src, 
 }
 
 // The tokens with a logit of `least` or more, in order of their indices, if they are kListMost or fewer.
-template <typename T, bool Held>
-__device__ __forceinline__ bool make_list(const Row<T, Held>& row, SampleLds& lds, Token* to, float least, List& list)
+template <typename T, bool Held, int NT>
+__device__ __forceinline__ bool make_list(const Row<T, Held, NT>& row, SampleLds& lds, float least, List& list)
 {
     constexpr int VEC = RowPiece<T>::kTokens;
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -429,54 +449,78 @@ __device__ __forceinline__ bool make_list(const Row<T, Held>& row, SampleLds& ld
     __syncthreads();
     int at = before_wave(lds.counts, wave, &list.n);
     __syncthreads();
-    list.at = to;
-    list.each_n = (list.n + kRowThreads - 1) / kRowThreads;
+    list.at = lds.list;
+    list.each_n = (list.n + NT - 1) / NT;
     if (list.n > kListMost) return false;
     row.each_piece([&](const uint4& r, int i) __attribute__((always_inline)) {
-        u64 there[VEC], any = 0;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) any |= there[e] = ballot(RowPiece<T>::value(r, e) >= least);
-        if (any == 0) return;                                      // (the same for the wave)
+        // (before this piece's tokens of this lane: those of earlier pieces, those of lower lanes)
         int place = at;
+        u64 any = 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            place += __builtin_amdgcn_mbcnt_hi((uint32_t)(there[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there[e], 0));
-            at += __builtin_popcountll(there[e]);
+            float x = RowPiece<T>::value(r, e);
+            asm volatile("" : "+v"(x));
+            const u64 there = ballot(x >= least);
+            any |= there;
+            place = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, (uint32_t)place));
+            at += __builtin_popcountll(there);
         }
+        if (any != 0) {                                            // (the same for the wave)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if ((there[e] >> lane) & 1ull) to[place++] = Token{ RowPiece<T>::value(r, e), i + e };
+            for (int e = 0; e < VEC; ++e) {
+                float x = RowPiece<T>::value(r, e);
+                asm volatile("" : "+v"(x));
+                if (x >= least) lds.list[place++] = Token{ x, i + e };
+            }
+        }
     });
     __syncthreads();
     return true;
 }
 
 // Drawn: a token is drawn; else the filtered logits are written.
-template <typename T, bool Held, bool Drawn, int S>
-__global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
+template <typename T, bool Held, bool Drawn, int NT, int S>
+__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs<S>)
 {
     const SampleArgs<S>& a = *(const SampleArgs<S>*)(__attribute__((address_space(4))) const SampleArgs<S>*)__builtin_amdgcn_kernarg_segment_ptr();
     __shared__ SampleLds lds;
     constexpr int VEC = RowPiece<T>::kTokens;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int r = blockIdx.x;
-    Row<T, Held> row;
+    Row<T, Held, NT> row;
     row.at = static_cast<const T*>(a.logits) + r * a.stride;
     row.V = a.V;
-    row.pieces = (a.V + kRowThreads * VEC - 1) / (kRowThreads * VEC);
+    row.pieces = (a.V + NT * VEC - 1) / (NT * VEC);
     row.first = wave * row.span() + lane * VEC;
     row.load();
     const int seq = __builtin_popcountll(ballot(lane < a.n_seq && r >= a.row0[lane < a.n_seq ? lane : 0])) - 1;
     const Filter filter = a.filter[seq];
-    clear_bins(lds);
+    clear_bins<NT>(lds);
+    if (NT / kWave < kMostWaves && tid >= NT / kWave && tid < kMostWaves) {      // what is left for waves that are not there
+        lds.sums[tid] = 0;
+        lds.counts[tid] = lds.kept[tid] = lds.odd[tid] = 0;
+        lds.hi[tid] = -INFINITY; lds.lo[tid] = INFINITY;
+    }
     // ---- the largest logit and the smallest; a row with a NaN or +inf, or without a finite logit, has no distribution
     float hi = -INFINITY, lo = INFINITY;
     bool odd = false;
-    row.each([&](float x, int i) __attribute__((always_inline)) {
-        odd |= (x != x) & (i < a.V);
-        hi = fmaxf(hi, x);
-        lo = fminf(lo, x);
+    row.each_piece([&](const uint4& p, int i) __attribute__((always_inline)) {
+        bool nan = false;
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) {
+            const float x = RowPiece<T>::value(p, e), y = RowPiece<T>::value(p, e + 1);
+            nan |= (x != x) | (y != y);
+            hi = max3(hi, x, y);
+            lo = min3(lo, x, y);
+        }
+        if (i + VEC <= a.V) odd |= nan;
+        else
+            for (int e = 0; e < VEC && i + e < a.V; ++e) {
+                const float x = logit_to_float(row.at[i + e]);
+                odd |= x != x;
+            }
     });
+    const float mine_hi = hi;                                      // of this thread's tokens
     hi = wave_max_dpp(hi);
     lo = -wave_max_dpp(-lo);
     const bool any_odd = ballot(odd) != 0;
@@ -490,11 +534,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
     List list;
     list.n = 0;
     bool listed = false;                                           // the list holds every token that is kept
-    Token* list_lds = nullptr;
-    if constexpr (Drawn) {
-        __shared__ ListLds room;
-        list_lds = room.list;
-    }
     const double per_nat = uniform(1.4426950408889634074 / (double)filter.temperature), top64 = uniform((double)top);
     auto weight = [=](float x) __attribute__((always_inline)) -> u64 { return weight_of(((double)x - top64) * per_nat); };
     if (none) {
@@ -507,7 +546,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
         if (lane == 0) lds.counts[wave] = first;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kRowWaves; ++w) first = min(first, lds.counts[w]);
+        for (int w = 0; w < NT / kWave; ++w) first = min(first, lds.counts[w]);
         cut = Cut{ top, uniform(first) };
     } else {
         bool cleared = true;
@@ -517,34 +556,46 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
             auto amount = [=](float x) __attribute__((always_inline)) -> u64 { return by_weight ? weight(x) : 1; };
             // (top-p keeps what has less than its share of the sum before it)
             auto target_of = [=](u64 total) -> u64 { return by_weight ? max((u64)1, (u64)ceil((double)filter.top_p * (double)total)) : (u64)filter.top_k; };
-            if (Drawn && listed && list.n <= kRankAll) {           // (a token a thread)
-                const Token k = list.at[tid];
+            const Bins bins(top, fminf(top - lo, by_weight ? 32.0f * filter.temperature : 64.0f));
+            if (!by_weight && filter.top_k <= NT) {
+                // As many threads as tokens are wanted have a token that is as large as the top_k-th of the threads' largest: the
+                // wanted ones are among the tokens that are that large.
+                if (mine_hi > -INFINITY) atomicAdd(&lds.hist[bins.of(mine_hi)], (u64)1);
+                __syncthreads();
+                u64 target;
+                const int bin = reach<NT>(lds, target_of, &target);
+                listed = make_list(row, lds, bins.least(bin), list);
+                clear_bins<NT>(lds);
+                __syncthreads();
+            }
+            if (listed && list.n <= kRankAll) {                    // (a token a thread)
+                const Token k = list.at[min(tid, kListMost - 1)];
                 const u64 mine = tid < list.n && cut.keeps(k.x, k.i) ? amount(k.x) : 0;
                 u64 total;
                 block_upto(lds, mine, &total);
-                if (tid < list.n) lds.ranked[tid] = Ranked{ k.x, k.i, mine };
+                if (tid < list.n) { lds.ranked[tid].x = k.x; lds.ranked[tid].i = k.i; }
                 __syncthreads();
-                cut = rank(lds, list.n, 0, target_of(total));
+                cut = rank<NT>(lds, list.n, 0, target_of(total), [=](float x, int i) -> u64 { return cut.keeps(x, i) ? amount(x) : 0; });
                 continue;
             }
-            const Bins bins(top, fminf(top - lo, by_weight ? 32.0f * filter.temperature : 64.0f));
-            const bool whole = cut.x == -INFINITY && cut.i >= a.V;
+            const bool whole = !listed && cut.x == -INFINITY && cut.i >= a.V;
             if (!cleared) {
-                clear_bins(lds);
+                clear_bins<NT>(lds);
                 __syncthreads();
             }
             cleared = false;
-            auto add = [&](float x, u64 n) __attribute__((always_inline)) { atomicAdd(&lds.hist[bins.of(x)], n); };
-            if (Drawn && listed) list.each([&](float x, int i) __attribute__((always_inline)) { if (cut.keeps(x, i)) add(x, amount(x)); });
-            else if (!whole) row.each([&](float x, int i) __attribute__((always_inline)) { if (cut.keeps(x, i)) add(x, weight(x)); });      // (top-k was first)
+            // (what weighs nothing, or is masked, is most of some rows and would meet in the last bin: it is added to a bin of the thread's)
+            auto add = [&](float x, u64 n) __attribute__((always_inline)) { atomicAdd(&lds.hist[n != 0 ? bins.of(x) : tid], n); };
+            if (listed) list.each([&](float x, int i) __attribute__((always_inline)) { add(x, cut.keeps(x, i) ? amount(x) : 0); });
+            else if (!whole) row.each([&](float x, int i) __attribute__((always_inline)) { add(x, cut.keeps(x, i) ? weight(x) : 0); });      // (top-k was first)
             else if (by_weight) row.each([&](float x, int) __attribute__((always_inline)) { add(x, weight(x)); });
-            else row.each([&](float x, int) __attribute__((always_inline)) { add(x, 1); });
+            else row.each([&](float x, int) __attribute__((always_inline)) { add(x, top - x < 65.0f); });
             __syncthreads();
             u64 target;
-            const int bin = reach(lds, target_of, &target);
+            const int bin = reach<NT>(lds, target_of, &target);
             const u64 before = uniform(lds.before);
-            if (Drawn && whole) listed = make_list(row, lds, list_lds, bins.least(bin), list);
-            if (Drawn && listed) cut = resolve(row, list, lds, cut, bins, bin, before, target, amount);
+            if (Drawn && whole) listed = make_list(row, lds, bins.least(bin), list);
+            if (listed) cut = resolve(row, list, lds, cut, bins, bin, before, target, amount);
             else cut = resolve(row, row, lds, cut, bins, bin, before, target, amount);
         }
         if (filter.min_p > 0.0f) {
@@ -565,11 +616,13 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
         T* const out = static_cast<T*>(a.out) + r * a.out_stride;
         constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80u;      // -inf
         __syncthreads();                                           // (in place: every thread has read what it wants of others)
-        row.each_piece([&](const uint4& in, int i) __attribute__((always_inline)) {
+        auto leave = [&](const uint4& in, int i, auto ties_c) __attribute__((always_inline)) {
+            constexpr bool ties = decltype(ties_c)::value;         // some of the equal ones at the cut go
             uint4 w = in;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const bool keep = cut.keeps(RowPiece<T>::value(in, e), i + e);
+                const float x = RowPiece<T>::value(in, e);
+                const bool keep = ties ? cut.keeps(x, i + e) : x >= cut.x;
                 if constexpr (sizeof(T) == 4) (&w.x)[e] = keep ? (&w.x)[e] : kNone;
                 else if (!keep) (&w.x)[e / 2] = (e & 1) ? ((&w.x)[e / 2] & 0xffffu) | kNone << 16 : ((&w.x)[e / 2] & 0xffff0000u) | kNone;
             }
@@ -582,14 +635,16 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
                     else out[i + e] = __builtin_bit_cast(__bf16, (unsigned short)((&w.x)[e / 2] >> (16 * (e & 1))));
                 }
             }
-        });
+        };
+        if (cut.i >= a.V) row.each_piece([&](const uint4& in, int i) __attribute__((always_inline)) { leave(in, i, std::false_type{}); });
+        else row.each_piece([&](const uint4& in, int i) __attribute__((always_inline)) { leave(in, i, std::true_type{}); });
     } else {
         if (none || greedy) {
             if (tid == 0) { a.token[r] = none ? -1 : cut.i; a.prob[r] = none ? 0.0f : 1.0f; a.n_kept[r] = none ? 0 : 1; }
             return;
         }
         const bool whole = cut.x == -INFINITY && cut.i >= a.V;     // every token is kept
-        if (!listed && cut.x > -INFINITY) listed = make_list(row, lds, list_lds, cut.x, list);
+        if (!listed && cut.x > -INFINITY) listed = make_list(row, lds, cut.x, list);
         const double u = (double)fminf(fmaxf(a.uniform[r], 0.0f), 1.0f - 0x1p-24f);
         auto kept_weight = [=](float x, int i) __attribute__((always_inline)) -> u64 { return cut.keeps(x, i) ? weight(x) : 0; };
         auto target_of = [=](u64 total) -> u64 { return (u64)(u * (double)total); };
@@ -613,25 +668,26 @@ __global__ __launch_bounds__(kRowThreads) void sample_kernel(SampleArgs<S>)
     }
 }
 
-template <typename T, bool Held, bool Drawn, int S>
+template <typename T, bool Held, bool Drawn, int NT, int S>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, Drawn, S>));
+    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, Drawn, NT, S>));
     SampleArgs<S> a;
     static_cast<SampleHead&>(a) = head;
     for (int s = 0; s < head.n_seq; ++s) { a.row0[s] = row0[s]; a.filter[s] = filter[s]; }
-    return kernel.launch(dim3(head.rows), kRowThreads, 0, stream, a);
+    return kernel.launch(dim3(head.rows), NT, 0, stream, a);
 }
 template <typename T, bool Held, bool Drawn>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    return head.n_seq <= 8 ? launch_rows<T, Held, Drawn, 8>(head, row0, filter, stream) : launch_rows<T, Held, Drawn, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
+    constexpr int NT = 1024;
+    return head.n_seq <= 8 ? launch_rows<T, Held, Drawn, NT, 8>(head, row0, filter, stream) : launch_rows<T, Held, Drawn, NT, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
 }
 template <typename T>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
     const bool drawn = head.out == nullptr;
-    if (head.V <= kHeldTokens * kRowThreads)
+    if (head.V <= kHeldTokens)
         return drawn ? launch_rows<T, true, true>(head, row0, filter, stream) : launch_rows<T, true, false>(head, row0, filter, stream);
     return drawn ? launch_rows<T, false, true>(head, row0, filter, stream) : launch_rows<T, false, false>(head, row0, filter, stream);
 }
@@ -645,7 +701,7 @@ hipError_t launch_sample(const SampleHead& a, const int* row0, const Filter* fil
 hipError_t prepare_sample()                      // (asking loads the code)
 {
     hipFunction_t f;
-    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, true, 8>)).find(&f);
+    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, true, 1024, 8>)).find(&f);
 }
 
 }  // namespace dyspec
