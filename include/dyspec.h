@@ -521,10 +521,12 @@ dyspec_status dyspec_prompt_attn_scored(const void* q, int64_t q_stride, const v
  *               after ring[n_pages - 1].  A full pool has state {0, n_pages, 0, 0} and every page's number in the ring
  *   page_table  DEVICE, rows table_stride apart, as dyspec_paged_kv's; entries that no place reaches are not touched
  *   held, wanted DEVICE [n_seq] i32
- *   granted     DEVICE [n_seq] i32, none of held and wanted: it can be the next call's held
+ *   granted     DEVICE [n_seq] i32, none of the lengths given: it can be the next call's held
  *   slots       DEVICE [n_slots] i64 or NULL, 8-byte aligned: where new tokens go, packed by sequences: for tokens
- *               held[s] .. wanted[s] - 1 the row of the pool (page * page_size + row), -1 for all of a sequence whose
- *               demand is not met.  What does not fit is left out, what is behind the last one stays as it is
+ *               slots_from[s] .. wanted[s] - 1 the row of the pool (page * page_size + row), -1 for all of a sequence
+ *               whose demand is not met.  What does not fit is left out, what is behind the last one stays as it is
+ *   slots_from  DEVICE [n_seq] i32 (negative ones count as 0), or NULL: held.  (After a draft tree a sequence holds
+ *               pages for more tokens than its context has: its new ones begin behind the context)
  *   n_seq       1 .. DYSPEC_MAX_SEQ
  * Calls on one pool must be ordered (a stream does that).  No workspace; the other arrays 4-byte aligned.
  */
@@ -536,7 +538,7 @@ typedef struct {
 } dyspec_page_pool;
 dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table, int32_t max_pages, int32_t table_stride,
                                const int32_t* held, const int32_t* wanted, int32_t n_seq, int32_t* granted,
-                               int64_t* slots, int64_t n_slots, void* hip_stream);
+                               int64_t* slots, int64_t n_slots, const int32_t* slots_from, void* hip_stream);
 
 /*
  * dyspec_sample -- a token a row, drawn from what temperature, top-k, top-p and min-p leave of it, by given random

@@ -131,7 +131,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.dyspec_prompt_attn_scored.restype = I32
     lib.dyspec_prompt_attn_scored.argtypes = [V, I64, V, I64, V, I64, PB, I32, I32, I32, I32, F, PS, V, V]
     lib.dyspec_page_plan.restype = I32
-    lib.dyspec_page_plan.argtypes = [ctypes.POINTER(_PagePool), V, I32, I32, V, V, I32, V, V, I64, V]
+    lib.dyspec_page_plan.argtypes = [ctypes.POINTER(_PagePool), V, I32, I32, V, V, I32, V, V, I64, V, V]
     lib.dyspec_sample.restype = I32
     lib.dyspec_sample.argtypes = [V, I32, I32, I64, PB, V, V, V, V, V, V, V, V, V]
     lib.dyspec_filter_logits.restype = I32
@@ -997,23 +997,23 @@ class PagePool:
         return PagePool(ring, torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=ring.device), page_size)
 
 
-def page_plan(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None):
+def page_plan(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None, slots_from=None):
     """dyspec_page_plan: every sequence gets pages for wanted[s] tokens in place of held[s], from the pool or back to it; returns
     granted [n_seq], the tokens that it now has pages for (held[s] where the pool was short, -1 for lengths that cannot be).
     page_table: int32 [n_seq or more, max_pages], a PagedCache's; held, wanted: int32 [n_seq]; slots: int64 [any], where the new
-    tokens' rows of the pool are noted, packed by sequences."""
-    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream)
+    tokens' rows of the pool are noted, packed by sequences: of tokens slots_from[s] (int32 [n_seq]; None: held[s]) to wanted[s] - 1."""
+    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream, slots_from)
     _issue(_lib.dyspec_page_plan, args, pool._device, "dyspec_page_plan")
     return granted
 
 
-def page_plan_call(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None) -> PreparedCall:
+def page_plan_call(pool: PagePool, page_table, held, wanted, slots=None, granted=None, stream=None, slots_from=None) -> PreparedCall:
     """page_plan's call, prepared: nothing is launched until the returned object is called."""
-    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream)
-    return DeviceCall(_lib.dyspec_page_plan, args, (pool, page_table, held, wanted, slots, granted), "dyspec_page_plan", granted, pool._device)
+    args, granted = _plan_args(pool, page_table, held, wanted, slots, granted, stream, slots_from)
+    return DeviceCall(_lib.dyspec_page_plan, args, (pool, page_table, held, wanted, slots, granted, slots_from), "dyspec_page_plan", granted, pool._device)
 
 
-def _plan_args(pool, page_table, held, wanted, slots, granted, stream):
+def _plan_args(pool, page_table, held, wanted, slots, granted, stream, slots_from):
     if _lib is None:
         load_library()
     torch = _torch
@@ -1021,6 +1021,7 @@ def _plan_args(pool, page_table, held, wanted, slots, granted, stream):
     if len(rows) != 2 or rows[0] < n_seq or page_table.dtype is not torch.int32 or page_table.get_device() != device or (rows[1] > 1 and page_table.stride(1) != 1):
         raise ValueError("page_table: int32 [n_seq or more, max_pages] on the pool's device expected")
     hp, wp = _dense(held, (n_seq,), torch.int32, device, "held"), _dense(wanted, (n_seq,), torch.int32, device, "wanted")
+    fp = 0 if slots_from is None else _dense(slots_from, (n_seq,), torch.int32, device, "slots_from")
     sp = n_slots = 0
     if slots is not None:
         n_slots = slots.numel()
@@ -1033,8 +1034,8 @@ def _plan_args(pool, page_table, held, wanted, slots, granted, stream):
     else:
         gp = _dense(granted, (n_seq,), torch.int32, device, "granted")
     if stream is not None:
-        _hand_over(stream, pool.ring, pool.state, page_table, held, wanted, slots, granted)
-    return (pool._ref, page_table.data_ptr(), rows[1], page_table.stride(0) if rows[0] > 1 else rows[1], hp, wp, n_seq, gp, sp, n_slots, raw), granted
+        _hand_over(stream, pool.ring, pool.state, page_table, held, wanted, slots, granted, slots_from)
+    return (pool._ref, page_table.data_ptr(), rows[1], page_table.stride(0) if rows[0] > 1 else rows[1], hp, wp, n_seq, gp, sp, n_slots, fp, raw), granted
 
 
 # ---------------------------------------------------------------------------------------- filtered logits and drawn tokens

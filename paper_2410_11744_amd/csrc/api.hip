@@ -1,6 +1,7 @@
 // extern "C" boundary: host-side validation, then kernel launches.  See include/dyspec.h
 // for the contract of every entry point.
 #include <atomic>
+#include <cmath>
 
 #include "attend.h"
 #include "kv_cache.h"
@@ -734,19 +735,21 @@ static bool overlap(const void* p, size_t n, const void* q, size_t m)
 }
 
 dyspec_status dyspec_page_plan(const dyspec_page_pool* pool, int32_t* page_table, int32_t max_pages, int32_t table_stride, const int32_t* held,
-                               const int32_t* wanted, int32_t n_seq, int32_t* granted, int64_t* slots, int64_t n_slots, void* hip_stream)
+                               const int32_t* wanted, int32_t n_seq, int32_t* granted, int64_t* slots, int64_t n_slots, const int32_t* slots_from,
+                               void* hip_stream)
 {
     if (!pool || !pool->ring || !pool->state || !page_table || !held || !wanted || !granted) return DYSPEC_BAD_ARG;
     if (!aligned(pool->ring, 4) || !aligned(pool->state, 4) || !aligned(page_table, 4) || !aligned(held, 4) || !aligned(wanted, 4) || !aligned(granted, 4) ||
-        !aligned(slots, 8) || (n_slots > 0 && !slots))
+        !aligned(slots, 8) || !aligned(slots_from, 4) || (n_slots > 0 && !slots))
         return DYSPEC_BAD_ARG;
     if (pool->page_size < 8 || pool->page_size > 65536 || (pool->page_size & (pool->page_size - 1))) return DYSPEC_UNSUPPORTED;
     if (n_seq < 1 || n_seq > DYSPEC_MAX_SEQ || pool->n_pages < 1 || max_pages < 0 || table_stride < max_pages || n_slots < 0) return DYSPEC_BAD_SHAPE;
     // (workgroups of other sequences read the lengths while these are written)
     const size_t bytes = 4 * (size_t)n_seq;
-    if (overlap(granted, bytes, held, bytes) || overlap(granted, bytes, wanted, bytes)) return DYSPEC_BAD_ARG;
+    if (overlap(granted, bytes, held, bytes) || overlap(granted, bytes, wanted, bytes) || (slots_from && overlap(granted, bytes, slots_from, bytes)))
+        return DYSPEC_BAD_ARG;
     PlanArgs a;
-    a.ring = pool->ring; a.state = pool->state; a.table = page_table; a.granted = granted; a.held = held; a.wanted = wanted;
+    a.ring = pool->ring; a.state = pool->state; a.table = page_table; a.granted = granted; a.held = held; a.wanted = wanted; a.slots_from = slots_from;
     a.slots = reinterpret_cast<long long*>(slots); a.n_slots = n_slots;
     a.n_pages = pool->n_pages; a.page_shift = log2_of(pool->page_size); a.max_pages = max_pages; a.table_stride = table_stride; a.n_seq = n_seq;
     return launch_page_plan(a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? DYSPEC_OK : DYSPEC_HIP_ERROR;
@@ -765,10 +768,12 @@ static dyspec_status check_filters(const dyspec_batch* b, const float* temperatu
     for (int s = 0; s < b->n_seq; ++s) {
         if (b->node_offset[s + 1] < b->node_offset[s]) return DYSPEC_BAD_SHAPE;
         row0[s] = b->node_offset[s];
-        filter[s] = Filter{ temperature[s], top_p ? top_p[s] : 1.0f, min_p ? min_p[s] : 0.0f, top_k ? top_k[s] : 0 };
-        const Filter& f = filter[s];
+        filter[s] = Filter{ temperature[s], top_p ? top_p[s] : 1.0f, min_p ? min_p[s] : 0.0f, top_k ? top_k[s] : 0, 0.0, 0.0 };
+        Filter& f = filter[s];
         if (!(f.temperature >= 0.0f) || f.temperature > 3.402823466e38f || !(f.top_p > 0.0f) || f.top_p > 1.0f || !(f.min_p >= 0.0f) || f.min_p > 1.0f || f.top_k < 0)
             return DYSPEC_BAD_ARG;
+        if (f.temperature > 0.0f) f.per_nat = 1.4426950408889634074 / (double)f.temperature;
+        if (f.min_p > 0.0f) f.least = std::log2((double)f.min_p);
     }
     *rows = b->node_offset[b->n_seq];
     return *rows <= kMostSampleRows ? DYSPEC_OK : DYSPEC_BAD_SHAPE;

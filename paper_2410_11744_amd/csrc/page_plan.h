@@ -6,7 +6,7 @@ namespace dyspec {
 
 struct PlanArgs {
     int *ring, *state, *table, *granted;
-    const int *held, *wanted;
+    const int *held, *wanted, *slots_from;       // slots_from: or nullptr
     long long* slots;                            // or nullptr
     long long n_slots;
     int n_pages, page_shift, max_pages, table_stride, n_seq;

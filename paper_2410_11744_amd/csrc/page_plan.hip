@@ -41,14 +41,15 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
     // ---- every sequence's lengths, a lane each
     const bool there = lane < a.n_seq;
     const int x = there ? a.held[lane] : 0, y = there ? a.wanted[lane] : 0;
+    const int z = a.slots_from ? (there ? max(a.slots_from[lane], 0) : 0) : x;      // first token that gets a slot
     const unsigned head = (unsigned)a.state[0] % n_pages;
     const long long count = min(max(a.state[1], 0), a.n_pages);
     const int page = 1 << a.page_shift;
     const bool sized = x >= 0 && y >= 0 && x <= DYSPEC_MAX_CONTEXT && y <= DYSPEC_MAX_CONTEXT;
     const int A = sized ? (x + page - 1) >> a.page_shift : 0, B = sized ? (y + page - 1) >> a.page_shift : 0;
     const bool right = sized && A <= a.max_pages && B <= a.max_pages;
-    const long long need = right ? max(B - A, 0) : 0, back = right ? max(A - B, 0) : 0, grows = right ? max(y - x, 0) : 0;
-    const long long need_upto = upto_lane(need, lane), back_upto = upto_lane(back, lane), grows_upto = upto_lane(grows, lane);
+    const long long need = right ? max(B - A, 0) : 0, back = right ? max(A - B, 0) : 0, marked = right ? max(y - z, 0) : 0;
+    const long long need_upto = upto_lane(need, lane), back_upto = upto_lane(back, lane), marked_upto = upto_lane(marked, lane);
     const bool fits = need_upto <= count;
     // what is taken in all: demands come in order, so it is the last sum that fits
     const unsigned long long fitting = __builtin_amdgcn_ballot_w64(fits);
@@ -61,8 +62,8 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
     const bool granted = before >= after || ((fitting >> s) & 1ull);
     int* const table = a.table + (long long)s * a.table_stride;
     const int first = blockIdx.y * kPlanThreads + (int)threadIdx.x, step = gridDim.y * kPlanThreads;
-    const unsigned from = (unsigned)((head + (unsigned long long)(granted ? of_lane(need_upto - need, s) : 0)) % n_pages);      // column `before`
-    auto fresh = [&](int column) { return a.ring[(unsigned)(((unsigned long long)from + (unsigned)(column - before)) % n_pages)]; };
+    const unsigned next = (unsigned)((head + (unsigned long long)(granted ? of_lane(need_upto - need, s) : 0)) % n_pages);      // column `before`
+    auto fresh = [&](int column) { return a.ring[(unsigned)(((unsigned long long)next + (unsigned)(column - before)) % n_pages)]; };
     if (ok && granted)
         for (int c = before + first; c < after; c += step) table[c] = fresh(c);
     if (ok && before > after) {
@@ -75,9 +76,10 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
         }
     }
     if (a.slots && ok) {
-        const long long at = of_lane(grows_upto - grows, s);
-        for (int t = first; t < wanted - held && at + t < a.n_slots; t += step) {
-            const int place = held + t, column = place >> a.page_shift;
+        const long long at = of_lane(marked_upto - marked, s);
+        const int from = __builtin_amdgcn_readlane(z, s);
+        for (int t = first; t < wanted - from && at + t < a.n_slots; t += step) {
+            const int place = from + t, column = place >> a.page_shift;
             const int p = !granted ? -1 : column < before ? table[column] : fresh(column);
             a.slots[at + t] = p < 0 ? -1 : ((long long)p << a.page_shift) + (place & (page - 1));
         }

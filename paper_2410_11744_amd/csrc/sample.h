@@ -5,7 +5,11 @@
 namespace dyspec {
 
 // Settings of a sequence's rows.
-struct Filter { float temperature, top_p, min_p; int top_k; };     // top_k 0, top_p 1, min_p 0: no such filter
+struct Filter {                                  // top_k 0, top_p 1, min_p 0: no such filter
+    float temperature, top_p, min_p;
+    int top_k;
+    double per_nat, least;                       // log2(e) / temperature, log2(min_p)
+};
 
 struct SampleHead {
     const void* logits;

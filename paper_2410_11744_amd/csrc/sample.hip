@@ -480,7 +480,7 @@ __device__ __forceinline__ bool make_list(const Row<T, Held, NT>& row, SampleLds
 
 // Drawn: a token is drawn; else the filtered logits are written.
 template <typename T, bool Held, bool Drawn, int NT, int S>
-__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs<S>)
+__global__ __launch_bounds__(NT, !Drawn && sizeof(T) == 2 ? 8 : 4) void sample_kernel(SampleArgs<S>)
 {
     const SampleArgs<S>& a = *(const SampleArgs<S>*)(__attribute__((address_space(4))) const SampleArgs<S>*)__builtin_amdgcn_kernarg_segment_ptr();
     __shared__ SampleLds lds;
@@ -534,7 +534,7 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs<S>)
     List list;
     list.n = 0;
     bool listed = false;                                           // the list holds every token that is kept
-    const double per_nat = uniform(1.4426950408889634074 / (double)filter.temperature), top64 = uniform((double)top);
+    const double per_nat = filter.per_nat, top64 = uniform((double)top);
     auto weight = [=](float x) __attribute__((always_inline)) -> u64 { return weight_of(((double)x - top64) * per_nat); };
     if (none) {
         cut = Cut{ INFINITY, -1 };
@@ -600,13 +600,13 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs<S>)
         }
         if (filter.min_p > 0.0f) {
             // the smallest logit whose weight, as a number of 64 bits, is min_p or more (those within 2^-54 of 1 are 1)
-            const double least = log2((double)filter.min_p) - 0x1p-54;
-            const float near = (float)((double)top + least / per_nat);
+            const double least = filter.least - 0x1p-54;
+            const float near = (float)(top64 + least * ((double)filter.temperature * 0.69314718055994530942));
             uint32_t key = max(ordered_bits(near), ordered_bits(-3.402823466e38f) + 2u) - 2u;
             float x;
             for (;; ++key) {
                 x = of_ordered_bits(key);
-                if (((double)x - (double)top) * per_nat >= least || x >= top) break;
+                if (((double)x - top64) * per_nat >= least || x >= top) break;
             }
             x = uniform(x);
             if (x > cut.x) cut = Cut{ x, a.V };

@@ -25,7 +25,7 @@ class Plain:
         self.ring[(head + np.arange(len(free))) % pool] = free
         self.head, self.count = head, len(free)
 
-    def plan(self, held, wanted, slots):
+    def plan(self, held, wanted, slots, slots_from=None):
         columns, pool = self.table.shape[1], len(self.ring)
         pages = lambda n: -(-n // self.page)
         granted, asked, taken, returned, at = [], 0, [], [], 0
@@ -45,7 +45,7 @@ class Plain:
             for c in range(b, a):
                 returned.append(self.table[s, c])
                 self.table[s, c] = -1
-            for place in range(x, y):
+            for place in range(x if slots_from is None else max(0, slots_from[s]), y):
                 if at < len(slots):
                     slots[at] = self.table[s, place // self.page] * self.page + place % self.page if ok else -1
                 at += 1
@@ -91,8 +91,10 @@ def test_many_steps(dy, n_seq, page, pages, columns, extra):
         room = int(rng.choice([0, 1, int(np.maximum(wanted - held, 0).sum()), 5000]))
         slots = torch.full((room,), -5, dtype=torch.int64, device="cuda")
         slots_want = np.full(room, -5, np.int64)
-        granted = dy.page_plan(pool, table, torch.from_numpy(held).cuda(), torch.from_numpy(wanted).cuda(), slots=slots if room or step % 2 else None)
-        want = plain.plan(held.tolist(), wanted.tolist(), slots_want)
+        since = None if step % 3 else (held * rng.random(n_seq)).astype(np.int32) - (rng.random(n_seq) < 0.1)      # inside what is held, or before it
+        granted = dy.page_plan(pool, table, torch.from_numpy(held).cuda(), torch.from_numpy(wanted).cuda(), slots=slots if room or step % 2 else None,
+                               slots_from=None if since is None else torch.from_numpy(since.astype(np.int32)).cuda())
+        want = plain.plan(held.tolist(), wanted.tolist(), slots_want, None if since is None else since.tolist())
         check(plain, pool, table, granted, want, slots, slots_want)
         denied += int((want != wanted).sum())
         free = plain.ring[(plain.head + np.arange(plain.count)) % pages]

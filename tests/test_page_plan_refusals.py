@@ -15,16 +15,17 @@ def lib():
 
 
 def plan(lib, ring=A, state=A + 0x1000, n_pages=100, page=16, table=A + 0x2000, max_pages=10, stride=10, held=A + 0x3000, wanted=A + 0x4000, n_seq=4,
-         granted=A + 0x5000, slots=A + 0x6000, n_slots=100):
-    return lib.dyspec_page_plan(ctypes.byref(binding._PagePool(ring, state, n_pages, page)), table, max_pages, stride, held, wanted, n_seq, granted, slots, n_slots, None)
+         granted=A + 0x5000, slots=A + 0x6000, n_slots=100, slots_from=None):
+    return lib.dyspec_page_plan(ctypes.byref(binding._PagePool(ring, state, n_pages, page)), table, max_pages, stride, held, wanted, n_seq, granted, slots, n_slots, slots_from, None)
 
 
 def test_addresses(lib):
     for name in ("ring", "state", "table", "held", "wanted", "granted"):
         assert plan(lib, **{name: None}) == BAD_ARG, name
         assert plan(lib, **{name: A + 2}) == BAD_ARG, name
+    assert plan(lib, slots_from=A + 2) == BAD_ARG and plan(lib, slots_from=A + 0x5008) == BAD_ARG
     assert plan(lib, slots=A + 4) == BAD_ARG and plan(lib, slots=None) == BAD_ARG
-    assert lib.dyspec_page_plan(None, A, 1, 1, A, A, 1, A, None, 0, None) == BAD_ARG
+    assert lib.dyspec_page_plan(None, A, 1, 1, A, A, 1, A, None, 0, None, None) == BAD_ARG
     # granted is written while lengths are read
     for shift in (0, 4, 12, -12):
         assert plan(lib, granted=A + 0x3000 + shift) == BAD_ARG and plan(lib, granted=A + 0x4000 + shift) == BAD_ARG, shift
