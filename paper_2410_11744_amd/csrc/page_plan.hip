@@ -15,7 +15,8 @@
 namespace dyspec {
 
 constexpr int kPlanThreads = 256;
-constexpr int kPlanShare = 4 * kPlanThreads;     // slots of a sequence that are worth a workgroup of their own
+constexpr int kPlanBatch = 4;                    // slots of a thread that are looked up together
+constexpr int kPlanShare = kPlanBatch * kPlanThreads;      // slots of a sequence that are worth a workgroup of their own
 constexpr int kPlanMost = 8;                     // workgroups of a sequence
 
 // Sum over the lanes up to and with this one.
@@ -62,8 +63,10 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
     const bool granted = before >= after || ((fitting >> s) & 1ull);
     int* const table = a.table + (long long)s * a.table_stride;
     const int first = blockIdx.y * kPlanThreads + (int)threadIdx.x, step = gridDim.y * kPlanThreads;
-    const unsigned next = (unsigned)((head + (unsigned long long)(granted ? of_lane(need_upto - need, s) : 0)) % n_pages);      // column `before`
-    auto fresh = [&](int column) { return a.ring[(unsigned)(((unsigned long long)next + (unsigned)(column - before)) % n_pages)]; };
+    // (`off` places on from `at`, both below n_pages: round the end once)
+    auto on = [=](unsigned at, unsigned off) { const unsigned x = at + off; return x >= n_pages ? x - n_pages : x; };
+    const unsigned next = on(head, (unsigned)(granted ? min(of_lane(need_upto - need, s), (long long)n_pages - 1) : 0));       // column `before`
+    auto fresh = [&](int column) { return a.ring[on(next, (unsigned)(column - before))]; };
     if (ok && granted)
         for (int c = before + first; c < after; c += step) table[c] = fresh(c);
     if (ok && before > after) {
@@ -71,17 +74,25 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
         for (int c = after + first; c < before; c += step) {
             const long long i = given + (c - after);
             const int p = table[c];
-            if (i < room) a.ring[(unsigned)((head + (unsigned long long)(count + i)) % n_pages)] = p;
+            if (i < room) a.ring[on(head, (unsigned)(count + i))] = p;
             table[c] = -1;
         }
     }
     if (a.slots && ok) {
         const long long at = of_lane(marked_upto - marked, s);
-        const int from = __builtin_amdgcn_readlane(z, s);
-        for (int t = first; t < wanted - from && at + t < a.n_slots; t += step) {
-            const int place = from + t, column = place >> a.page_shift;
-            const int p = !granted ? -1 : column < before ? table[column] : fresh(column);
-            a.slots[at + t] = p < 0 ? -1 : ((long long)p << a.page_shift) + (place & (page - 1));
+        const int from = __builtin_amdgcn_readlane(z, s), upto = (int)min((long long)wanted, from + max(a.n_slots - at, 0LL));
+        for (int p0 = from + first; p0 < upto; p0 += kPlanBatch * step) {
+            int page_of[kPlanBatch];
+#pragma unroll
+            for (int y = 0; y < kPlanBatch; ++y) {
+                const int column = (int)min((long long)p0 + (long long)y * step, (long long)upto - 1) >> a.page_shift;
+                page_of[y] = !granted ? -1 : column < before ? table[column] : fresh(column);
+            }
+#pragma unroll
+            for (int y = 0; y < kPlanBatch; ++y) {
+                const int place = p0 + y * step;
+                if (place < upto) a.slots[at + (place - from)] = page_of[y] < 0 ? -1 : ((long long)page_of[y] << a.page_shift) + (place & (page - 1));
+            }
         }
     }
     __syncthreads();                                       // (every wave that goes by the ring's state has it)
@@ -90,7 +101,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
     // ---- the ring's state changes when every workgroup has read it
     const unsigned last = gridDim.x * gridDim.y - 1u;
     if (last == 0u || __builtin_amdgcn_atomic_inc32(reinterpret_cast<unsigned*>(a.state) + 2, last, __ATOMIC_RELAXED, "agent") == last) {
-        a.state[0] = (int)((head + (unsigned long long)taken) % n_pages);
+        a.state[0] = (int)on(head, taken < (long long)n_pages ? (unsigned)taken : 0u);
         a.state[1] = (int)(count - taken + room);
     }
 }
