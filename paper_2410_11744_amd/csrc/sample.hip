@@ -478,9 +478,9 @@ __device__ __forceinline__ bool make_list(const Row<T, Held, NT>& row, SampleLds
     return true;
 }
 
-// Drawn: a token is drawn; else the filtered logits are written.
-template <typename T, bool Held, bool Drawn, int NT, int S>
-__global__ __launch_bounds__(NT, !Drawn && sizeof(T) == 2 ? 8 : 4) void sample_kernel(SampleArgs<S>)
+// Drawn: a token is drawn; else the filtered logits are written.  WAVES: of a SIMD, for which registers are left.
+template <typename T, bool Held, bool Drawn, int NT, int WAVES, int S>
+__global__ __launch_bounds__(NT, WAVES) void sample_kernel(SampleArgs<S>)
 {
     const SampleArgs<S>& a = *(const SampleArgs<S>*)(__attribute__((address_space(4))) const SampleArgs<S>*)__builtin_amdgcn_kernarg_segment_ptr();
     __shared__ SampleLds lds;
@@ -668,20 +668,32 @@ __global__ __launch_bounds__(NT, !Drawn && sizeof(T) == 2 ? 8 : 4) void sample_k
     }
 }
 
-template <typename T, bool Held, bool Drawn, int NT, int S>
+template <typename T, bool Held, bool Drawn, int NT, int WAVES, int S>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, Drawn, NT, S>));
+    static Kernel kernel(reinterpret_cast<const void*>(&sample_kernel<T, Held, Drawn, NT, WAVES, S>));
     SampleArgs<S> a;
     static_cast<SampleHead&>(a) = head;
     for (int s = 0; s < head.n_seq; ++s) { a.row0[s] = row0[s]; a.filter[s] = filter[s]; }
     return kernel.launch(dim3(head.rows), NT, 0, stream, a);
 }
+template <typename T, bool Held, bool Drawn, int NT, int WAVES>
+static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
+{
+    return head.n_seq <= 8 ? launch_rows<T, Held, Drawn, NT, WAVES, 8>(head, row0, filter, stream) : launch_rows<T, Held, Drawn, NT, WAVES, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
+}
+// A row's passes take turns with its waits, so where there are more rows than CUs two rows share one: of fp32 by workgroups of 512
+// threads (512 rows of 32000 through top-p: 46.5 us with 1024 threads, 40.7 with 512), of bf16, held in half the registers, by the
+// ones of 1024 with 64 registers a thread (2417 rows: 151 us with a CU each, 126; 134 with 512 threads).  One row alone is faster
+// with 1024 threads and as many registers as they want (a draw of one token: 12.9 us, 14.7 with 64 registers, 14.6 with 512 threads).
+constexpr int kCus = 256;
 template <typename T, bool Held, bool Drawn>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
 {
-    constexpr int NT = 1024;
-    return head.n_seq <= 8 ? launch_rows<T, Held, Drawn, NT, 8>(head, row0, filter, stream) : launch_rows<T, Held, Drawn, NT, DYSPEC_MAX_SEQ>(head, row0, filter, stream);
+    if constexpr (Held && !Drawn)
+        if (head.rows > kCus)
+            return launch_rows<T, Held, Drawn, sizeof(T) == 4 ? 512 : 1024, sizeof(T) == 4 ? 4 : 8>(head, row0, filter, stream);
+    return launch_rows<T, Held, Drawn, 1024, 4>(head, row0, filter, stream);
 }
 template <typename T>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
@@ -701,7 +713,7 @@ hipError_t launch_sample(const SampleHead& a, const int* row0, const Filter* fil
 hipError_t prepare_sample()                      // (asking loads the code)
 {
     hipFunction_t f;
-    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, true, 1024, 8>)).find(&f);
+    return Kernel(reinterpret_cast<const void*>(&sample_kernel<float, true, true, 1024, 4, 8>)).find(&f);
 }
 
 }  // namespace dyspec

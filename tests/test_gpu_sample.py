@@ -236,3 +236,21 @@ def test_streams_beside_each_other(dy):
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert torch.equal(g.token, w.token) and torch.equal(g.prob, w.prob)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [1, 5, 300, 9000, 32768, 33000])
+def test_more_rows_than_the_chip_has_places(dy, vocab, dtype):
+    """Many rows share the chip in other workgroups than few do: the same bits."""
+    rows, per = 300, 20
+    logits, uniform = table(rows, vocab, dtype, vocab + 1)
+    logits[7, 0] = np.nan
+    logits[8] = 1.5
+    settings = [SETTINGS[i % len(SETTINGS)] for i in range(rows // per)]
+    t, k, p, m = columns(settings)
+    t = [float(x) for x in t]
+    many = dy.filter_logits(logits, dy.Batch.from_sizes([per] * len(settings)), t, top_k=k, top_p=p, min_p=m)
+    for s in range(len(settings)):
+        some = dy.filter_logits(logits[s * per:(s + 1) * per], dy.Batch.from_sizes([per]), t[s], top_k=k[s], top_p=p[s], min_p=m[s])
+        assert torch.equal(bits(many[s * per:(s + 1) * per]), bits(some)), settings[s]
+    check(dy, logits[:20], [20], uniform[:20], settings[:1], least=0.0)
