@@ -7,17 +7,18 @@
 //   B < A   ring[head + count + sum of (A - B) + c - B] = table[c],    table[c] = -1
 // Pages are taken from one end and given back behind the other, so no place of the ring is read and written in one call.
 //
-// What bounds it: two trips to memory one after the other (the lengths and the ring's state, then the pages).
+// What bounds it: trips to memory one after the other (the lengths and the ring's state, then the pages; with several workgroups the
+// arrival), not the bytes: a token each of 64 sequences 3.9 us, of which an empty kernel takes 2; 64 sequences of which 16 end and 16 come
+// with prompts of 500 to 8000 tokens 6.1 us for 0.7 MB.
 #include "page_plan.h"
 
 #include "launch.h"
 
 namespace dyspec {
 
-constexpr int kPlanThreads = 256;
+constexpr int kPlanFew = 256, kPlanMany = 1024;   // threads of a workgroup
 constexpr int kPlanBatch = 4;                    // slots of a thread that are looked up together
-constexpr int kPlanShare = kPlanBatch * kPlanThreads;      // slots of a sequence that are worth a workgroup of their own
-constexpr int kPlanMost = 8;                     // workgroups of a sequence
+constexpr int kPlanMost = 2;                     // workgroups of a sequence
 
 // Sum over the lanes up to and with this one.
 __device__ __forceinline__ long long upto_lane(long long v, int lane)
@@ -35,7 +36,7 @@ __device__ __forceinline__ long long of_lane(long long x, int s)
     return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), s) << 32) | (unsigned)__builtin_amdgcn_readlane((int)x, s));
 }
 
-__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
+__global__ __launch_bounds__(kPlanMany) void page_plan_kernel(PlanArgs a)
 {
     const int s = blockIdx.x, lane = threadIdx.x & 63;
     const unsigned n_pages = (unsigned)a.n_pages;
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanArgs a)
     const bool ok = (__builtin_amdgcn_ballot_w64(right) >> s) & 1ull;
     const bool granted = before >= after || ((fitting >> s) & 1ull);
     int* const table = a.table + (long long)s * a.table_stride;
-    const int first = blockIdx.y * kPlanThreads + (int)threadIdx.x, step = gridDim.y * kPlanThreads;
+    const int first = blockIdx.y * blockDim.x + threadIdx.x, step = gridDim.y * blockDim.x;
     // (`off` places on from `at`, both below n_pages: round the end once)
     auto on = [=](unsigned at, unsigned off) { const unsigned x = at + off; return x >= n_pages ? x - n_pages : x; };
     const unsigned next = on(head, (unsigned)(granted ? min(of_lane(need_upto - need, s), (long long)n_pages - 1) : 0));       // column `before`
@@ -110,9 +111,12 @@ static Kernel plan_kernel(reinterpret_cast<const void*>(&page_plan_kernel));
 
 hipError_t launch_page_plan(const PlanArgs& a, hipStream_t stream)
 {
+    // Few large workgroups: each arrives at the ring's state by an atomic of its own, and those take turns (64 sequences, 66000 slots:
+    // 8.9 us with eight workgroups of 256 threads a sequence, 6.1 with up to two of 1024).
     const long long most = a.slots ? max((long long)a.max_pages, a.n_slots) : a.max_pages;
-    const unsigned cuts = (unsigned)min((long long)kPlanMost, max(1LL, most / kPlanShare));
-    return plan_kernel.launch(dim3(a.n_seq, cuts), kPlanThreads, 0, stream, a);
+    const int threads = most <= kPlanBatch * kPlanFew ? kPlanFew : kPlanMany;
+    const unsigned cuts = most <= kPlanBatch * kPlanMany ? 1 : kPlanMost;
+    return plan_kernel.launch(dim3(a.n_seq, cuts), threads, 0, stream, a);
 }
 
 hipError_t prepare_page_plan()                   // (asking loads the code)
