@@ -842,10 +842,12 @@ def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mas
     context and, causally or by an ancestor mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d].
     cap: scores s count as cap * tanh(s / cap); window: of keys less than that many positions back; rel_pos: int32 [sum N] positions of
     the new tokens relative to each sequence's context (a tree's depths, as for kv_append), by default 0, 1, ..."""
-    where = "dyspec_paged_attn" if cap is None and window is None else "dyspec_paged_attn_scored"
     args, out, _ = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, False, cap, window, rel_pos)
     if args is not None:
-        _issue(getattr(_lib, where), args, cache._device, where)
+        if cap is None and window is None:
+            _issue(_lib.dyspec_paged_attn, args, cache._device, "dyspec_paged_attn")
+        else:
+            _issue(_lib.dyspec_paged_attn_scored, args, cache._device, "dyspec_paged_attn_scored")
     return out
 
 
@@ -860,9 +862,7 @@ def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, an
 
 
 def _scores(cap, window, rel_pos, total: int, device: int):
-    """The C struct for capped scores and windows, None where there is neither."""
-    if cap is None and window is None:
-        return None
+    """The C struct for capped scores and windows, of which there is one."""
     if cap is not None and not cap > 0:
         raise ValueError("cap: a positive number, or None")
     if window is not None and not window >= 1:
@@ -890,7 +890,7 @@ def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared, 
             words = memo["chunk_words"] = max(1, -(-int(np.diff(batch.node_offset).max()) // 64))
         mp = _dense(anc_mask, (total, words), torch.int64, device, "anc_mask")
     raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
-    scores = _scores(cap, window, rel_pos, total, device)
+    scores = None if cap is None and window is None else _scores(cap, window, rel_pos, total, device)
     if out is None:
         with where:
             out = torch.empty_like(q)
@@ -919,10 +919,12 @@ def prompt_attn(q, k, v, batch: Batch, softmax_scale: float, out=None, stream=No
     """dyspec_prompt_attn, with cap or window dyspec_prompt_attn_scored: packed prompts attend to themselves, causally.  q [sum N, Hq, d],
     k, v [sum N, Hkv, d], which may be slices of one projection's rows; the batch's n_nodes are the prompts' lengths, its prefix_len
     zeros.  cap, window, rel_pos as for paged_attn."""
-    where = "dyspec_prompt_attn" if cap is None and window is None else "dyspec_prompt_attn_scored"
     args, out, device = _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap, window, rel_pos)
     if args is not None:
-        _issue(getattr(_lib, where), args, device, where)
+        if cap is None and window is None:
+            _issue(_lib.dyspec_prompt_attn, args, device, "dyspec_prompt_attn")
+        else:
+            _issue(_lib.dyspec_prompt_attn_scored, args, device, "dyspec_prompt_attn_scored")
     return out
 
 
@@ -956,7 +958,7 @@ def _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap=None, window=No
         op = out.data_ptr()
     else:
         op = _dense(out, shape, dtype, device, "out")
-    scores = _scores(cap, window, rel_pos, total, device)
+    scores = None if cap is None and window is None else _scores(cap, window, rel_pos, total, device)
     if total == 0:
         return None, out, device
     if stream is not None:

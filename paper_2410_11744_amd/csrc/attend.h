@@ -47,11 +47,12 @@ struct AttendArgs {
     int Hq, Hkv, G, d;
     uint32_t g_magic;              // r / G = hi(r * g_magic), G = 1: r
     float c2;                      // softmax scale * log2(e): weights are exp2(c2 * score); of capped scores see capped_score
-    float cap, cap_in;             // capped scores: the cap, what <q, k> is multiplied by; else 0
-    int window;
-    const int* rel;                // positions of the new tokens, by the context's length less, or nullptr: 0, 1, ...
     int n_seq;                     // entries of the table
     AttendSeq seq[DYSPEC_MAX_SEQ];
+    // (behind the table: what every kernel reads first stays within as few lines as it was, 0.2 us of a short call)
+    const int* rel;                // positions of the new tokens, by the context's length less, or nullptr: 0, 1, ...
+    float cap, cap_in;             // capped scores: the cap, what <q, k> is multiplied by; else 0
+    int window;
 };
 
 // The arguments where they are: read from the kernel's argument segment, whose first parameter they have to be.  (Taken as a

@@ -55,7 +55,6 @@ def test_binding():
     for bad in (dict(cap=0.0), dict(cap=-3), dict(cap=float("nan")), dict(window=0), dict(window=-5)):
         with pytest.raises(ValueError):
             binding._scores(bad.get("cap"), bad.get("window"), None, 4, 0)
-    assert binding._scores(None, None, None, 4, 0) is None
     x = binding._scores(None, 1 << 40, None, 4, 0)
     assert x.window == (1 << 31) - 1 and x.cap == 0.0
 
