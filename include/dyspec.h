@@ -1,8 +1,8 @@
 /*
  * dyspec.h -- C ABI of the MI355X (gfx950) library for one DySpec speculative step
  * (arXiv 2410.11744): greedy token-tree construction, tree-masked attention and
- * multi-candidate tree verification; and for the paged key/value cache and the prompts
- * around it.
+ * multi-candidate tree verification; for the paged key/value cache and the prompts
+ * around it, its page tables, filtered logits and drawn tokens.
  *
  * Conventions shared by every entry point
  *  - Pointers marked DEVICE address HBM of the current HIP device; pointers marked HOST

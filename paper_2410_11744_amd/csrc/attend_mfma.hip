@@ -24,6 +24,11 @@
 // library: 1.34).  A tree of 512 rows over 4096 tokens in pages of 16, one row block a CU (70 to 80 us, 0.86 to 0.98 PFLOP/s), is another
 // matter: the matrix cores are busy 46 % of the cycles at 2.0 GHz.  17 us go without any context (launch, start, the tree's own tiles,
 // end), 14 to 15 with every 1024 tokens of it (1.2 PFLOP/s).
+//
+// Capped scores (attend.h) take an exponential and a reciprocal more for each, in items of their own two pairs ahead of the exponents; the
+// vector unit is the bound then (16.5 issue slots a score, 5.5 without).  Prompts of 5000, 1290, 333
+// and 1 tokens, 32 heads on 8: 222 us, with a window of 2048 164, with a cap as well 191 (148 GFLOP, 775 TFLOP/s; vector unit busy 61 % and matrix
+// cores 34 % of the cycles).  A tree of 512 rows over 4096 tokens, 64 heads on 8: 80 us, window 2048 50, with a cap 58.
 #include <atomic>
 
 #include "attend.h"

@@ -18,6 +18,10 @@
 //
 // A workgroup has one row, held in registers up to 32768 tokens, else read again for every pass; each of its 16 waves has a run of
 // the vocabulary, so that sums over waves, and then over the threads of one run, find a place in the order of the indices.
+//
+// What bounds it: the vector unit of the CU that has the row.  A weight takes 24 instructions, most of 64 bits, a pass over 32000 of them 6 us, one that counts or compares 1 to 2; eleven barriers a draw.  512 rows of 32000 fp32 through top-p: 40.8 us (131 MB, 3.2 TB/s,
+// of the 5.2 that a copy reaches); 2517 rows of bf16 with eight sequences' settings 125 us (vector unit issuing 68 % of the cycles); one token
+// 12.9 us, 64 tokens of mixed settings 19.5.
 #include "sample.h"
 
 #include "lane_ops.h"
@@ -684,7 +688,7 @@ static hipError_t launch_rows(const SampleHead& head, const int* row0, const Fil
 }
 // A row's passes take turns with its waits, so where there are more rows than CUs two rows share one: of fp32 by workgroups of 512
 // threads (512 rows of 32000 through top-p: 46.5 us with 1024 threads, 40.7 with 512), of bf16, held in half the registers, by the
-// ones of 1024 with 64 registers a thread (2417 rows: 151 us with a CU each, 126; 134 with 512 threads).  One row alone is faster
+// ones of 1024 with 64 registers a thread (2517 rows: 151 us with a CU each, 126; 134 with 512 threads).  One row alone is faster
 // with 1024 threads and as many registers as they want (a draw of one token: 12.9 us, 14.7 with 64 registers, 14.6 with 512 threads).
 constexpr int kCus = 256;
 template <typename T, bool Held, bool Drawn>
