@@ -841,7 +841,7 @@ def paged_attn(q, batch: Batch, cache: PagedCache, softmax_scale: float, anc_mas
     """dyspec_paged_attn, with cap or window dyspec_paged_attn_scored: the new tokens (appended before) attend to the pages: to their
     context and, causally or by an ancestor mask [sum N, max(1, ceil(max N / 64))], to each other.  q/out [sum N, Hq, d].
     cap: scores s count as cap * tanh(s / cap); window: of keys less than that many positions back; rel_pos: int32 [sum N] positions of
-    the new tokens relative to each sequence's context (a tree's depths, as for kv_append), by default 0, 1, ..."""
+    the new tokens relative to each sequence's context (a tree's depths, as for kv_append; only a window reads them), by default 0, 1, ..."""
     args, out, _ = _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, False, cap, window, rel_pos)
     if args is not None:
         if cap is None and window is None:
@@ -1095,11 +1095,21 @@ def _per_sequence(x, kind, n_seq: int, what: str):
     """A C array of one number a sequence, None for None."""
     if x is None:
         return None
-    if not isinstance(x, (list, tuple)):
-        x = [x] * n_seq if isinstance(x, (int, float)) else np.asarray(x).tolist()
+    if isinstance(x, (int, float)):
+        x = [x] * n_seq
+    elif not isinstance(x, (list, tuple)):
+        x = np.asarray(x).tolist()
+        if not isinstance(x, list):
+            x = [x] * n_seq
     if len(x) != n_seq:
         raise ValueError(f"{what}: a number, or one for each of the {n_seq} sequences expected")
-    return (kind * n_seq)(*x)
+    try:
+        a = (kind * n_seq)(*x)
+    except TypeError:                                              # (elements of arrays)
+        a = (kind * n_seq)(*np.asarray(x).tolist())
+    if kind is ctypes.c_int32 and list(a) != list(x):      # (ctypes keeps the low bits of what does not fit)
+        raise ValueError(f"{what}: 32-bit numbers expected")
+    return a
 
 
 def _settings(batch, temperature, top_k, top_p, min_p):

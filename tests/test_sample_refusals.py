@@ -77,6 +77,20 @@ def test_wrong_numbers_of_settings():
     assert list(t) == [0.5, 1.0] and list(k) == [7, 7] and list(p) == [0.25, 0.5] and m is None
 
 
+def test_settings_of_other_kinds():
+    """Numbers as arrays' elements, and what does not fit 32 bits: refused, not taken for another number."""
+    b = binding.Batch.from_sizes([1, 1])
+    t, k, p, m = binding._settings(b, np.float64(0.7), np.int64(40), np.array(0.5), None)
+    assert list(t) == [np.float32(0.7)] * 2 and list(k) == [40, 40] and list(p) == [0.5, 0.5] and m is None
+    assert list(binding._settings(b, 1.0, [np.int32(3), 2**31 - 1], None, None)[1]) == [3, 2**31 - 1]
+    for bad in (2**31, 2**32 + 1, [5, -2**31 - 1], 1 << 70):
+        with pytest.raises(ValueError):
+            binding._settings(b, 1.0, bad, None, None)
+    for bad in (1.5, [2, 2.5]):
+        with pytest.raises(TypeError):
+            binding._settings(b, 1.0, bad, None, None)
+
+
 def test_the_plain_form_by_hand():
     x = np.log(np.array([1.0, 4.0, 2.0, 1.0]))                # weights 1/4, 1, 1/2, 1/4 of the largest
     for args, kept, token in [((0.0, 1.0), [0, 1, 2, 3], 0), ((0.2, 1.0), [0, 1, 2, 3], 1), ((0.99, 1.0), [0, 1, 2, 3], 3), ((0.5, 0.0), [1], 1),
