@@ -10,7 +10,8 @@
 // With few rows the four waves share one block of 16 rows and deal the keys among themselves; they merge through LDS.
 //
 // What bounds it: the matrix pipe (32 cycles per 16x16x4; two products of 2 * 16 * keys * d), and for small prompts the start: prompts
-// of 1 to 641 tokens, 8 heads on 4 of 64, take 16.8 us, about ten of them lookups, first trips to memory and the last row block's walk; in a window of 100, capped, 12.0.
+// of 1 to 641 tokens, 8 heads on 4 of 64, take 16.8 us, about ten of them lookups, first trips to memory and the last row block's walk; in a window
+// of 100, with capped scores, 12.0.
 #include "attend.h"
 
 namespace dyspec {

@@ -210,6 +210,21 @@ def test_only_the_window_is_read(dy):
         check(c, got, 0.0, window)
 
 
+def test_pages_behind_the_window_given_away(dy):
+    """Every page whose keys are all behind the window is gone, those that a walk begins with among them; what is read in their place holds
+    NaN.  A tree's positions, single tokens, and several."""
+    new, context, window, page = (1, 33, 1), (3000, 1000, 777), 256, 16
+    for dtype, d in ((BF16, 128), (BF16, 64), (F32, 64)):
+        c = Paged(new, context, 8, 2, d, dtype, page, 6)
+        k, v = (torch.cat([x, torch.full_like(x[:1], math.nan)]) for x in (c.cache.k, c.cache.v))
+        for rel in (None, np.concatenate([np.minimum(np.arange(n), 3) for n in new]).astype(np.int32)):
+            table = c.cache.page_table.clone()
+            for s in range(3):
+                table[s, :(context[s] + 1 - window) // page] = -1
+            out = dy.paged_attn(c.q_dev, c.batch, dy.PagedCache(k, v, table), c.scale, window=window, rel_pos=None if rel is None else dev(rel))
+            check(c, out, 0.0, window, rel)
+
+
 def test_graphs_and_streams(dy):
     """Prepared calls of capped and windowed layers, recorded and replayed beside eager ones of other streams."""
     mask, depth = random_mask((64,), 1)
