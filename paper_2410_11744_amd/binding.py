@@ -9,6 +9,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -1091,31 +1092,28 @@ def filter_logits_call(logits, batch: Batch, temperature, top_k=None, top_p=None
     return DeviceCall(_lib.dyspec_filter_logits, args, (logits, batch._c(), held, out), "dyspec_filter_logits", out, device)
 
 
-def _per_sequence(x, kind, n_seq: int, what: str):
-    """A C array of one number a sequence, None for None."""
+def _per_sequence(x, code: str, n_seq: int, what: str):
+    """One number a sequence as C has them ('f': fp32, 'i': int32), None for None."""
     if x is None:
         return None
     if isinstance(x, (int, float)):
-        x = [x] * n_seq
+        x = (x,) * n_seq
     elif not isinstance(x, (list, tuple)):
         x = np.asarray(x).tolist()
         if not isinstance(x, list):
-            x = [x] * n_seq
+            x = (x,) * n_seq
     if len(x) != n_seq:
         raise ValueError(f"{what}: a number, or one for each of the {n_seq} sequences expected")
     try:
-        a = (kind * n_seq)(*x)
-    except TypeError:                                              # (elements of arrays)
-        a = (kind * n_seq)(*np.asarray(x).tolist())
-    if kind is ctypes.c_int32 and list(a) != list(x):      # (ctypes keeps the low bits of what does not fit)
-        raise ValueError(f"{what}: 32-bit numbers expected")
-    return a
+        return struct.pack(f"{n_seq}{code}", *x)                   # (64 of them 1 us, as a ctypes array 4.4)
+    except (struct.error, OverflowError) as e:
+        raise ValueError(f"{what}: 32-bit numbers expected ({e})") from None
 
 
 def _settings(batch, temperature, top_k, top_p, min_p):
     n = batch.n_seq
-    return (_per_sequence(temperature, ctypes.c_float, n, "temperature"), _per_sequence(top_k, ctypes.c_int32, n, "top_k"),
-            _per_sequence(top_p, ctypes.c_float, n, "top_p"), _per_sequence(min_p, ctypes.c_float, n, "min_p"))
+    return (_per_sequence(temperature, "f", n, "temperature"), _per_sequence(top_k, "i", n, "top_k"),
+            _per_sequence(top_p, "f", n, "top_p"), _per_sequence(min_p, "f", n, "min_p"))
 
 
 def _logit_rows(t, total: int, what: str) -> int:

@@ -21,7 +21,7 @@
 //
 // What bounds it: the vector unit of the CU that has the row.  A weight takes 24 instructions, most of 64 bits, a pass over 32000 of them 6 us, one that counts or compares 1 to 2; eleven barriers a draw.  512 rows of 32000 fp32 through top-p: 40.8 us (131 MB, 3.2 TB/s,
 // of the 5.2 that a copy reaches); 2517 rows of bf16 with eight sequences' settings 125 us (vector unit issuing 68 % of the cycles); one token
-// 12.9 us, 64 tokens of mixed settings 19.5.
+// 12.9 us, 64 tokens of mixed settings 18.2.
 #include "sample.h"
 
 #include "lane_ops.h"

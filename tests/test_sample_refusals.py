@@ -68,27 +68,29 @@ def test_batches(lib):
     assert lib.dyspec_filter_logits(A, 0, 9, 9, none, one[0], None, None, None, FAR, 9, None) == 0
 
 
+def given(settings):
+    return [None if b is None else np.frombuffer(b, t).tolist() for b, t in zip(settings, (np.float32, np.int32, np.float32, np.float32))]
+
+
 def test_wrong_numbers_of_settings():
     b = binding.Batch.from_sizes([1, 1])
     for bad in ([1.0], [1.0] * 3, np.ones(3)):
         with pytest.raises(ValueError):
             binding._settings(b, bad, None, None, None)
-    t, k, p, m = binding._settings(b, np.float32([0.5, 1.0]), 7, [0.25, 0.5], None)
-    assert list(t) == [0.5, 1.0] and list(k) == [7, 7] and list(p) == [0.25, 0.5] and m is None
+    t, k, p, m = given(binding._settings(b, np.float32([0.5, 1.0]), 7, [0.25, 0.5], None))
+    assert t == [0.5, 1.0] and k == [7, 7] and p == [0.25, 0.5] and m is None
 
 
 def test_settings_of_other_kinds():
     """Numbers as arrays' elements, and what does not fit 32 bits: refused, not taken for another number."""
     b = binding.Batch.from_sizes([1, 1])
-    t, k, p, m = binding._settings(b, np.float64(0.7), np.int64(40), np.array(0.5), None)
-    assert list(t) == [np.float32(0.7)] * 2 and list(k) == [40, 40] and list(p) == [0.5, 0.5] and m is None
-    assert list(binding._settings(b, 1.0, [np.int32(3), 2**31 - 1], None, None)[1]) == [3, 2**31 - 1]
-    for bad in (2**31, 2**32 + 1, [5, -2**31 - 1], 1 << 70):
+    t, k, p, m = given(binding._settings(b, np.float64(0.7), np.int64(40), np.array(0.5), None))
+    assert t == [np.float32(0.7)] * 2 and k == [40, 40] and p == [0.5, 0.5] and m is None
+    assert given(binding._settings(b, 1.0, [np.int32(3), 2**31 - 1], None, None))[1] == [3, 2**31 - 1]
+    for bad in (2**31, 2**32 + 1, [5, -2**31 - 1], 1 << 70, 1.5, [2, 2.5]):
         with pytest.raises(ValueError):
             binding._settings(b, 1.0, bad, None, None)
-    for bad in (1.5, [2, 2.5]):
-        with pytest.raises(TypeError):
-            binding._settings(b, 1.0, bad, None, None)
+    assert given(binding._settings(b, 1e39, None, None, None))[0] == [float("inf")] * 2      # (refused by the call)
 
 
 def test_the_plain_form_by_hand():
