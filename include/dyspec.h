@@ -526,7 +526,7 @@ dyspec_status dyspec_prompt_attn_scored(const void* q, int64_t q_stride, const v
  *   slots       DEVICE [n_slots] i64 or NULL, 8-byte aligned: where new tokens go, packed by sequences: for tokens
  *               slots_from[s] .. wanted[s] - 1 the row of the pool (page * page_size + row), -1 for all of a sequence
  *               whose demand is not met.  What does not fit is left out, what is behind the last one stays as it is
- *   slots_from  DEVICE [n_seq] i32 (negative ones count as 0), or NULL: held.  (After a draft tree a sequence holds
+ *   slots_from  DEVICE [n_seq] i32 (negative ones count as 0; from wanted[s] on: no slot), or NULL: held.  (After a draft tree a sequence holds
  *               pages for more tokens than its context has: its new ones begin behind the context)
  *   n_seq       1 .. DYSPEC_MAX_SEQ
  * Calls on one pool must be ordered (a stream does that).  No workspace; the other arrays 4-byte aligned.

@@ -43,14 +43,16 @@ __global__ __launch_bounds__(kPlanMany) void page_plan_kernel(PlanArgs a)
     // ---- every sequence's lengths, a lane each
     const bool there = lane < a.n_seq;
     const int x = there ? a.held[lane] : 0, y = there ? a.wanted[lane] : 0;
-    const int z = a.slots_from ? (there ? max(a.slots_from[lane], 0) : 0) : x;      // first token that gets a slot
+    const int since = a.slots_from ? (there ? a.slots_from[lane] : 0) : x;
     const unsigned head = (unsigned)a.state[0] % n_pages;
     const long long count = min(max(a.state[1], 0), a.n_pages);
     const int page = 1 << a.page_shift;
     const bool sized = x >= 0 && y >= 0 && x <= DYSPEC_MAX_CONTEXT && y <= DYSPEC_MAX_CONTEXT;
     const int A = sized ? (x + page - 1) >> a.page_shift : 0, B = sized ? (y + page - 1) >> a.page_shift : 0;
     const bool right = sized && A <= a.max_pages && B <= a.max_pages;
-    const long long need = right ? max(B - A, 0) : 0, back = right ? max(A - B, 0) : 0, marked = right ? max(y - z, 0) : 0;
+    // first token that gets a slot: no further on than the last one's end, so that places (in 32 bits) stay below 2^30 and a few thousand
+    const int z = right ? min(max(since, 0), y) : 0;
+    const long long need = right ? max(B - A, 0) : 0, back = right ? max(A - B, 0) : 0, marked = right ? y - z : 0;
     const long long need_upto = upto_lane(need, lane), back_upto = upto_lane(back, lane), marked_upto = upto_lane(marked, lane);
     const bool fits = need_upto <= count;
     // what is taken in all: demands come in order, so it is the last sum that fits

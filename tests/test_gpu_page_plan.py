@@ -218,3 +218,26 @@ def test_pools_beside_each_other(dy):
             want = plains[i].plan(held[i].tolist(), wanted.tolist(), [])
             check(plains[i], sets[i][0], sets[i][1], granted, want, torch.zeros(0, dtype=torch.int64), np.zeros(0, np.int64))
             held[i] = want
+
+
+@pytest.mark.parametrize("n_seq,page,columns,n_slots", [(1, 16, 20, 300), (7, 32, 200, 3000), (64, 16, 300, 20000)])
+def test_slots_from_any_number(dy, n_seq, page, columns, n_slots):
+    """slots_from at, just above and far above wanted, up to the largest number: no slot for such a sequence, and nothing beside the slots is
+    touched.  (Sums of such numbers and a thread's own do not fit 32 bits.)"""
+    rng = np.random.default_rng(n_seq)
+    far = [1 << 30, (1 << 30) + 1, 2**31 - 2049, 2**31 - 2048, 2**31 - 1024, 2**31 - 257, 2**31 - 256, 2**31 - 2, 2**31 - 1, -2**31]
+    plain = Plain(n_seq, columns, page, rng.permutation(n_seq * columns).astype(np.int32), n_seq * columns)
+    pool, table, whole = on_device(dy, plain, 3)
+    held = np.zeros(n_seq, np.int32)
+    for step in range(len(far) + 3):
+        wanted = rng.integers(0, columns * page + 1, n_seq).astype(np.int32)
+        near = wanted.astype(np.int64) + rng.integers(-3, 3, n_seq)
+        since = np.where((np.arange(n_seq) + step) % 3 == 0, near, far[step] if step < len(far) else wanted.astype(np.int64) + step - len(far)).astype(np.int32)
+        room = torch.full((n_slots + 64,), -5, dtype=torch.int64, device="cuda")
+        slots, slots_want = room[32:32 + n_slots], np.full(n_slots, -5, np.int64)
+        granted = dy.page_plan(pool, table, torch.from_numpy(held).cuda(), torch.from_numpy(wanted).cuda(), slots=slots, slots_from=torch.from_numpy(since).cuda())
+        want = plain.plan(held.tolist(), wanted.tolist(), slots_want, since.tolist())
+        check(plain, pool, table, granted, want, slots, slots_want)
+        assert bool((room[:32] == -5).all()) and bool((room[32 + n_slots:] == -5).all())
+        held = want
+    assert bool((whole[-1] == 99).all()) and bool((whole[:, columns:] == 99).all())
