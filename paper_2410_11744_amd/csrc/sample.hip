@@ -26,6 +26,7 @@
 
 #include "lane_ops.h"
 #include "launch.h"
+#include "min_p_cut.h"
 #include "vocab_common.h"
 
 namespace dyspec {
@@ -94,14 +95,6 @@ __device__ __forceinline__ u64 weight_of(double z)
     const double w = __hiloint2double(__double2hiint(p) + ((n + kWeightBits) << 20), __double2loint(p)) + constant(4503599627370496.0);
     return (u64)__double_as_longlong(w) & 0xfffffffffffffull;
 }
-
-// Ascending with x; -0 and 0 alike.
-__device__ __forceinline__ uint32_t ordered_bits(float x)
-{
-    const uint32_t u = __float_as_uint(x + 0.0f);
-    return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float of_ordered_bits(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
 // A row as a thread has it.  Wave w has tokens w * span .. of the row, lane l of it the kTokens from w * span + (64 p + l) * kTokens
 // on, p < pieces.  Places past the row's end hold a NaN, which no comparison keeps.
@@ -603,16 +596,7 @@ __global__ __launch_bounds__(NT, WAVES) void sample_kernel(SampleArgs<S>)
             else cut = resolve(row, row, lds, cut, bins, bin, before, target, amount);
         }
         if (filter.min_p > 0.0f) {
-            // the smallest logit whose weight, as a number of 64 bits, is min_p or more (those within 2^-54 of 1 are 1)
-            const double least = filter.least - 0x1p-54;
-            const float near = (float)(top64 + least * ((double)filter.temperature * 0.69314718055994530942));
-            uint32_t key = max(ordered_bits(near), ordered_bits(-3.402823466e38f) + 2u) - 2u;
-            float x;
-            for (;; ++key) {
-                x = of_ordered_bits(key);
-                if (((double)x - top64) * per_nat >= least || x >= top) break;
-            }
-            x = uniform(x);
+            const float x = uniform(min_p_cut(top, filter.temperature, per_nat, filter.least, [] {}));
             if (x > cut.x) cut = Cut{ x, a.V };
         }
     }

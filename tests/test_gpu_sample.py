@@ -254,3 +254,19 @@ def test_more_rows_than_the_chip_has_places(dy, vocab, dtype):
         some = dy.filter_logits(logits[s * per:(s + 1) * per], dy.Batch.from_sizes([per]), t[s], top_k=k[s], top_p=p[s], min_p=m[s])
         assert torch.equal(bits(many[s * per:(s + 1) * per]), bits(some)), settings[s]
     check(dy, logits[:20], [20], uniform[:20], settings[:1], least=0.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [70, 5000, 40000])
+def test_min_p_cuts_next_to_zero(dy, vocab, dtype):
+    """Settings whose cut is the difference of two near numbers: it lies next to a logit of zero, where floats are far denser than what the
+    difference is known to.  Logits on both sides of it, 1e-5 and more away."""
+    for top, temperature, min_p in [(0.0866413191, 0.0650000051, 0.263699979), (1.79451227, 0.782053828, 0.100800216), (3.0, 1.0, float(np.exp(-3.0))),
+                                    (-2.0, 1.0, 0.5), (2.5, 1e-30, 0.3), (1.0, 1e30, 1.0)]:
+        g = torch.Generator(device="cuda").manual_seed(vocab)
+        x = torch.rand((3, vocab), generator=g, device="cuda") * 3 - 2.9
+        x[:, :8] = torch.tensor([1e-5, -1e-5, 1e-3, -1e-3, 0.05, -0.05, 1e-4, -1e-4], device="cuda")
+        x = torch.minimum(x, torch.tensor(top, device="cuda")).to(dtype)
+        x[:, vocab // 2] = torch.tensor(top).to(dtype)
+        x = torch.minimum(x, x[:, vocab // 2:vocab // 2 + 1])
+        check(dy, x, [1, 1, 1], torch.tensor([0.1, 0.5, 0.9], device="cuda"), [(temperature, 0, 1, min_p), (temperature, 20, 1, min_p), (temperature, 0, 0.9, min_p)], least=0.5)
