@@ -390,11 +390,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = max3(mx, sm[i], sm[i + 1]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-        const float m_new = max3(m_run, mx, kLowest);
-        const float alpha = fast_exp2((m_run - m_new) * c2);
         // A row without a sum so far starts at zero whatever acc holds: the first half's second product takes what lies in V's slot then,
-        // query rows, at weights of zero, and a row's NaN is nothing to other rows.
-        const bool fresh = m_run <= kLowest;
+        // query rows, at weights of zero, and a row's NaN is nothing to other rows.  It keeps its reference of -inf until it sees a key,
+        // however many halves it sits through that only others see: the half in which it does is then done again, whatever the scale.
+        const bool fresh = m_run == -INFINITY;
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = m_new == m_run ? 1.0f : fast_exp2((m_run - m_new) * c2);
         m_run = m_new;
         l_run *= alpha;
         if (__all(fresh)) {
@@ -532,8 +533,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_mfma_kernel(AttendArgs)
     // ---- the rows leave.  With two tiles a step the two waves of a row block merge first: each finishes half of the dims, leaves
     //      the other half with its (max, sum) in LDS and takes its own of the other wave.
     l_run += __shfl_xor(l_run, 32, kWave);
-    if (__any(m_run <= kLowest)) {                                 // rows that saw no key here: zeros, as above
-        const bool none = m_run <= kLowest;
+    if (__any(m_run == -INFINITY)) {                               // rows that saw no key here: zeros, as above
+        const bool none = m_run == -INFINITY;
         m_run = fmaxf(m_run, kLowest);
 #pragma unroll
         for (int db = 0; db < DB; ++db)

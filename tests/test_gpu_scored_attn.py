@@ -259,3 +259,32 @@ def test_empty_batches(dy):
     table = torch.zeros((2, 4), dtype=torch.int32, device="cuda")
     assert dy.paged_attn(z, none, dy.PagedCache(c.cache.k, c.cache.v, table), 0.1, cap=5, window=3).shape == (0, 4, 64)
     assert dy.prompt_attn(z, z[:, :2], z[:, :2], dy.Batch.from_sizes([0]), 0.1, cap=5).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("kind", ["causal", "tree", "positions", "near"])
+@pytest.mark.parametrize("form,dtype,Hq,Hkv,d", [(f, *s) for s in ((BF16, 4, 4, 128), (BF16, 8, 2, 64), (F32, 4, 2, 64)) for f in FORMS if s[0] is BF16 or f[0] >= 4], ids=str)
+def test_a_scale_of_nearly_nothing(dy, form, dtype, Hq, Hkv, d, kind):
+    """All weights alike, so that no running reference is ever passed by much, in rows that first sit through keys only others see: those
+    of a window, or (near) of masks whose rows see two tokens and no context.  Beside a query that is no number, whose row alone is none."""
+    print("form", form, dtype, Hq, Hkv, d, kind, flush=True)
+    new, context = (300, 1, 90), (0, 0, 0) if kind == "near" else (130, 2000, 0)
+    mask, rel = random_mask(new, 12) if kind in ("tree", "positions") else (None, None)
+    if kind == "near":
+        mask, at = np.zeros((sum(new), 5), np.uint64), 0
+        for n in new:
+            for j in range(n):
+                for see in (j, j - j % 7):
+                    mask[at + j, see // 64] |= np.uint64(1) << np.uint64(see % 64)
+            at += n
+    c = Paged(new, context, Hq, Hkv, d, dtype, 16, 59, mask=mask if kind in ("tree", "near") else None)
+    c.scale = 1e-38
+    window = 0 if kind == "near" else 40
+    rel = rel if kind == "positions" else None
+    st, want = in_form(dy, form, c, 0.0, window, rel)
+    assert st == 0
+    check(c, want, 0.0, window, rel, form)
+    c.q_dev[20, 1, 7] = math.nan
+    out = in_form(dy, form, c, 0.0, window, rel)[1]
+    assert bool(torch.isnan(out[20, 1]).all())
+    out[20, 1] = want[20, 1]
+    check(c, out, 0.0, window, rel, form)
