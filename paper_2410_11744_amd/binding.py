@@ -864,12 +864,13 @@ def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, an
 
 def _scores(cap, window, rel_pos, total: int, device: int):
     """The C struct for capped scores and windows, of which there is one."""
-    if cap is not None and not cap > 0:
-        raise ValueError("cap: a positive number, or None")
     if window is not None and not window >= 1:
         raise ValueError("window: at least 1, or None")
     rp = 0 if rel_pos is None else _dense(rel_pos, (total,), _torch.int32, device, "rel_pos")
-    return _Scores(cap or 0.0, min(window or 0, (1 << 31) - 1), rp)
+    x = _Scores(cap or 0.0, min(window or 0, (1 << 31) - 1), rp)
+    if cap is not None and not x.cap > 0:                          # (as the call has it: what rounds to zero would be none)
+        raise ValueError("cap: a positive number of 32 bits, or None")
+    return x
 
 
 def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared, cap=None, window=None, rel_pos=None):

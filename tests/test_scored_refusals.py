@@ -59,6 +59,14 @@ def test_binding():
     assert x.window == (1 << 31) - 1 and x.cap == 0.0
 
 
+def test_caps_of_no_32_bits():
+    """A cap that rounds to zero would be none at all: refused.  The smallest that does not goes on to the call, which says what it takes."""
+    for bad in (1e-46, 7e-46, 1e-300, 5e-324, -1e-50):
+        with pytest.raises(ValueError):
+            binding._scores(bad, None, None, 4, 0)
+    assert binding._scores(1.5e-45, None, None, 4, 0).cap > 0 and binding._scores(50, None, None, 4, 0).cap == 50.0
+
+
 def test_the_plain_form_by_hand():
     assert visible_rows(3, 2, None, 2).tolist() == [[False, True, True, False, False], [False, False, True, True, False], [False, False, False, True, True]]
     # a tree: rows 1 and 2 are children of row 0, at depth 1
