@@ -863,10 +863,13 @@ def paged_attn_call(q, batch: Batch, cache: PagedCache, softmax_scale: float, an
 
 
 def _scores(cap, window, rel_pos, total: int, device: int):
-    """The C struct for capped scores and windows, of which there is one."""
+    """The C struct for capped scores and windows; None where there are neither.  (rel_pos is looked at all the same: a layer without a
+    window takes the call of one that has it, as it is.)"""
     if window is not None and not window >= 1:
         raise ValueError("window: at least 1, or None")
     rp = 0 if rel_pos is None else _dense(rel_pos, (total,), _torch.int32, device, "rel_pos")
+    if cap is None and window is None:
+        return None
     x = _Scores(cap or 0.0, min(window or 0, (1 << 31) - 1), rp)
     if cap is not None and not x.cap > 0:                          # (as the call has it: what rounds to zero would be none)
         raise ValueError("cap: a positive number of 32 bits, or None")
@@ -892,7 +895,7 @@ def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared, 
             words = memo["chunk_words"] = max(1, -(-int(np.diff(batch.node_offset).max()) // 64))
         mp = _dense(anc_mask, (total, words), torch.int64, device, "anc_mask")
     raw, where = (torch._C._cuda_getCurrentRawStream(device), _current) if stream is None else _stream_of(stream, device)
-    scores = None if cap is None and window is None else _scores(cap, window, rel_pos, total, device)
+    scores = None if cap is None and window is None and rel_pos is None else _scores(cap, window, rel_pos, total, device)
     if out is None:
         with where:
             out = torch.empty_like(q)
@@ -960,7 +963,7 @@ def _prompt_args(q, k, v, batch, softmax_scale, out, stream, cap=None, window=No
         op = out.data_ptr()
     else:
         op = _dense(out, shape, dtype, device, "out")
-    scores = None if cap is None and window is None else _scores(cap, window, rel_pos, total, device)
+    scores = None if cap is None and window is None and rel_pos is None else _scores(cap, window, rel_pos, total, device)
     if total == 0:
         return None, out, device
     if stream is not None:

@@ -288,3 +288,21 @@ def test_a_scale_of_nearly_nothing(dy, form, dtype, Hq, Hkv, d, kind):
     assert bool(torch.isnan(out[20, 1]).all())
     out[20, 1] = want[20, 1]
     check(c, out, 0.0, window, rel, form)
+
+
+def test_positions_are_looked_at_whether_they_are_read_or_not(dy):
+    """rel_pos of another size, type or device is refused by calls without a window too; one that fits changes nothing there."""
+    new, context = (40, 3), (100, 20)
+    mask, depth = random_mask(new, 5)
+    c = Paged(new, context, 4, 2, 64, F32, 16, 3, mask=mask)
+    k, v = (torch.randn((43, 2, 64), device="cuda") for _ in range(2))
+    prompts = dy.Batch.from_sizes(new)
+    for scores in (dict(), dict(cap=9.0), dict(window=20)):
+        calls = [lambda f, rel: f(c.q_dev, c.batch, c.cache, c.scale, anc_mask=c.mask_dev, rel_pos=rel, **scores), lambda f, rel: f(c.q_dev, k, v, prompts, c.scale, rel_pos=rel, **scores)]
+        for call, fs in zip(calls, ((dy.paged_attn, dy.paged_attn_call), (dy.prompt_attn, dy.prompt_attn_call))):
+            for f in fs:
+                for bad in (dev(depth[:-1]), dev(depth).long(), dev(depth).cpu(), torch.zeros(86, dtype=torch.int32, device="cuda")[::2]):
+                    with pytest.raises(ValueError, match="rel_pos"):
+                        call(f, bad)
+            if "window" not in scores:
+                assert torch.equal(call(fs[0], dev(depth)), call(fs[0], None)) and torch.equal(call(fs[1], dev(depth))(), call(fs[0], None))
