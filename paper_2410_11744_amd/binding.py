@@ -904,7 +904,7 @@ def _attn_args(q, batch, cache, softmax_scale, anc_mask, out, stream, prepared, 
         op = _dense(out, shape, dtype, device, "out")
     if total == 0:
         return None, out, None
-    key = ("ws_paged", Hq, Hkv, d, code) if scores is None else ("ws_paged", Hq, Hkv, d, code, cap, window, rel_pos is None)
+    key = ("ws_paged", Hq, Hkv, d, code) if scores is None else ("ws_paged", Hq, Hkv, d, code, scores.cap, scores.window, rel_pos is None)
     nbytes = memo.get(key)
     if nbytes is None:
         nbytes = memo[key] = int(_lib.dyspec_paged_attn_workspace_bytes(ref, Hq, Hkv, d, code) if scores is None else

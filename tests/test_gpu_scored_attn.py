@@ -306,3 +306,19 @@ def test_positions_are_looked_at_whether_they_are_read_or_not(dy):
                         call(f, bad)
             if "window" not in scores:
                 assert torch.equal(call(fs[0], dev(depth)), call(fs[0], None)) and torch.equal(call(fs[1], dev(depth))(), call(fs[0], None))
+
+
+def test_workspaces_go_by_the_numbers(dy):
+    """What a batch remembers of a call is its cap and window, not the objects that hold them: a cap in a tensor that is written anew, or in
+    another tensor, is taken as it stands."""
+    c = Paged((1, 1), (9000, 40), 8, 2, 128, BF16, 16, 4)
+    cap = torch.tensor(300.0)                                      # (fp32 throughout; 50: the bf16 matrix cores)
+    first = dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, cap=cap)
+    assert torch.equal(first, dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, cap=300.0))
+    cap.fill_(50.0)
+    want = dy.paged_attn(c.q_dev, dy.Batch.from_sizes((1, 1), (9000, 40)), c.cache, c.scale, cap=50.0)
+    assert torch.equal(dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, cap=cap), want)
+    known = len(c.batch._memo())
+    for _ in range(5):
+        assert torch.equal(dy.paged_attn(c.q_dev, c.batch, c.cache, c.scale, cap=torch.tensor(50.0)), want)
+    assert len(c.batch._memo()) == known
