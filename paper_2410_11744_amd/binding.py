@@ -1063,7 +1063,7 @@ class Sampled:
 def sample(logits, batch: Batch, uniform, temperature, top_k=None, top_p=None, min_p=None, out: Optional[Sampled] = None, stream=None) -> Sampled:
     """dyspec_sample: a token for every row of logits [rows, vocab] (a batch's n_nodes are its sequences' rows) by the given random
     numbers uniform [rows] fp32 in [0, 1), after temperature, top-k, top-p and min-p: a number for all sequences, or one each; None:
-    no such filter."""
+    no such filter.  These settings are read on the host when the call is made or prepared (a recorded graph keeps its own)."""
     args, out, device, _ = _sample_args(logits, batch, uniform, temperature, top_k, top_p, min_p, out, stream)
     if args is not None:
         _issue(_lib.dyspec_sample, args, device, "dyspec_sample")
@@ -1103,7 +1103,10 @@ def _per_sequence(x, code: str, n_seq: int, what: str):
     if isinstance(x, (int, float)):
         x = (x,) * n_seq
     elif not isinstance(x, (list, tuple)):
-        x = np.asarray(x).tolist()
+        try:
+            x = np.asarray(x).tolist()
+        except (TypeError, RuntimeError):                          # (a device's tensor, one with a gradient)
+            raise ValueError(f"{what}: numbers on the host expected, got {type(x).__name__}") from None
         if not isinstance(x, list):
             x = (x,) * n_seq
     if len(x) != n_seq:

@@ -93,6 +93,17 @@ def test_settings_of_other_kinds():
     assert given(binding._settings(b, 1e39, None, None, None))[0] == [float("inf")] * 2      # (refused by the call)
 
 
+def test_settings_that_are_not_on_the_host():
+    """Refused by name: tensors of a device, which numpy cannot read (here one without data, and one whose gradient is wanted)."""
+    import torch
+    b = binding.Batch.from_sizes([1, 1])
+    for bad in (torch.ones(2, device="meta"), torch.ones(2, requires_grad=True)):
+        for at, name in enumerate(("temperature", "top_k", "top_p", "min_p")):
+            with pytest.raises(ValueError, match=name):
+                binding._settings(b, *[bad if at == x else 1.0 if x == 0 else None for x in range(4)])
+    assert given(binding._settings(b, torch.tensor([0.5, 1.0]), torch.tensor([3, 4]), torch.tensor(0.5), None))[:3] == [[0.5, 1.0], [3, 4], [0.5, 0.5]]
+
+
 def test_the_plain_form_by_hand():
     x = np.log(np.array([1.0, 4.0, 2.0, 1.0]))                # weights 1/4, 1, 1/2, 1/4 of the largest
     for args, kept, token in [((0.0, 1.0), [0, 1, 2, 3], 0), ((0.2, 1.0), [0, 1, 2, 3], 1), ((0.99, 1.0), [0, 1, 2, 3], 3), ((0.5, 0.0), [1], 1),
