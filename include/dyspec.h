@@ -449,7 +449,7 @@ size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_
  *               k, new token j prefix_len[s] + j, or prefix_len[s] + rel_pos[j] (a draft tree passes its depths, as to
  *               dyspec_kv_append; 0 .. N - 1, others count as the nearest).  What keys that no row sees hold does not
  *               matter; their pages may be gone, with any number in the table (up to 63 before a window are read).
- * cap 0 and window 0 (or scores NULL): dyspec_paged_attn.  cap is at most 1e30, scale / cap within 1.2e-38 .. 1e37.
+ * cap 0 and window 0 (or scores NULL): dyspec_paged_attn.  A cap is within 1e-30 .. 1e30, scale / cap within 1.2e-38 .. 1e37.
  * workspace as for dyspec_paged_attn, dyspec_paged_attn_scored_workspace_bytes() bytes.
  */
 typedef struct {

@@ -42,6 +42,19 @@ def test_scores(lib):
         assert call(lib, cap=5.0, window=7, rel=A, **none) == 0                      # no token: nothing is launched
 
 
+def test_the_ends_of_caps(lib):
+    """1e-30 .. 1e30, at scales whose ratio to them is in range."""
+    none = dict(new=(0, 0))
+    for call in (attn, prompt):
+        for cap, scale in ((1e-31, 1e-20), (9.99e-31, 1e-20), (1.001e30, 1.0)):
+            assert call(lib, cap=cap, scale=scale) == BAD_ARG and call(lib, cap=cap, scale=scale, **none) == BAD_ARG, cap
+        for cap, scale in ((1.001e-30, 1e-20), (9.99e29, 1.0)):
+            assert call(lib, cap=cap, scale=scale, **none) == 0, cap
+        # the ratio's ends
+        assert call(lib, cap=1.0, scale=1.3e-38, **none) == 0 and call(lib, cap=1.0, scale=1.1e-38, **none) == BAD_ARG
+        assert call(lib, cap=0.01, scale=9.9e34, **none) == 0 and call(lib, cap=0.01, scale=1.1e35, **none) == BAD_ARG
+
+
 def test_workspaces(lib):
     b = ctypes.byref(binding.Batch.from_sizes((1,), (100000,))._c())
     size = lambda x: lib.dyspec_paged_attn_scored_workspace_bytes(b, 8, 2, 128, binding.BF16, x)
