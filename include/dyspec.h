@@ -444,7 +444,7 @@ size_t dyspec_paged_attn_workspace_bytes(const dyspec_batch* batch, int32_t n_q_
 /*
  * dyspec_paged_attn_scored -- dyspec_paged_attn where scores are capped, keys kept to a window, or both:
  *   cap > 0     a score s = scale * <q, k> counts as cap * tanh(s / cap).  (bf16 with head_dim 64 or 128: on the bf16 matrix cores
- *               up to a cap of 256, where it is within 2^-22 * cap; elsewhere, and beyond, in fp32 throughout)
+ *               up to a cap of 256, where it is within 2^-22 * cap + 2^-23 * |s|; elsewhere, and beyond, in fp32 throughout)
  *   window > 0  a row also sees no key whose position is `window` or more before its own.  Key k of the context has position
  *               k, new token j prefix_len[s] + j, or prefix_len[s] + rel_pos[j] (a draft tree passes its depths, as to
  *               dyspec_kv_append; 0 .. N - 1, others count as the nearest).  What keys that no row sees hold does not

@@ -165,9 +165,10 @@ __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const AttendS
 // ---- capped scores: y = scale <q, k> / cap, cap * tanh(y) = cap * (1 - 2 / (1 + exp(2 y)))
 //
 // Softmax only knows differences of scores, so the bf16 kernels work on -1 / (1 + exp(2 y)), in [-1, 0], with c2 = 2 cap log2(e) and
-// cap_in = 2 log2(e) scale / cap: one multiplication, one exponential, one sum, one reciprocal.  Its error (2^-25, half a step at the end
-// of the range, and about as much of the reciprocal) times 2 cap is 6e-6 at a cap of 50 and 3e-5 at kMostBf16Cap, far below a weight's
-// rounding to bf16 (2^-8 of it); scores small against larger caps would lose more, and go to the fp32 kernel.
+// cap_in = 2 log2(e) scale / cap: one multiplication, one exponential, one sum, one reciprocal.  Where v = 1 / (1 + exp(2 y)), their errors of
+// up to 2^-23, 2^-24 and 2^-24 move it by v (1 - v) 2^-23 + v 2^-24 + 2^-24, the product's by less than 2^-24 |y|: times 2 cap within
+// cap * 2^-22 and 2^-23 of the score itself.  That is 1.2e-5 at a cap of 50 and 6.1e-5 at kMostBf16Cap, far below a weight's rounding to
+// bf16 (2^-8 of it); scores small against larger caps would lose more, and go to the fp32 kernel.
 //
 // That one (Exact) keeps tanh(y) itself, c2 = cap log2(e), cap_in = scale / cap, right to a few 2^-24 of it however small: below 0.55 by an odd
 // polynomial (through Chebyshev's nodes, 4e-9), above as 1 - 2 / (1 + exp(2 y)), which is at least one half there.

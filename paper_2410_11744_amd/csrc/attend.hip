@@ -9,7 +9,8 @@ namespace dyspec {
 // A kernel as the choice sees it: a launch, then items (workgroups).  One that has a CU to itself takes `once` and `step` per
 // `keys` keys, more by the share `alone` over its sequence's row blocks (the first to read a key reads it from memory); of a CU
 // that is full, with `per_cu` items, each takes up `busy_once` and `busy_step`.  Microseconds.  The bf16 kernels' are fitted to
-// measurements, those of the fp32 kernel are estimates, the same for all head sizes above 64.  How far the choice is from the best of
+// measurements, those of the fp32 kernel are estimates, the same for all head sizes above 64.  They are the costs of plain scores, by which
+// capped ones (whose steps take up to a fifth longer) are dealt out as well.  How far the choice is from the best of
 // all kernels, each whole and in 2 to 32 parts (1 to 64 sequences, 1 to 4096 new tokens, 0 to 16384 tokens of context, 1 to 32 KV heads, 1 to
 // 8 query heads each; geometric mean, nine in ten, worst):
 //   bf16, 128   pages (153 shapes) 1.3 %, 7 %, 35 %: 256 tokens over 16384, 8 heads on 1, 47.0 us against 34.8 by attend_short.hip in 4 parts

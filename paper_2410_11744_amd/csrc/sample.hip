@@ -19,9 +19,11 @@
 // A workgroup has one row, held in registers up to 32768 tokens, else read again for every pass; each of its 16 waves has a run of
 // the vocabulary, so that sums over waves, and then over the threads of one run, find a place in the order of the indices.
 //
-// What bounds it: the vector unit of the CU that has the row.  A weight takes 24 instructions, most of 64 bits, a pass over 32000 of them 6 us, one that counts or compares 1 to 2; eleven barriers a draw.  512 rows of 32000 fp32 through top-p: 40.8 us (131 MB, 3.2 TB/s,
-// of the 5.2 that a copy reaches); 2517 rows of bf16 with eight sequences' settings 125 us (vector unit issuing 68 % of the cycles); one token
-// 12.9 us, 64 tokens of mixed settings 18.2.
+// What bounds it: the CU that has the row, and its passes one after the other.  A weight takes 24 instructions, most of 64 bits, a pass over
+// 32000 of them 6 us, one that counts or compares 1 to 2; eleven barriers a draw.  2517 rows of bf16 with eight sequences' settings 125 to 129 us
+// (vector unit issuing 68 % of the cycles).  512 rows of 32000 fp32 through top-p 40.8 us (131 MB, 3.2 TB/s of the 5.2 that a copy reaches; the
+// vector unit 45 %): two rows a CU that start together, so that loads, weights and stores come in turn.  One token 12.9 us, 64 tokens of
+// mixed settings 18.2.  Rows above 32768 tokens are read again for every pass: one row of 131072 fp32 through top-p 64 us, drawn from 109.
 #include "sample.h"
 
 #include "lane_ops.h"
@@ -674,6 +676,8 @@ static hipError_t launch_rows(const SampleHead& head, const int* row0, const Fil
 // threads (512 rows of 32000 through top-p: 46.5 us with 1024 threads, 40.7 with 512), of bf16, held in half the registers, by the
 // ones of 1024 with 64 registers a thread (2517 rows: 151 us with a CU each, 126; 134 with 512 threads).  One row alone is faster
 // with 1024 threads and as many registers as they want (a draw of one token: 12.9 us, 14.7 with 64 registers, 14.6 with 512 threads).
+// Draws have a CU a row however many there are; above 256 rows they would gain as well (32000 tokens through top-p, one and two rows a
+// CU: fp32 300 rows 40.7 and 36.9 us, 754 65.5 and 57.8, 2048 164 and 127; bf16 512 rows 40.2 and 38.9, 2048 154 and 121), which is open.
 constexpr int kCus = 256;
 template <typename T, bool Held, bool Drawn>
 static hipError_t launch_rows(const SampleHead& head, const int* row0, const Filter* filter, hipStream_t stream)
