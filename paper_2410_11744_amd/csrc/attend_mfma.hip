@@ -27,7 +27,7 @@
 //
 // Capped scores (attend.h) take an exponential and a reciprocal more for each, in items of their own two pairs ahead of the exponents; the
 // vector unit is then busy 62 % of the cycles and the matrix cores 35 %; why the two waves of a SIMD overlap no further was not found.
-// Prompts of 5000, 1290, 333 and 1 tokens, 32 heads on 8: 222 to 227 us, with a cap 275, with a window of 2048 164, with both 191 to 210, by
+// Prompts of 5000, 1290, 333 and 1 tokens, 32 heads on 8: 216 to 227 us, with a cap 275, with a window of 2048 164, with both 191 to 210, by
 // the card (148 GFLOP, 700 to 775 TFLOP/s).  An odd polynomial in place of both instructions, where a half's scores are small, is slower (195 ->
 // 204 us).  A tree of 512 rows over 4096 tokens, 64 heads on 8: 80 us, window 2048 50, with a cap 58 to 63.
 #include <atomic>
